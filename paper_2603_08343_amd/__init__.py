@@ -20,3 +20,11 @@ from .binding import (  # noqa: F401
     wht_affine_status_string,
     wht_affine_version,
 )
+from .attention import (  # noqa: F401
+    WhtAttentionError,
+    wht_attention_append,
+    wht_attention_paged,
+    wht_attention_rope_table,
+    wht_attention_status_string,
+    wht_attention_workspace_bytes,
+)

@@ -1,5 +1,6 @@
-"""Compile the HIP library (csrc/wht_affine.hip) for gfx950 into libwht_affine.so, and the tensor calls'
-marshalling (csrc/torch_marshal.cpp) into the extension module _torch_marshal.so, in-tree.
+"""Compile the HIP libraries for gfx950 -- csrc/wht_affine.hip into libwht_affine.so, csrc/wht_attention.hip into
+libwht_attention.so -- and the tensor calls' marshalling (csrc/torch_marshal.cpp) into the extension module
+_torch_marshal.so, in-tree.
 
 hipcc cross-compiles without a GPU; the extension module takes the host compiler and torch's headers.
 Run as `python -m paper_2603_08343_amd.build`.
@@ -30,6 +31,10 @@ MARSHAL_LIB = os.path.join(HERE, "_torch_marshal.so")
 ROUTE_SRC = os.path.join(HERE, "csrc", "route_query.cpp")
 ROUTE_LIB = os.path.join(HERE, "libwht_route.so")
 
+# the paged cache and its attention, in a library of their own
+ATTENTION_SRC = os.path.join(HERE, "csrc", "wht_attention.hip")
+ATTENTION_LIB = os.path.join(HERE, "libwht_attention.so")
+
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # packed float32 VALU forms are kept out of the generated code on the test machines.  The
@@ -41,6 +46,8 @@ HIPCC_FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 HEADER = os.path.join(os.path.dirname(HERE), "include", "wht_affine.h")
+ATTENTION_HEADER = os.path.join(os.path.dirname(HERE), "include", "wht_attention.h")
+ATTENTION_SOURCES = [ATTENTION_SRC, ATTENTION_HEADER, HEADER] + [os.path.join(HERE, "csrc", f) for f in ("attention_device.h", "attention_plan.h")]
 SOURCES = [SRC, HEADER] + [os.path.join(HERE, "csrc", f) for f in ("wht_device.h", "wht_plan.h", "wht_route.h", "wht_validate.h")]
 
 
@@ -49,6 +56,7 @@ def build(verbose: bool = False, extra=()) -> str:
     _compile(SRC, POISON_LIB, verbose, (*extra, "-DWHT_POISON_LDS"))
     _compile_marshal(verbose)
     _compile_route(verbose)
+    _compile(ATTENTION_SRC, ATTENTION_LIB, verbose, extra)
     return _compile(SRC, LIB, verbose, extra)
 
 
@@ -90,13 +98,15 @@ def _compile(src: str, lib: str, verbose: bool, extra=()) -> str:
 def ensure_built(verbose: bool = False) -> str:
     """For harnesses (tests, smoke check, benchmark): compile only if nothing has been built yet.
     The binding itself never builds: a missing library is an error there."""
-    if not all(os.path.exists(lib) for lib in (LIB, COPY_LIB, POISON_LIB, MARSHAL_LIB, ROUTE_LIB)):
+    if not all(os.path.exists(lib) for lib in (LIB, COPY_LIB, POISON_LIB, MARSHAL_LIB, ROUTE_LIB, ATTENTION_LIB)):
         build(verbose=verbose)
     elif any(os.path.getmtime(f) > os.path.getmtime(MARSHAL_LIB) for f in (MARSHAL_SRC, HEADER)):
         raise RuntimeError(f"{MARSHAL_LIB} is older than its source: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > os.path.getmtime(ROUTE_LIB)
              for f in (ROUTE_SRC, os.path.join(HERE, "csrc", "wht_route.h"), os.path.join(HERE, "csrc", "wht_validate.h"), HEADER)):
         raise RuntimeError(f"{ROUTE_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
+    elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_LIB) for f in ATTENTION_SOURCES):
+        raise RuntimeError(f"{ATTENTION_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > min(os.path.getmtime(LIB), os.path.getmtime(POISON_LIB))
              for f in SOURCES if os.path.exists(f)):
         # a stale binary would be validated and recorded under the new sources' name

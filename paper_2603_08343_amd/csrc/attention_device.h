@@ -1,0 +1,907 @@
+// Kernels of the paged cache and its attention (include/wht_attention.h) for gfx950.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "attention_plan.h"
+
+namespace wht {
+
+typedef __bf16 bf16;
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
+constexpr float kLn2 = 0.693147180559945309f;
+#define WHT_NEG_INF (-__builtin_inff())
+
+// ------------------------------------------------------------------------------------------------
+// The batch
+
+struct Batch {
+    const int *table, *lengths, *q_starts;
+    int64_t table_stride;
+    int B, T, most;                     // most: tokens a sequence has at most
+};
+
+struct Sequence { int first, queries, length; };     // first row, new tokens, own tokens
+
+__device__ __forceinline__ Sequence sequence(const Batch& bt, int b) {
+    int lo = b, hi = b + 1;
+    if (bt.q_starts) { lo = bt.q_starts[b]; hi = bt.q_starts[b + 1]; }
+    lo = min(max(lo, 0), bt.T);
+    hi = min(max(hi, lo), bt.T);
+    return {lo, hi - lo, min(max(bt.lengths[b], 0), bt.most)};
+}
+
+// The sequence that row t belongs to, -1 for none: the number of sequences that end at or before t.  A wave looks at 64 evenly
+// spaced ends at a time, so that two dependent loads serve 4096 sequences.
+__device__ __forceinline__ int sequence_of(const Batch& bt, int t) {
+    if (!bt.q_starts) return t < bt.B ? t : -1;
+    int lo = 0, n = bt.B;               // the answer is in [lo, lo + n]
+    while (n > 0) {
+        const int step = (n + 63) >> 6, lane = threadIdx.x & 63, at = (lane + 1) * step - 1;
+        const bool ended = at < n && bt.q_starts[1 + lo + at] <= t;
+        const int whole = __popcll(__ballot(ended));
+        lo += whole * step;
+        n = min(n - whole * step, step - 1);
+    }
+    return lo < bt.B ? lo : -1;
+}
+
+// ------------------------------------------------------------------------------------------------
+// Append: bound by memory, and one token by the latency of its chain (length -> table entry -> store).  A workgroup takes one token, so that what is
+// looked up for it -- sequence, page, angles -- is looked up once; a thread takes the same 16-byte vector pair of every
+// (256 / vectors)-th head, with that pair's cosines and sines in registers over the heads.
+
+struct AppendArgs {
+    Batch batch;
+    const unsigned char *q, *kn, *vn;
+    unsigned char *q_out, *k, *v;
+    int64_t q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, qo_ts, qo_hs;       // bytes
+    int64_t page_stride, head_stride, token_stride;                 // bytes
+    const float* rope;
+    int64_t rope_rows;
+    int q_heads, heads, pages, page_shift, rotary, interleaved, position;
+};
+
+template <class T> struct Vec16 { static constexpr int n = 16 / sizeof(T); T e[n]; };
+
+template <class T>
+__device__ __forceinline__ void load16(float (&f)[16 / sizeof(T)], const unsigned char* p) {
+    const u32x4 raw = *reinterpret_cast<const u32x4*>(p);
+    const Vec16<T> v = __builtin_bit_cast(Vec16<T>, raw);
+#pragma unroll
+    for (int i = 0; i < Vec16<T>::n; ++i) f[i] = (float)v.e[i];
+}
+template <class T>
+__device__ __forceinline__ void store16(unsigned char* p, const float (&f)[16 / sizeof(T)]) {
+    Vec16<T> v;
+#pragma unroll
+    for (int i = 0; i < Vec16<T>::n; ++i) v.e[i] = (T)f[i];
+    *reinterpret_cast<u32x4*>(p) = __builtin_bit_cast(u32x4, v);
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
+    constexpr int N = 16 / sizeof(T), kPairs = D / (2 * N), kHeads = 256 / kPairs;
+    const int t = blockIdx.x, pair = threadIdx.x % kPairs, first = threadIdx.x / kPairs;
+    const int b = sequence_of(a.batch, t);
+    int64_t place = -1, position = -1;
+    if (b >= 0) {
+        const Sequence s = sequence(a.batch, b);
+        const int p = s.length - s.queries + (t - s.first);
+        if (t >= s.first && t < s.first + s.queries) {
+            position = (int64_t)a.position + p;
+            if (p >= 0) {
+                const int page = a.batch.table[b * a.batch.table_stride + (p >> a.page_shift)];
+                if (page >= 0 && page < a.pages) place = page * a.page_stride + (p & ((1 << a.page_shift) - 1)) * a.token_stride;
+            }
+        }
+    }
+    const bool turns = a.rotary > 0, known = !turns || (position >= 0 && position < a.rope_rows);
+    if (!known) place = -1;
+    // where the pair's two vectors stand in a head, and its angles
+    const int half = a.rotary / 2, turned = a.rotary / (2 * N);     // vector pairs that turn
+    const bool turn = known && pair < turned;
+    int e0 = pair * 2 * N, e1 = e0 + N;
+    if (pair < turned && !a.interleaved) { e0 = pair * N; e1 = half + pair * N; }
+    float c[N], s[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) { c[i] = 1.0f; s[i] = 0.0f; }
+    if (turn) {
+        const f32x4* cs = reinterpret_cast<const f32x4*>(a.rope + position * a.rotary + pair * 2 * N);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const f32x4 w = cs[i];
+            c[2 * i] = w[0]; s[2 * i] = w[1]; c[2 * i + 1] = w[2]; s[2 * i + 1] = w[3];
+        }
+    }
+    auto rotate = [&](float (&x)[N], float (&y)[N]) {
+        if (!turn) return;
+        if (a.interleaved) {
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                const float u = x[2 * i], w = x[2 * i + 1], g = y[2 * i], h = y[2 * i + 1];
+                x[2 * i] = u * c[i] - w * s[i];
+                x[2 * i + 1] = w * c[i] + u * s[i];
+                y[2 * i] = g * c[N / 2 + i] - h * s[N / 2 + i];
+                y[2 * i + 1] = h * c[N / 2 + i] + g * s[N / 2 + i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float u = x[i], w = y[i];
+                x[i] = u * c[i] - w * s[i];
+                y[i] = w * c[i] + u * s[i];
+            }
+        }
+    };
+    if (first >= kHeads) return;                                    // 96 wide: 256 is no multiple of the pairs
+    constexpr int kSize = sizeof(T);
+    if (a.q) {
+        for (int h = first; h < a.q_heads; h += kHeads) {
+            unsigned char* to = a.q_out + t * a.qo_ts + h * a.qo_hs;
+            float x[N], y[N];
+            if (b >= 0 && known) {
+                const unsigned char* from = a.q + t * a.q_ts + h * a.q_hs;
+                load16<T>(x, from + e0 * kSize);
+                load16<T>(y, from + e1 * kSize);
+                rotate(x, y);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = y[i] = b >= 0 ? __builtin_nanf("") : 0.0f;
+            }
+            store16<T>(to + e0 * kSize, x);
+            store16<T>(to + e1 * kSize, y);
+        }
+    }
+    if (place < 0) return;
+    for (int h = first; h < a.heads; h += kHeads) {
+        const unsigned char* from = a.kn + t * a.k_ts + h * a.k_hs;
+        const int64_t to = place + h * a.head_stride;
+        float x[N], y[N];
+        load16<T>(x, from + e0 * kSize);
+        load16<T>(y, from + e1 * kSize);
+        const unsigned char* vf = a.vn + t * a.v_ts + h * a.v_hs;
+        const u32x4 v0 = *reinterpret_cast<const u32x4*>(vf + e0 * kSize), v1 = *reinterpret_cast<const u32x4*>(vf + e1 * kSize);
+        rotate(x, y);
+        store16<T>(a.k + to + e0 * kSize, x);
+        store16<T>(a.k + to + e1 * kSize, y);
+        *reinterpret_cast<u32x4*>(a.v + to + e0 * kSize) = v0;
+        *reinterpret_cast<u32x4*>(a.v + to + e1 * kSize) = v1;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Attention.  For one key head, R = up to 32 rows (queries) are the columns of
+//
+//     S^T = K Q^T   [keys x rows]        O^T += V^T P^T   [head_dim x rows],     P = exp2(S scale log2(e) - m)
+//
+// on the 32 x 32 matrix instructions.  The scores of a column then lie in the two lanes r and r + 32, 16 keys each, so that the softmax's
+// maximum is 16 register operations and one exchange, a column's factor is one register, and -- the order of the keys within a
+// product being free -- the weights are the second product's B operand where they stand: no value of S or P changes lanes.
+
+struct AttentionArgs {
+    Batch batch;
+    const unsigned char *q, *k, *v;
+    unsigned char* out;
+    float *lse, *part, *sums;
+    int* cum;
+    const int* prefix_table;
+    int64_t q_ts, q_hs, out_ts, out_hs;             // bytes
+    int64_t head_stride;                            // bytes
+    unsigned page_stride, token_stride;             // bytes
+    int q_heads, heads, G, pages, page_shift, prefix, max_q;
+    int splits, tiles, rows_cap;                    // rows_cap: rows of one slot of partial results
+    int stacked;                                    // rows of all sequences against the prefix alone
+    int use_prefix;                                 // the range begins with the prefix
+    float scale;                                    // scale * log2(e)
+};
+
+template <class T, int D>
+struct Head {
+    static constexpr int kChunks = D * sizeof(T) / 16;              // 16-byte chunks of a row
+    static constexpr int kRowBytes = kChunks * 16;
+    static constexpr int kSteps = kChunks / 2;                      // chunk pairs: lanes below 32 take the even one, the others the odd one
+    static constexpr int kBlocks = D / 32;
+    static constexpr bool kF32 = sizeof(T) == 4;
+
+    // Where chunk c of row r stands in LDS.  K is read a chunk per row over 32 rows: 16 rows' reads have to reach all 16 groups of
+    // four banks.  V is read 64 (bf16: transposing reads, four rows each) or 128 bytes of a row at a time.
+    static __device__ __forceinline__ int k_place(int r, int c) {
+        if constexpr (kChunks == 8) return c ^ ((r >> 1) & 7);
+        else if constexpr (kChunks == 16 || kChunks == 32) return c ^ (r & 15);
+        else { const int p = c + ((r >> (kChunks == 12 ? 2 : 1)) & (kChunks == 12 ? 3 : 7)); return p >= kChunks ? p - kChunks : p; }
+    }
+    static __device__ __forceinline__ int k_chunk(int r, int p) {
+        if constexpr (kChunks == 12 || kChunks == 24) { const int c = p - ((r >> (kChunks == 12 ? 2 : 1)) & (kChunks == 12 ? 3 : 7)); return c < 0 ? c + kChunks : c; }
+        else return k_place(r, p);
+    }
+    static __device__ __forceinline__ int v_place(int r, int c) {
+        if constexpr (!kF32) {
+            if constexpr (kChunks == 16) return c ^ ((r & 3) << 2);
+            else if constexpr (kChunks == 8) return c ^ (((r >> 1) & 1) << 2);
+            else return c;
+        } else {
+            if constexpr (kChunks == 24) { const int p = c + 8 * ((r >> 2) & 1); return p >= 24 ? p - 24 : p; }
+            else return c ^ (((r >> 2) & 1) << 3);
+        }
+    }
+    static __device__ __forceinline__ int v_chunk(int r, int p) {
+        if constexpr (kF32 && kChunks == 24) { const int c = p - 8 * ((r >> 2) & 1); return c < 0 ? c + 24 : c; }
+        else return v_place(r, p);
+    }
+};
+
+// What a lane of a row (column of the products) keeps: the row's maximum so far (scaled, base 2), this lane's share of the sum,
+// and its half of the row's outputs.
+template <class H>
+struct RowState {
+    float m, l;
+    f32x16 o[H::kBlocks];
+    __device__ __forceinline__ void clear() {
+        m = WHT_NEG_INF;
+        l = 0.0f;
+#pragma unroll
+        for (int d = 0; d < H::kBlocks; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    }
+};
+
+__device__ __forceinline__ float other_half(float x) {
+    return __shfl_xor(x, 32);
+}
+
+__device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
+
+// 16 bytes per lane from memory to LDS at base + 16 * lane, past the registers.  Assembly, because the compiler would otherwise wait for
+// every such load in flight before any read of LDS; which have landed is known where wait_loads stands.  Reads of what is overwritten
+// have returned (lgkmcnt).
+__device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned to) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(to) : "memory");
+}
+template <int PENDING> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PENDING) : "memory"); }
+__device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void workgroup_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Loaded in place of keys that are not there.
+static __device__ __align__(16) unsigned char zero_chunk[16];
+
+// S^T of 32 keys (rows `row` = lane % 32 of the LDS block) and the wave's rows.
+template <class T, int D>
+__device__ __forceinline__ f32x16 scores(const unsigned char* kbuf, const u32x4 (&q)[Head<T, D>::kSteps]) {
+    using H = Head<T, D>;
+    const int lane = threadIdx.x & 63, row = lane & 31, h = lane >> 5;
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < H::kSteps; ++c) {
+        const u32x4 k = *reinterpret_cast<const u32x4*>(kbuf + row * H::kRowBytes + H::k_place(row, 2 * c + h) * 16);
+        if constexpr (!H::kF32) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[c]), s, 0, 0, 0);
+        } else {
+            const f32x4 kf = __builtin_bit_cast(f32x4, k), qf = __builtin_bit_cast(f32x4, q[c]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[i], qf[i], s, 0, 0, 0);
+        }
+    }
+    return s;
+}
+
+// Key, of 32, whose score a lane's register i holds.
+__device__ __forceinline__ int key_of(int i) { return (i >> 2) * 8 + ((threadIdx.x >> 5) & 1) * 4 + (i & 3); }
+
+// Running maximum and sum over NS blocks of scores, which become weights.
+template <class H, int NS>
+__device__ __forceinline__ void weigh(f32x16 (&s)[NS], float scale, RowState<H>& st) {
+    float mx = s[0][0];
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
+    mx = fmaxf(mx, other_half(mx));
+    const float now = fmaxf(st.m, mx * scale);
+    const float base = now == WHT_NEG_INF ? 0.0f : now;             // nothing seen yet: weights of zero
+    if (__any(now > st.m)) {
+        const float f = __builtin_amdgcn_exp2f(st.m - base);
+        st.l *= f;
+#pragma unroll
+        for (int d = 0; d < H::kBlocks; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st.o[d][i] *= f;
+        st.m = now;
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], scale, -base));
+            sum += s[n][i];
+        }
+    st.l += sum;
+}
+
+// Values that are not finite, as zeros.
+__device__ __forceinline__ bf16x8 finite(bf16x8 v, bool& found) {
+    u32x4 x = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool lo = (x[i] & 0x7f80u) == 0x7f80u, hi = (x[i] & 0x7f800000u) == 0x7f800000u;
+        found |= lo | hi;
+        x[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+    }
+    return __builtin_bit_cast(bf16x8, x);
+}
+__device__ __forceinline__ float finite(float v, bool& found) {
+    const bool odd = !(fabsf(v) < __builtin_inff());
+    found |= odd;
+    return odd ? 0.0f : v;
+}
+
+// o += (V^T P^T) over 32 keys, for the 32 columns of V from 32 d on.
+template <class T, int D, bool GUARD>
+__device__ __forceinline__ void block_product(const unsigned char* vbuf, int d, const f32x16& p, f32x16& o, bool& found) {
+    using H = Head<T, D>;
+    const int lane = threadIdx.x & 63;
+    if constexpr (!H::kF32) {
+        // a transposing read gives lane i of 16 the i-th of 16 columns, four rows of it, that the 16 lanes address as 4 x 4 pieces of 8 bytes
+        const int g = lane >> 4, in = lane & 15, row = (g >> 1) * 4 + (in >> 2);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            bf16x8 v, w;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = (bf16)p[ks * 8 + i];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = ks * 16 + e * 8 + row;
+                const unsigned char* at = vbuf + r * H::kRowBytes + H::v_place(r, d * 4 + (g & 1) * 2 + ((in & 3) >> 1)) * 16 + (in & 1) * 8;
+                const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)lds_address(at));
+                const bf16x4 y = __builtin_bit_cast(bf16x4, x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[e * 4 + i] = y[i];
+            }
+            if constexpr (GUARD) v = finite(v, found);
+            o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, o, 0, 0, 0);
+        }
+    } else {
+        const int col = lane & 31;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = key_of(i);
+            float v = *reinterpret_cast<const float*>(vbuf + r * H::kRowBytes + H::v_place(r, d * 8 + (col >> 2)) * 16 + (col & 3) * 4);
+            if constexpr (GUARD) v = finite(v, found);
+            o = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], o, 0, 0, 0);
+        }
+    }
+}
+
+// The first of 32 keys whose value in a column is +infinity or NaN (above), -infinity or NaN (below); 32 where there is none.
+template <int D> struct FirstOdd { int above[D], below[D]; };
+
+template <class T, int D>
+__device__ __forceinline__ void add_odd(const unsigned char* vbuf, int seen, FirstOdd<D>& first, RowState<Head<T, D>>& st) {
+    using H = Head<T, D>;
+    const int lane = threadIdx.x & 63;
+    for (int c = lane; c < D; c += 64) {
+        int above = 32, below = 32;
+#pragma unroll 1
+        for (int k = 31; k >= 0; --k) {
+            const float v = (float)*reinterpret_cast<const T*>(vbuf + k * H::kRowBytes + H::v_place(k, c * (int)sizeof(T) / 16) * 16 + c * (int)sizeof(T) % 16);
+            if (!(fabsf(v) < __builtin_inff())) {
+                if (v != WHT_NEG_INF) above = k;
+                if (v != -WHT_NEG_INF) below = k;
+            }
+        }
+        first.above[c] = above;
+        first.below[c] = below;
+    }
+    reads_done();                                                   // the wave's own writes: no other wave looks at `first`
+#pragma unroll
+    for (int d = 0; d < H::kBlocks; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int c = d * 32 + key_of(i);
+            st.o[d][i] += (first.above[c] < seen ? -WHT_NEG_INF : 0.0f) + (first.below[c] < seen ? WHT_NEG_INF : 0.0f);
+            if ((i & 3) == 3) asm volatile("" ::: "memory");        // rare: its registers count, its time does not
+        }
+    reads_done();
+}
+
+// O^T += V^T P^T over 32 keys.  A key that a row does not see has a weight of zero, and zero times infinity would still be NaN: where rows of
+// the tile see different keys (GUARD; a row sees the first `seen` of the 32), values that are not finite stay out of the product, and the
+// rows that see one get it by itself.
+template <class T, int D, bool GUARD>
+__device__ __forceinline__ void accumulate(const unsigned char* vbuf, const f32x16& p, int seen, FirstOdd<D>& first, RowState<Head<T, D>>& st) {
+    bool found = false;
+#pragma unroll
+    for (int d = 0; d < Head<T, D>::kBlocks; ++d) block_product<T, D, GUARD>(vbuf, d, p, st.o[d], found);
+    if constexpr (GUARD)
+        if (__any(found)) add_odd<T, D>(vbuf, seen, first, st);
+}
+
+// A row of q, as the B operand of the first product; zeros where there is no row.
+template <class T, int D>
+__device__ __forceinline__ void load_row(const unsigned char* p, bool there, u32x4 (&q)[Head<T, D>::kSteps]) {
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int c = 0; c < Head<T, D>::kSteps; ++c) {
+        if (there) q[c] = *reinterpret_cast<const u32x4*>(p + (2 * c + h) * 16);
+        else q[c] = u32x4{0, 0, 0, 0};
+    }
+}
+
+// The pages of up to kListed * page_size keys at a time, in LDS; -1 where a number names no page.
+constexpr int kListed = 512;
+struct PageList { int page[kListed + 4]; int bad; };
+
+__device__ __forceinline__ void list_pages(PageList& list, const int* table, int first, int count, int pages) {
+    __syncthreads();                                                // the last use of the list is over
+    if (threadIdx.x == 0) list.bad = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < count; i += 256) {
+        const int page = table[first + i];
+        const bool good = page >= 0 && page < pages;
+        list.page[i] = good ? page : -1;
+        if (!good) list.bad = 1;
+    }
+    __syncthreads();
+}
+
+// Where key `key` of a table's tokens stands relative to the cache's start; -1 where it is not there.
+__device__ __forceinline__ int64_t key_offset(const AttentionArgs& a, const PageList& list, int first, int key, int keys) {
+    if (key >= keys) return -1;
+    const int page = list.page[(key >> a.page_shift) - first];
+    if (page < 0) return -1;
+    return (int64_t)((uint64_t)(unsigned)page * a.page_stride + (unsigned)(key & ((1 << a.page_shift) - 1)) * a.token_stride);
+}
+
+__device__ __forceinline__ void hide(f32x16& s, int key0, int limit, const AttentionArgs& a, const PageList& list, int first) {
+    const bool bad = list.bad != 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int key = key0 + key_of(i);
+        bool seen = key < limit;
+        if (bad && seen) seen = list.page[(key >> a.page_shift) - first] >= 0;
+        s[i] = seen ? s[i] : WHT_NEG_INF;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Few rows (decoding): memory-bound.  The four waves of a workgroup hold the same rows and take 32 of every 128 keys each, through
+// LDS slots of their own, so that no barrier stands in the loop; V of a block is in flight while its scores are formed, K of
+// the next one while V is used.  All (sequence, head) items' units of 128 keys form one line that the workgroups of the grid share evenly,
+// whatever the sequences' lengths: a workgroup's share begins and ends anywhere in an item.  Every piece of an item leaves a slot of
+// partial results, numbered item + workgroup (each step along the line raises one of the two), which join_kernel puts together.
+
+template <class T, int D, bool MULTI>
+struct FewRange {
+    using H = Head<T, D>;
+    static constexpr int kLoads = H::kChunks / 2;                   // of one wave for 32 rows
+
+    static __device__ __forceinline__ void addresses(int64_t (&off)[kLoads], const AttentionArgs& a, const PageList& list, int first, int key0, int keys) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) off[i] = key_offset(a, list, first, key0 + (i * 64 + lane) / H::kChunks, keys);
+    }
+    template <bool V>
+    static __device__ __forceinline__ void issue(const int64_t (&off)[kLoads], const unsigned char* base, unsigned to) {
+        const int lane = threadIdx.x & 63;
+        reads_done();
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = (i * 64 + lane) / H::kChunks, p = (i * 64 + lane) % H::kChunks;
+            const int c = V ? H::v_chunk(r, p) : H::k_chunk(r, p);
+            load_to_lds(off[i] >= 0 ? base + off[i] + c * 16 : zero_chunk, to + i * 1024);
+        }
+    }
+
+    // units [u0, u1) of `table`'s `keys` tokens; limit: how many of them this lane's row sees, all_see: how many every row sees
+    static __device__ __forceinline__ void run(const AttentionArgs& a, PageList& list, const int* table, int u0, int u1, int keys, int limit, int all_see,
+                                               const unsigned char* kbase, const unsigned char* vbase, const unsigned char* buf,
+                                               const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd, RowState<H>& st) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const unsigned char *kbuf = buf, *vbuf = buf + 32 * H::kRowBytes;
+        const unsigned kto = __builtin_amdgcn_readfirstlane(lds_address(kbuf)), vto = __builtin_amdgcn_readfirstlane(lds_address(vbuf));
+        const int per_list = (kListed << a.page_shift) / kUnitKeys;
+        for (int lo = u0; lo < u1; lo += per_list) {
+            const int hi = min(u1, lo + per_list), end = min(hi * kUnitKeys, keys), first = (lo * kUnitKeys) >> a.page_shift;
+            list_pages(list, table + first, 0, ((end - 1) >> a.page_shift) - first + 1, a.pages);
+            const bool bad = __builtin_amdgcn_readfirstlane(list.bad) != 0;
+            int key0 = lo * kUnitKeys + wave * 32;
+            if (key0 >= end) continue;
+            int64_t off[kLoads];
+            addresses(off, a, list, first, key0, keys);
+            issue<false>(off, kbase, kto);
+            issue<true>(off, vbase, vto);
+            while (true) {
+                const int next = key0 + kUnitKeys;
+                const bool more = next < end;
+                wait_loads<kLoads>();
+                f32x16 s[1] = {scores<T, D>(kbuf, q)};
+                if (more) {
+                    addresses(off, a, list, first, next, keys);
+                    issue<false>(off, kbase, kto);
+                }
+                if (bad || key0 + 32 > all_see) hide(s[0], key0, limit, a, list, first);
+                weigh<H, 1>(s, a.scale, st);
+                if (more) wait_loads<kLoads>();
+                else wait_loads<0>();
+                accumulate<T, D, MULTI>(vbuf, s[0], limit - key0, odd, st);
+                if (!more) break;
+                issue<true>(off, vbase, vto);
+                key0 = next;
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ int item_units(const AttentionArgs& a, int b) {
+    const int front = a.use_prefix ? ceil_div(a.prefix, kUnitKeys) : 0;
+    if (a.stacked) return front;
+    const Sequence s = sequence(a.batch, b);
+    return s.queries > 0 ? front + ceil_div(s.length, kUnitKeys) : 0;
+}
+
+template <class T, int D, bool MULTI>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel(AttentionArgs a) {
+    using H = Head<T, D>;
+    constexpr int kWaveBytes = 2 * 32 * H::kRowBytes;
+    static_assert(kWaveBytes >= 32 * D * 4, "a wave's outputs are handed over where its keys stood");
+    __shared__ __align__(16) unsigned char buf[4 * kWaveBytes];
+    __shared__ PageList list;
+    __shared__ FirstOdd<D> odd[4];
+    __shared__ float sums[4][32][2];
+    __shared__ int scan[4], found[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int B = a.stacked ? 1 : a.batch.B;
+
+    // each thread's run of sequences, the runs' prefix sums, and the sequence in which this workgroup's share begins
+    const int run = ceil_div(B, 256), b0 = min(B, tid * run), b1 = min(B, b0 + run);
+    int mine = 0;
+    for (int b = b0; b < b1; ++b) mine += item_units(a, b);
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(upto, o);
+        if (lane >= o) upto += x;
+    }
+    if (lane == 63) scan[wave] = upto;
+    __syncthreads();
+    int before = upto - mine, all = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) { if (w < wave) before += scan[w]; all += scan[w]; }
+    if (blockIdx.x == 0 && !a.stacked) {
+        int c = before;
+        for (int b = b0; b < b1; ++b) { a.cum[b] = c; c += item_units(a, b); }
+        if (tid == 255) a.cum[B] = all;
+    }
+    const int total = all * a.heads, per = line_share(total, (int)gridDim.x);
+    int u = blockIdx.x * per;
+    const int end = min(total, u + per);
+    if (u >= end) return;
+    if (mine > 0 && u >= before * a.heads && u < (before + mine) * a.heads) {
+        int b = b0, c = before;
+        for (int n; u >= (c + (n = item_units(a, b))) * a.heads; ++b) c += n;
+        found[0] = b;
+        found[1] = c;
+    }
+    __syncthreads();
+    int b = __builtin_amdgcn_readfirstlane(found[0]), cum = __builtin_amdgcn_readfirstlane(found[1]);
+
+    while (u < end) {
+        const int n = item_units(a, b);
+        if (u >= (cum + n) * a.heads) { cum += n; ++b; continue; }
+        const int within = u - cum * a.heads, head = within / n, u0 = within - head * n, u1 = min(n, u0 + (end - u));
+        const Sequence s = a.stacked ? Sequence{0, a.batch.T, 0} : sequence(a.batch, b);
+        const int rows = min(s.queries * a.G, a.rows_cap), row = lane & 31;
+        const int token = row / a.G, qh = head * a.G + row % a.G;
+        u32x4 q[H::kSteps];
+        load_row<T, D>(a.q + (s.first + token) * a.q_ts + qh * a.q_hs, row < rows, q);
+        RowState<H> st;
+        st.clear();
+        const unsigned char *kbase = a.k + head * a.head_stride, *vbase = a.v + head * a.head_stride;
+        const int front = a.use_prefix ? ceil_div(a.prefix, kUnitKeys) : 0;
+        if (u0 < front) FewRange<T, D, MULTI>::run(a, list, a.prefix_table, u0, min(u1, front), a.prefix, a.prefix, a.prefix, kbase, vbase, buf + wave * kWaveBytes, q, odd[wave], st);
+        if (u1 > front && !a.stacked) {
+            const int limit = min(max(s.length - s.queries + token + 1, 0), s.length), all_see = min(max(s.length - s.queries + 1, 0), s.length);
+            const int keys = min(max(s.length - s.queries + min(s.queries, a.max_q), 0), s.length);       // what the last of the rows sees
+            FewRange<T, D, MULTI>::run(a, list, a.batch.table + b * a.batch.table_stride, max(u0 - front, 0), u1 - front, keys, limit, all_see, kbase, vbase,
+                                buf + wave * kWaveBytes, q, odd[wave], st);
+        }
+        // the four waves' results of the piece, together
+        st.l += other_half(st.l);
+        if (lane < 32) { sums[wave][row][0] = st.m; sums[wave][row][1] = st.l; }
+        __syncthreads();
+        float m = WHT_NEG_INF, l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m = fmaxf(m, sums[w][row][0]);
+        const float base = m == WHT_NEG_INF ? 0.0f : m, f = __builtin_amdgcn_exp2f(st.m - base);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) l += sums[w][row][1] * __builtin_amdgcn_exp2f(sums[w][row][0] - base);
+        float* own = reinterpret_cast<float*>(buf + wave * kWaveBytes);
+        if (row < rows) {
+#pragma unroll
+            for (int d = 0; d < H::kBlocks; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f32x4 x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = st.o[d][4 * i + e] * f;
+                    *reinterpret_cast<f32x4*>(own + row * D + d * 32 + i * 8 + (lane >> 5) * 4) = x;
+                }
+        }
+        const int64_t slot = (int64_t)((a.stacked ? 0 : b) * a.heads + head + blockIdx.x) * a.rows_cap;
+        if (wave == 0 && lane < rows) {
+            a.sums[(slot + lane) * 2] = m;
+            a.sums[(slot + lane) * 2 + 1] = l;
+        }
+        __syncthreads();
+        for (int i = tid; i < rows * (D / 4); i += 256) {
+            f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x += *reinterpret_cast<const f32x4*>(buf + w * kWaveBytes + i * 16);
+            *reinterpret_cast<f32x4*>(a.part + slot * D + i * 4) = x;
+        }
+        __syncthreads();
+        u += u1 - u0;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Many rows: a workgroup takes 128 rows, 32 per wave, and all its waves the same 64 keys a step, which lie in LDS twice over: the next step's
+// are in flight during the products.
+
+template <class T, int D>
+struct ManyRange {
+    using H = Head<T, D>;
+    static constexpr int kLoads = H::kChunks / 4;                   // of one wave for a quarter of 64 rows
+    static constexpr int kTileBytes = kStepKeys * H::kRowBytes;
+
+    static __device__ __forceinline__ void issue(const AttentionArgs& a, const PageList& list, int first, int key0, int keys, const unsigned char* kbase,
+                                                 const unsigned char* vbase, unsigned kto, unsigned vto) {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int n = (wave * kLoads + i) * 64 + lane, r = n / H::kChunks, p = n % H::kChunks;
+            const int64_t off = key_offset(a, list, first, key0 + r, keys);
+            load_to_lds(off >= 0 ? kbase + off + H::k_chunk(r, p) * 16 : zero_chunk, kto + (wave * kLoads + i) * 1024);
+            load_to_lds(off >= 0 ? vbase + off + H::v_chunk(r, p) * 16 : zero_chunk, vto + (wave * kLoads + i) * 1024);
+        }
+    }
+
+    // steps [t0, t1) of `table`'s `keys` tokens; limit: how many this lane's row sees; all_see, any_sees: every, any row of the wave
+    static __device__ __forceinline__ void run(const AttentionArgs& a, PageList& list, const int* table, int t0, int t1, int keys, int limit, int all_see, int any_sees,
+                                               const unsigned char* kbase, const unsigned char* vbase, const unsigned char* buf,
+                                               const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd, RowState<H>& st) {
+        const unsigned at = __builtin_amdgcn_readfirstlane(lds_address(buf));
+        const int per_list = (kListed << a.page_shift) / kStepKeys;
+        for (int lo = t0; lo < t1; lo += per_list) {
+            const int hi = min(t1, lo + per_list), end = min(hi * kStepKeys, keys), first = (lo * kStepKeys) >> a.page_shift;
+            list_pages(list, table + first, 0, ((end - 1) >> a.page_shift) - first + 1, a.pages);
+            const bool bad = __builtin_amdgcn_readfirstlane(list.bad) != 0;
+            issue(a, list, first, lo * kStepKeys, keys, kbase, vbase, at, at + kTileBytes);
+            for (int t = lo; t < hi; ++t) {
+                const int key0 = t * kStepKeys, side = (t - lo) & 1;
+                wait_loads<0>();
+                workgroup_barrier();                                // everyone's loads of this step have landed, everyone's reads of the last are done
+                const unsigned other = at + (side ^ 1) * 2 * kTileBytes;
+                if (t + 1 < hi) issue(a, list, first, key0 + kStepKeys, keys, kbase, vbase, other, other + kTileBytes);
+                if (key0 < any_sees) {
+                    const unsigned char* kbuf = buf + side * 2 * kTileBytes;
+                    f32x16 s[2] = {scores<T, D>(kbuf, q), scores<T, D>(kbuf + 32 * H::kRowBytes, q)};
+                    if (bad || key0 + kStepKeys > all_see) {
+                        hide(s[0], key0, limit, a, list, first);
+                        hide(s[1], key0 + 32, limit, a, list, first);
+                    }
+                    weigh<H, 2>(s, a.scale, st);
+                    const unsigned char* vbuf = kbuf + kTileBytes;
+                    if (all_see < min(key0 + kStepKeys, keys)) {
+                        accumulate<T, D, true>(vbuf, s[0], limit - key0, odd, st);
+                        accumulate<T, D, true>(vbuf + 32 * H::kRowBytes, s[1], limit - key0 - 32, odd, st);
+                    } else {
+                        accumulate<T, D, false>(vbuf, s[0], 0, odd, st);
+                        accumulate<T, D, false>(vbuf + 32 * H::kRowBytes, s[1], 0, odd, st);
+                    }
+                }
+            }
+        }
+    }
+};
+
+template <class T>
+__device__ __forceinline__ void store4(unsigned char* p, f32x4 x) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = x;
+    else {
+        bf16x4 y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = (bf16)x[i];
+        *reinterpret_cast<bf16x4*>(p) = y;
+    }
+}
+
+// Rows that no tile covers: padding (zeros) and tokens from the max_q-th of their sequence on (NaN).
+constexpr int kFillGroups = 8;
+template <class T, int D>
+__device__ __forceinline__ void fill_rows(const AttentionArgs& a, int group) {
+    auto fill = [&](int lo, int hi, float value, float lse) {
+        const int64_t n = (int64_t)(hi - lo) * a.q_heads * (D / 4);
+        for (int64_t i = threadIdx.x; i < n; i += 256) {
+            const int64_t row = i / (D / 4);
+            const int64_t t = lo + row / a.q_heads, h = row % a.q_heads;
+            store4<T>(a.out + t * a.out_ts + h * a.out_hs + (i % (D / 4)) * 4 * sizeof(T), f32x4{value, value, value, value});
+            if (a.lse && i % (D / 4) == 0) a.lse[t * a.q_heads + h] = lse;
+        }
+    };
+    for (int b = group; b < a.batch.B; b += kFillGroups) {
+        const Sequence s = sequence(a.batch, b);
+        if (s.queries > a.max_q) fill(s.first + a.max_q, s.first + s.queries, __builtin_nanf(""), __builtin_nanf(""));
+    }
+    const int last = min(max(a.batch.q_starts ? a.batch.q_starts[a.batch.B] : a.batch.B, 0), a.batch.T);
+    const int left = a.batch.T - last;
+    fill(last + (int)((int64_t)left * group / kFillGroups), last + (int)((int64_t)left * (group + 1) / kFillGroups), 0.0f, WHT_NEG_INF);
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void many_rows_kernel(AttentionArgs a) {
+    using H = Head<T, D>;
+    using R = ManyRange<T, D>;
+    __shared__ __align__(16) unsigned char buf[4 * R::kTileBytes];
+    __shared__ PageList list;
+    __shared__ FirstOdd<D> odd[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int B = a.stacked ? 1 : a.batch.B;
+    // Workgroups go to the 8 dies in turn: a die takes whole groups (a sequence's head and share of its keys), so that their keys are in its L2
+    // once, tile after tile, the tiles that see most first.
+    const int groups = B * a.heads * a.splits, x = blockIdx.x & 7, y = blockIdx.x >> 3;
+    const int group = x + 8 * (y / a.tiles), tile = a.tiles - 1 - y % a.tiles;
+    if (group >= groups) {
+        // the grid's last workgroups, one per die
+        if (!a.stacked && a.splits == 1 && y / a.tiles == ceil_div(groups, 8)) fill_rows<T, D>(a, x);
+        return;
+    }
+    const int split = group % a.splits, head = group / a.splits % a.heads, b = group / a.splits / a.heads;
+    const Sequence s = a.stacked ? Sequence{0, a.batch.T, 0} : sequence(a.batch, b);
+    const int queries = a.stacked ? s.queries : min(s.queries, a.max_q);
+    const int64_t rows = (int64_t)queries * a.G;
+    if ((int64_t)tile * kTileRows >= rows) return;
+    const int row0 = tile * kTileRows + wave * 32, row = row0 + (lane & 31);
+    const int token = row / a.G, qh = head * a.G + row % a.G;
+    const bool there = row < rows;
+    u32x4 q[H::kSteps];
+    load_row<T, D>(a.q + (s.first + (there ? token : 0)) * a.q_ts + qh * a.q_hs, there, q);
+    // own tokens that row r of the tile sees: length - queries + its token + 1
+    auto sees = [&](int64_t r) { return a.stacked ? 0 : min(max(s.length - s.queries + (int)(min(r, rows - 1) / a.G) + 1, 0), s.length); };
+    const int keys = sees(tile * kTileRows + kTileRows - 1);
+    const int limit = sees(row), all_see = sees(row0), any_sees = row0 < rows ? sees(row0 + 31) : 0;
+    const int front = a.use_prefix ? ceil_div(a.prefix, kStepKeys) : 0;
+    const int total = front + ceil_div(keys, kStepKeys), per = ceil_div(total, a.splits);
+    const int t0 = min(total, split * per), t1 = min(total, t0 + per);
+    RowState<H> st;
+    st.clear();
+    const unsigned char *kbase = a.k + head * a.head_stride, *vbase = a.v + head * a.head_stride;
+    if (t0 < min(t1, front)) R::run(a, list, a.prefix_table, t0, min(t1, front), a.prefix, a.prefix, a.prefix, row0 < rows ? a.prefix : 0, kbase, vbase, buf, q, odd[wave], st);
+    if (max(t0, front) < t1)
+        R::run(a, list, a.batch.table + b * a.batch.table_stride, max(t0 - front, 0), t1 - front, keys, limit, all_see, any_sees, kbase, vbase, buf, q, odd[wave], st);
+    if (!there) return;
+    st.l += other_half(st.l);
+    const int64_t t = s.first + token;
+    if (a.splits > 1 || a.stacked) {
+        const int64_t at = ((int64_t)split * a.batch.T + t) * a.q_heads + qh;
+        if (lane < 32) { a.sums[at * 2] = st.m; a.sums[at * 2 + 1] = st.l; }
+#pragma unroll
+        for (int d = 0; d < H::kBlocks; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4*>(a.part + at * D + d * 32 + i * 8 + (lane >> 5) * 4) = f32x4{st.o[d][4 * i], st.o[d][4 * i + 1], st.o[d][4 * i + 2], st.o[d][4 * i + 3]};
+    } else {
+        const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
+        if (a.lse && lane < 32) a.lse[t * a.q_heads + qh] = st.l == 0.0f ? WHT_NEG_INF : (st.m + __builtin_amdgcn_logf(st.l)) * kLn2;
+#pragma unroll
+        for (int d = 0; d < H::kBlocks; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store4<T>(a.out + t * a.out_ts + qh * a.out_hs + (d * 32 + i * 8 + (lane >> 5) * 4) * sizeof(T),
+                          f32x4{st.o[d][4 * i] * inv, st.o[d][4 * i + 1] * inv, st.o[d][4 * i + 2] * inv, st.o[d][4 * i + 3] * inv});
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Joins the partial results of a row: out = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p.  A wave per row.
+
+struct JoinArgs {
+    Batch batch;
+    unsigned char* out;
+    float* lse;
+    const float *front_part, *front_sums, *own_part, *own_sums;
+    const int* cum;
+    int64_t out_ts, out_hs;
+    int q_heads, heads, G, max_q, prefix, grid;         // grid: workgroups of the few-rows kernels
+    int front, front_few, front_splits;                 // front: there is one
+    int own_few, own_splits, own_cap, own_prefix;       // own_prefix: the own range begins with the prefix
+};
+
+struct Parts { const float *part, *sums; int64_t at, step; int n; };        // rows at, at + step, ...
+
+// The pieces of an item that covers units [u0, u0 + n) of a line of `total`.
+__device__ __forceinline__ Parts slots(const float* part, const float* sums, int item, int u0, int n, int total, int grid, int cap, int row) {
+    const Slots p = item_slots(item, u0, n, total, grid);
+    return {part, sums, p.first * cap + row, cap, p.count};
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= (int64_t)a.batch.T * a.q_heads) return;
+    const int t = (int)(r / a.q_heads), qh = (int)(r % a.q_heads), head = qh / a.G, g = qh % a.G;
+    const int b = __builtin_amdgcn_readfirstlane(sequence_of(a.batch, t));
+    float value = 0.0f, m = WHT_NEG_INF, l = 0.0f;
+    f32x2 o = {0.0f, 0.0f};
+    if (b >= 0) {
+        const Sequence s = sequence(a.batch, b);
+        const int j = t - s.first;
+        if (j < 0 || j >= s.queries || j >= a.max_q) value = l = __builtin_nanf("");
+        else {
+            Parts parts[2] = {{nullptr, nullptr, 0, 0, 0}, {nullptr, nullptr, 0, 0, 0}};
+            if (a.front) {
+                const int units = ceil_div(a.prefix, kUnitKeys);
+                if (a.front_few) parts[0] = slots(a.front_part, a.front_sums, head, head * units, units, a.heads * units, a.grid, a.batch.T * a.G, t * a.G + g);
+                else parts[0] = {a.front_part, a.front_sums, r, (int64_t)a.batch.T * a.q_heads, a.front_splits};
+            }
+            if (a.own_few) {
+                const int units = (a.own_prefix ? ceil_div(a.prefix, kUnitKeys) : 0) + ceil_div(s.length, kUnitKeys);
+                parts[1] = slots(a.own_part, a.own_sums, b * a.heads + head, a.cum[b] * a.heads + head * units, units, a.cum[a.batch.B] * a.heads, a.grid, a.own_cap, j * a.G + g);
+            } else parts[1] = {a.own_part, a.own_sums, r, (int64_t)a.batch.T * a.q_heads, a.own_splits};
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const Parts& p = parts[k];
+                for (int lo = 0; lo < p.n; lo += 64) {
+                    const int n = min(64, p.n - lo);
+                    float pm = WHT_NEG_INF, pl = 0.0f;
+                    if (lane < n) {
+                        pm = p.sums[(p.at + (lo + lane) * p.step) * 2];
+                        pl = p.sums[(p.at + (lo + lane) * p.step) * 2 + 1];
+                    }
+                    float most = pm;
+#pragma unroll
+                    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+                    const float now = fmaxf(m, most), base = now == WHT_NEG_INF ? 0.0f : now;
+                    const float f = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(pm - base);
+                    float sum = pl * w;
+#pragma unroll
+                    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+                    l = l * f + sum;
+                    o *= f;
+                    m = now;
+                    for (int i = 0; i < n; ++i) {
+                        const float wi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), i));
+                        if (lane < D / 2) o += wi * *reinterpret_cast<const f32x2*>(p.part + (p.at + (lo + i) * p.step) * D + 2 * lane);
+                    }
+                }
+            }
+        }
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (lane < D / 2) {
+        unsigned char* to = a.out + t * a.out_ts + qh * a.out_hs + 2 * lane * sizeof(T);
+        const f32x2 x = o * inv + value;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x2*>(to) = x;
+        else *reinterpret_cast<bf16x2*>(to) = bf16x2{(bf16)x[0], (bf16)x[1]};
+    }
+    if (a.lse && lane == 0) a.lse[r] = l == 0.0f ? WHT_NEG_INF : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+}  // namespace wht

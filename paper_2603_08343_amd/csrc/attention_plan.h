@@ -1,0 +1,153 @@
+// How an attention call's work is cut and where its partial results lie (include/wht_attention.h): plain arithmetic on sizes, which
+// the host decides a call by and the kernels look their share up with.  Compiles without HIP.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/wht_attention.h"
+
+#if defined(__HIPCC__)
+#define WHT_HD __host__ __device__ __forceinline__
+#else
+#define WHT_HD inline
+#endif
+
+namespace wht {
+
+WHT_HD int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+WHT_HD int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+// A row is one query of one head.  Rows that read the same keys -- G = q_heads / heads query heads, all new tokens of the
+// sequence -- are taken together as the columns of one matrix product with the keys.
+constexpr int kFewRows = 32;        // few-rows kernel: one tile of rows, the waves share the keys out
+constexpr int kTileRows = 128;      // many-rows kernel: 32 rows per wave, all waves take the same keys
+constexpr int kUnitKeys = 128;      // keys of one step of a workgroup in the few-rows kernel: 32 per wave
+constexpr int kStepKeys = 64;       // the same in the many-rows kernel
+constexpr int kWorkgroups = 512;    // two per compute unit
+
+enum class Range { Own, Prefix, Both };
+
+// What one call launches.  `front`: the rows of all sequences against the prefix; `own`: each sequence's rows against its own
+// keys -- or, where there is no front, against prefix and own keys as one range.
+struct AttentionPlan {
+    bool front, front_few, own_few;
+    int front_splits, own_splits;           // many-rows kernel: workgroups that share a tile's keys
+    bool combine;
+    size_t front_rows, own_rows;            // rows of partial results
+    size_t front_at, own_at, front_sums_at, own_sums_at, cum_at, bytes;     // byte offsets in the workspace
+};
+
+inline int splits_for(int64_t tiles, int64_t keys) {
+    // enough workgroups for every compute unit, at least 256 keys each
+    int64_t s = tiles > 0 ? kWorkgroups / tiles : 1;
+    const int64_t most = ceil_div64(keys, 256);
+    if (s > most) s = most;
+    return s < 1 ? 1 : (int)s;
+}
+
+inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t head_dim, int32_t max_q,
+                                    int64_t max_length, int64_t prefix) {
+    AttentionPlan p{};
+    const int64_t G = q_heads / heads;
+    p.own_few = max_q * G <= kFewRows;
+    // Several sequences of few rows each: their rows together read the prefix once.  Where a sequence's own rows fill
+    // tiles by themselves nothing is saved by that, and prefix and own keys are one range.
+    p.front = prefix > 0 && B > 1 && p.own_few;
+    p.front_few = T * G <= kFewRows;
+    p.front_splits = p.own_splits = 1;
+    if (p.front) {
+        if (p.front_few) p.front_rows = (size_t)(heads + kWorkgroups) * (size_t)(T * G);
+        else {
+            p.front_splits = splits_for(ceil_div64(T * G, kTileRows) * heads, prefix);
+            p.front_rows = (size_t)p.front_splits * (size_t)(T * q_heads);
+        }
+    }
+    if (p.own_few) p.own_rows = ((size_t)B * heads + kWorkgroups) * (size_t)(max_q * G);
+    else {
+        p.own_splits = splits_for(ceil_div64((int64_t)max_q * G, kTileRows) * heads * B, max_length + prefix);
+        if (p.own_splits > 1) p.own_rows = (size_t)p.own_splits * (size_t)(T * q_heads);
+    }
+    p.combine = p.front || p.own_few || p.own_splits > 1;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
+    p.front_at = take(p.front_rows * head_dim * 4);
+    p.own_at = take(p.own_rows * head_dim * 4);
+    p.front_sums_at = take(p.front_rows * 8);
+    p.own_sums_at = take(p.own_rows * 8);
+    p.cum_at = take(p.own_few ? ((size_t)B + 1) * 4 : 0);
+    p.bytes = at;
+    return p;
+}
+
+// The few-rows kernel's line: the units of all items one after the other, `per` of them to a workgroup.  The pieces of an item of n
+// units from u0 on lie in the slots item + w of the workgroups w that it meets: first .. first + count - 1.
+struct Slots { int64_t first; int count; };
+WHT_HD int line_share(int total, int workgroups) { return ceil_div(total, workgroups); }
+WHT_HD Slots item_slots(int item, int u0, int n, int total, int workgroups) {
+    if (n == 0) return {0, 0};
+    const int per = line_share(total, workgroups), w0 = u0 / per, w1 = (u0 + n - 1) / per;
+    return {(int64_t)item + w0, w1 - w0 + 1};
+}
+
+// Argument checks, in the order of the status codes.
+inline bool good_rows(const wht_attention_rows_t* r, int heads, int head_dim, int size) {
+    return ((uintptr_t)r->data & 15u) == 0 && r->token_stride * size % 16 == 0 && r->head_stride * size % 16 == 0 && r->token_stride >= 0 &&
+           (r->head_stride >= head_dim || heads == 1) && r->head_stride >= 0 && r->head_stride * size < (int64_t)1 << 31;
+}
+
+inline int check_cache(const wht_attention_cache_t* c, const wht_attention_batch_t* b, int32_t dtype) {
+    if (!c || !b || !c->k || !c->v || !b->table || !b->lengths) return WHT_ERR_NULL_PTR;
+    if (dtype != WHT_DTYPE_F32 && dtype != WHT_DTYPE_BF16) return WHT_ERR_BAD_DTYPE;
+    const int size = dtype == WHT_DTYPE_F32 ? 4 : 2;
+    if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return WHT_ERR_BAD_DIM;
+    if (c->page_size < WHT_ATTENTION_MIN_PAGE || c->page_size > WHT_ATTENTION_MAX_PAGE || (c->page_size & (c->page_size - 1)) != 0) return WHT_ERR_BAD_DIM;
+    if (c->heads < 1 || c->heads > 1024 || c->pages < 1 || b->B < 0 || b->width < 1 || b->table_stride < 0) return WHT_ERR_BAD_DIM;
+    if ((int64_t)b->width * c->page_size > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
+    // the kernels multiply a page's number by its stride in bytes (both 32 bits) and keep a row's place in its page in 31
+    if (c->page_stride < 0 || c->page_stride * size >= (int64_t)1 << 32 || c->token_stride < c->head_dim ||
+        (c->page_size - 1) * c->token_stride * size >= (int64_t)1 << 31 || c->head_stride < 0) return WHT_ERR_BAD_DIM;
+    if (((uintptr_t)c->k & 15u) != 0 || ((uintptr_t)c->v & 15u) != 0 || c->page_stride * size % 16 != 0 || c->head_stride * size % 16 != 0 ||
+        c->token_stride * size % 16 != 0) return WHT_ERR_MISALIGNED;
+    if (((uintptr_t)b->table & 3u) != 0 || ((uintptr_t)b->lengths & 3u) != 0 || ((uintptr_t)b->q_starts & 3u) != 0) return WHT_ERR_MISALIGNED;
+    return WHT_OK;
+}
+
+inline int check_append(const wht_attention_rows_t* q, const wht_attention_rows_t* k, const wht_attention_rows_t* v,
+                        const wht_attention_rows_t* q_out, int64_t T, int32_t q_heads, const wht_attention_cache_t* c,
+                        const wht_attention_batch_t* b, const float* rope, int64_t rope_rows, int32_t rotary, int64_t position,
+                        int32_t dtype) {
+    if (!q || !k || !v || !q_out || !k->data || !v->data || (q->data && !q_out->data) || (rotary != 0 && !rope)) return WHT_ERR_NULL_PTR;
+    if (int rc = check_cache(c, b, dtype)) return rc;
+    const int size = dtype == WHT_DTYPE_F32 ? 4 : 2;
+    if (T < 0 || T > (int64_t)1 << 30 || (q->data && (q_heads < 1 || q_heads > 1024))) return WHT_ERR_BAD_DIM;
+    if (rotary < 0 || rotary % 16 != 0 || rotary > c->head_dim || rope_rows < 0 || rope_rows > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
+    if (position < 0 || position > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
+    if (!good_rows(k, c->heads, c->head_dim, size) || !good_rows(v, c->heads, c->head_dim, size) || ((uintptr_t)rope & 15u) != 0) return WHT_ERR_MISALIGNED;
+    if (q->data && (!good_rows(q, q_heads, c->head_dim, size) || !good_rows(q_out, q_heads, c->head_dim, size))) return WHT_ERR_MISALIGNED;
+    return WHT_OK;
+}
+
+inline int check_sizes(int64_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t head_dim, int32_t max_q, int64_t max_length,
+                       int64_t prefix, int32_t dtype) {
+    if (dtype != WHT_DTYPE_F32 && dtype != WHT_DTYPE_BF16) return WHT_ERR_BAD_DTYPE;
+    if (head_dim != 64 && head_dim != 96 && head_dim != 128) return WHT_ERR_BAD_DIM;
+    if (T < 0 || B < 0 || B > 1 << 20 || heads < 1 || heads > 1024 || q_heads < 1 || q_heads > 1024 || q_heads % heads != 0) return WHT_ERR_BAD_DIM;
+    if (T * q_heads > (int64_t)1 << 30 || max_q < 1 || (int64_t)max_q * (q_heads / heads) > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
+    if (prefix < 0 || prefix > (int64_t)1 << 30 || max_length < 0 || max_length > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
+    return WHT_OK;
+}
+
+inline int check_paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out, const float* lse, int64_t T, int32_t q_heads,
+                       const wht_attention_cache_t* c, const wht_attention_batch_t* b, const int32_t* prefix_table, int64_t prefix,
+                       int32_t max_q, int64_t max_length, float scale, int32_t dtype) {
+    if (!q || !out || !q->data || !out->data || (prefix > 0 && !prefix_table)) return WHT_ERR_NULL_PTR;
+    if (int rc = check_cache(c, b, dtype)) return rc;
+    if (int rc = check_sizes(T, b->B, q_heads, c->heads, c->head_dim, max_q, max_length, prefix, dtype)) return rc;
+    if (!(scale > 0.0f) || !(scale <= 3.0e38f)) return WHT_ERR_BAD_DIM;
+    const int size = dtype == WHT_DTYPE_F32 ? 4 : 2;
+    if (!good_rows(q, q_heads, c->head_dim, size) || !good_rows(out, q_heads, c->head_dim, size)) return WHT_ERR_MISALIGNED;
+    if (((uintptr_t)lse & 3u) != 0 || ((uintptr_t)prefix_table & 3u) != 0) return WHT_ERR_MISALIGNED;
+    return WHT_OK;
+}
+
+}  // namespace wht

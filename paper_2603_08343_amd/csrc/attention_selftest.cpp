@@ -1,0 +1,151 @@
+// CPU check of the arithmetic that attention calls are cut by (attention_plan.h): the few-rows kernel's line of units, its slots and
+// what join looks up, over batches of all kinds; the workspace's parts; and every status of the argument checks.  Runs under the
+// sanitizers (tests/test_attention_host.py).
+#include <stdio.h>
+#include <stdlib.h>
+
+#include <map>
+#include <random>
+#include <set>
+#include <vector>
+
+#include "attention_plan.h"
+
+using namespace wht;
+
+#define CHECK(c) do { if (!(c)) { printf("FAILED %s:%d: %s\n", __FILE__, __LINE__, #c); exit(1); } } while (0)
+
+// Walks the line as the workgroups do, and compares what each item leaves with what item_slots says.
+static void walk(const std::vector<int>& lengths, int heads, int front) {
+    const int B = (int)lengths.size(), W = kWorkgroups;
+    std::vector<int> units(B), cum(B + 1, 0);
+    for (int b = 0; b < B; ++b) {
+        units[b] = ceil_div(front, kUnitKeys) + ceil_div(lengths[b], kUnitKeys);
+        cum[b + 1] = cum[b] + units[b];
+    }
+    const int total = cum[B] * heads, per = line_share(total, W);
+    std::map<int, std::vector<int64_t>> of;             // item -> slots, in order
+    std::set<int64_t> used;
+    int covered = 0;
+    for (int w = 0; w < W; ++w) {
+        int u = w * per, end = total < u + per ? total : u + per, b = 0;
+        while (u < end) {
+            if (u >= cum[b + 1] * heads) { ++b; continue; }
+            const int n = units[b], within = u - cum[b] * heads, head = within / n, u0 = within - head * n;
+            const int u1 = n < u0 + (end - u) ? n : u0 + (end - u);
+            const int64_t slot = (int64_t)b * heads + head + w;
+            CHECK(used.insert(slot).second);
+            CHECK(slot >= 0 && slot < (int64_t)B * heads + W);
+            of[b * heads + head].push_back(slot);
+            covered += u1 - u0;
+            u += u1 - u0;
+        }
+    }
+    CHECK(covered == total);
+    for (int b = 0; b < B; ++b)
+        for (int h = 0; h < heads; ++h) {
+            const Slots s = item_slots(b * heads + h, cum[b] * heads + h * units[b], units[b], total, W);
+            const auto& got = of[b * heads + h];
+            CHECK(s.count == (int)got.size());
+            for (int i = 0; i < s.count; ++i) CHECK(got[i] == s.first + i);
+        }
+}
+
+static void plans() {
+    std::mt19937 rng(7);
+    auto upto = [&](int n) { return (int)(rng() % (unsigned)n); };
+    for (int i = 0; i < 20000; ++i) {
+        const int heads = 1 + upto(32), G = 1 + upto(16), B = upto(300), dim = 64 + 32 * upto(3), max_q = i % 2 ? 1 : 1 + upto(5000);
+        const int64_t T = 1 + upto(9000), prefix = i % 3 ? upto(40000) : 0, most = upto(100000);
+        const AttentionPlan p = plan_attention(T, B, heads * G, heads, dim, max_q, most, prefix);
+        CHECK(p.own_few == (max_q * G <= kFewRows));
+        CHECK(p.front_splits >= 1 && p.own_splits >= 1 && p.front_splits <= kWorkgroups && p.own_splits <= kWorkgroups);
+        if (p.own_few) CHECK(p.own_rows >= ((size_t)B * heads + kWorkgroups) * (size_t)(max_q * G));
+        if (p.front && !p.front_few) CHECK(p.front_rows == (size_t)p.front_splits * (size_t)T * (size_t)(heads * G));
+        if (!p.combine) CHECK(!p.front && !p.own_few && p.own_rows == 0);
+        const size_t at[] = {p.front_at, p.own_at, p.front_sums_at, p.own_sums_at, p.cum_at, p.bytes};
+        const size_t need[] = {p.front_rows * dim * 4, p.own_rows * dim * 4, p.front_rows * 8, p.own_rows * 8, p.own_few ? ((size_t)B + 1) * 4 : 0};
+        for (int k = 0; k < 5; ++k) CHECK(at[k] % 256 == 0 && at[k] + need[k] <= at[k + 1]);
+    }
+}
+
+static void statuses() {
+    void* P = reinterpret_cast<void*>((uintptr_t)0x1000);
+    const int32_t* I = static_cast<const int32_t*>(P);
+    const wht_attention_cache_t c0{P, P, 8 * 64 * 128, 64 * 128, 128, 10, 8, 64, 128};
+    const wht_attention_batch_t b0{I, I, nullptr, 4, 3, 4};
+    const wht_attention_rows_t r0{P, 48 * 128, 128}, none{nullptr, 0, 0};
+    const float* F = static_cast<const float*>(P);
+    auto append = [&](wht_attention_cache_t c, wht_attention_batch_t b, wht_attention_rows_t q, wht_attention_rows_t k, const float* rope, int64_t rope_rows,
+                      int32_t rotary, int64_t position, int32_t dtype, int64_t T = 3, int32_t q_heads = 32) {
+        return check_append(&q, &k, &k, &q, T, q_heads, &c, &b, rope, rope_rows, rotary, position, dtype);
+    };
+    auto cache = [&](auto f) { wht_attention_cache_t c = c0; f(c); return append(c, b0, r0, r0, F, 100, 128, 0, 1); };
+    auto batch = [&](auto f) { wht_attention_batch_t b = b0; f(b); return append(c0, b, r0, r0, F, 100, 128, 0, 1); };
+    auto rows = [&](auto f) { wht_attention_rows_t r = r0; f(r); return append(c0, b0, r0, r, F, 100, 128, 0, 1); };
+    CHECK(append(c0, b0, r0, r0, F, 100, 128, 0, 1) == WHT_OK);
+    CHECK(append(c0, b0, none, r0, F, 100, 64, 0, 1) == WHT_OK);                 // no queries
+    CHECK(append(c0, b0, r0, r0, nullptr, 0, 0, 0, 1) == WHT_OK);                // no rotation
+    CHECK(append(c0, b0, r0, none, F, 100, 128, 0, 1) == WHT_ERR_NULL_PTR);
+    CHECK(append(c0, b0, r0, r0, nullptr, 100, 128, 0, 1) == WHT_ERR_NULL_PTR);
+    CHECK(append(c0, b0, r0, r0, F, 100, 128, 0, 2) == WHT_ERR_BAD_DTYPE);
+    CHECK(append(c0, b0, r0, r0, F, 100, 136, 0, 1) == WHT_ERR_BAD_DIM);
+    CHECK(append(c0, b0, r0, r0, F, 100, 24, 0, 1) == WHT_ERR_BAD_DIM);
+    CHECK(append(c0, b0, r0, r0, F, 100, -16, 0, 1) == WHT_ERR_BAD_DIM);
+    CHECK(append(c0, b0, r0, r0, F, -1, 128, 0, 1) == WHT_ERR_BAD_DIM);
+    CHECK(append(c0, b0, r0, r0, F, 100, 128, -1, 1) == WHT_ERR_BAD_DIM);
+    CHECK(append(c0, b0, r0, r0, F, 100, 128, 0, 1, -1) == WHT_ERR_BAD_DIM);
+    CHECK(append(c0, b0, r0, r0, F, 100, 128, 0, 1, 3, 0) == WHT_ERR_BAD_DIM);
+    CHECK(cache([](auto& c) { c.k = nullptr; }) == WHT_ERR_NULL_PTR);
+    CHECK(cache([](auto& c) { c.head_dim = 80; }) == WHT_ERR_BAD_DIM);
+    CHECK(cache([](auto& c) { c.page_size = 48; }) == WHT_ERR_BAD_DIM);
+    CHECK(cache([](auto& c) { c.page_size = 4; }) == WHT_ERR_BAD_DIM);
+    CHECK(cache([](auto& c) { c.page_size = 2048; }) == WHT_ERR_BAD_DIM);
+    CHECK(cache([](auto& c) { c.heads = 0; }) == WHT_ERR_BAD_DIM);
+    CHECK(cache([](auto& c) { c.pages = 0; }) == WHT_ERR_BAD_DIM);
+    CHECK(cache([](auto& c) { c.token_stride = 64; }) == WHT_ERR_BAD_DIM);       // tokens over one another
+    CHECK(cache([](auto& c) { c.page_stride = (int64_t)1 << 31; }) == WHT_ERR_BAD_DIM);
+    CHECK(cache([](auto& c) { c.token_stride = (int64_t)1 << 25; }) == WHT_ERR_BAD_DIM);
+    CHECK(cache([](auto& c) { c.token_stride = 132; }) == WHT_ERR_MISALIGNED);
+    CHECK(cache([](auto& c) { c.v = reinterpret_cast<void*>((uintptr_t)0x1008); }) == WHT_ERR_MISALIGNED);
+    CHECK(batch([](auto& b) { b.table = nullptr; }) == WHT_ERR_NULL_PTR);
+    CHECK(batch([](auto& b) { b.lengths = nullptr; }) == WHT_ERR_NULL_PTR);
+    CHECK(batch([](auto& b) { b.width = 0; }) == WHT_ERR_BAD_DIM);
+    CHECK(batch([](auto& b) { b.B = -1; }) == WHT_ERR_BAD_DIM);
+    CHECK(batch([](auto& b) { b.width = 1 << 25; }) == WHT_ERR_BAD_DIM);
+    CHECK(batch([](auto& b) { b.q_starts = reinterpret_cast<const int32_t*>((uintptr_t)0x1002); }) == WHT_ERR_MISALIGNED);
+    CHECK(rows([](auto& r) { r.token_stride = 48 * 128 + 4; }) == WHT_ERR_MISALIGNED);
+    CHECK(rows([](auto& r) { r.head_stride = 64; }) == WHT_ERR_MISALIGNED);
+    CHECK(rows([](auto& r) { r.data = reinterpret_cast<void*>((uintptr_t)0x1004); }) == WHT_ERR_MISALIGNED);
+
+    auto paged = [&](wht_attention_rows_t q, int32_t q_heads, const int32_t* prefix_table, int64_t prefix, int32_t max_q, int64_t most, float scale, int32_t dtype) {
+        return check_paged(&q, &q, nullptr, 3, q_heads, &c0, &b0, prefix_table, prefix, max_q, most, scale, dtype);
+    };
+    CHECK(paged(r0, 32, nullptr, 0, 1, 256, 1.0f, 1) == WHT_OK);
+    CHECK(paged(r0, 32, I, 100, 7, 0, 1e-3f, 1) == WHT_OK);
+    CHECK(paged(none, 32, I, 100, 1, 256, 1.0f, 1) == WHT_ERR_NULL_PTR);
+    CHECK(paged(r0, 32, nullptr, 100, 1, 256, 1.0f, 1) == WHT_ERR_NULL_PTR);
+    CHECK(paged(r0, 32, I, 100, 1, 256, 1.0f, 3) == WHT_ERR_BAD_DTYPE);
+    CHECK(paged(r0, 20, I, 100, 1, 256, 1.0f, 1) == WHT_ERR_BAD_DIM);            // heads do not divide
+    CHECK(paged(r0, 32, I, -1, 1, 256, 1.0f, 1) == WHT_ERR_BAD_DIM);
+    CHECK(paged(r0, 32, I, 100, 0, 256, 1.0f, 1) == WHT_ERR_BAD_DIM);
+    CHECK(paged(r0, 32, I, 100, 1, -1, 1.0f, 1) == WHT_ERR_BAD_DIM);
+    for (float s : {0.0f, -1.0f, __builtin_nanf(""), __builtin_inff()}) CHECK(paged(r0, 32, I, 100, 1, 256, s, 1) == WHT_ERR_BAD_DIM);
+}
+
+int main() {
+    std::mt19937 rng(3);
+    for (int i = 0; i < 300; ++i) {
+        std::vector<int> lengths(rng() % 200);
+        const int most = 1 << (rng() % 16);
+        for (int& n : lengths) n = (int)(rng() % (unsigned)most) * (rng() % 5 != 0);
+        walk(lengths, 1 + (int)(rng() % 40), i % 3 ? 0 : (int)(rng() % 5000));
+    }
+    walk({}, 8, 0);
+    walk({0, 0}, 8, 0);
+    walk({1}, 1, 0);
+    plans();
+    statuses();
+    printf("attention_selftest: ok\n");
+    return 0;
+}
