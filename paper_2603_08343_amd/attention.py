@@ -2,11 +2,14 @@
 attention whose concatenated head outputs the Walsh-Hadamard output layer takes.
 
 Argument marshalling only, as in `binding`: torch supplies device memory and the stream, every step runs in the HIP kernels; wrong
-arguments raise TypeError or ValueError, a status of the library WhtAttentionError.
+arguments raise TypeError or ValueError, a status of the library WhtAttentionError.  A call on the current stream first goes to the
+extension module _attention_marshal (csrc/attention_marshal.cpp), which does the same in native code and hands back None for
+anything but a plain valid call; the code here then decides, and words the errors.
 """
 import ctypes
 import math
 import os
+import warnings
 
 from .binding import DTYPE_BF16, DTYPE_F32, _DeviceGuard, _stream_handle, _torch
 
@@ -135,6 +138,14 @@ def _batch(table, lengths, q_starts, T, device, torch):
     return Batch(at, lengths.data_ptr() or at, None if q_starts is None else q_starts.data_ptr(), table.stride(0), B, width)
 
 
+def _empty(shape, dtype, device, stream, torch):
+    """Memory for a call on `stream`, of that stream's own: what the current stream last freed may still be in use there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 _dummies = {}
 
 
@@ -142,6 +153,38 @@ def device_dummy(torch, device):
     if device not in _dummies:
         _dummies[device] = torch.zeros(64, dtype=torch.int32, device=device)
     return _dummies[device].data_ptr()
+
+
+_native_module = None
+
+
+class _NoNative:
+    """Stands in for the extension module where it cannot be used: declines every call."""
+    append = paged = staticmethod(lambda *args: None)
+
+
+def _load_native(torch, lib):
+    current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    try:
+        from . import _attention_marshal
+        built_for = getattr(_attention_marshal, "torch_version", "unknown")
+        if current_stream is None or built_for != str(torch.__version__):
+            raise ImportError(f"built for torch {built_for}, this is {torch.__version__}")
+    except ImportError as e:
+        warnings.warn(f"the extension module _attention_marshal cannot be used ({e}): tensor calls take about 10 us longer "
+                      "each; build it with `python -m paper_2603_08343_amd.build`", RuntimeWarning, stacklevel=4)
+        return _NoNative
+    names = ("wht_attention_append", "wht_attention_workspace_bytes", "wht_attention_paged")
+    _attention_marshal.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names), current_stream)
+    return _attention_marshal
+
+
+def _native():
+    """The extension module, loaded and told the library's addresses on the first tensor call."""
+    global _native_module
+    if _native_module is None:
+        _native_module = _load_native(_torch(), library())
+    return _native_module
 
 
 def wht_attention_append(q, k, v, k_pages, v_pages, table, lengths, rope, q_starts=None, position=0, interleaved=False, q_out=None,
@@ -153,6 +196,12 @@ def wht_attention_append(q, k, v, k_pages, v_pages, table, lengths, rope, q_star
       table int32 [B, width], lengths int32 [B] (the new tokens included), q_starts int32 [B + 1] (None: a token each)
       rope [positions, rotary / 2, 2] float32 (wht_attention_rope_table) or None; position: of a sequence's first own token
     """
+    if stream is None:
+        done = _native().append(q, k, v, k_pages, v_pages, table, lengths, rope, q_starts, position, interleaved, q_out)
+        if done is not None:
+            if type(done) is int:
+                raise WhtAttentionError(done, "wht_attention_append")
+            return None if q is None else done
     torch = _torch()
     cache = _cache(k_pages, v_pages)
     code = _code(k_pages, torch)
@@ -166,7 +215,7 @@ def wht_attention_append(q, k, v, k_pages, v_pages, table, lengths, rope, q_star
         if q.shape[0] != T:
             raise ValueError("q and k must have the same number of rows")
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = _empty(q.shape, q.dtype, q.device, stream, torch)
         outr = _rows(q_out, "q_out", k_pages, q_heads)
         if q_out.shape[0] != T:
             raise ValueError("q_out and q must have the same number of rows")
@@ -198,6 +247,13 @@ def wht_attention_paged(q, k_pages, v_pages, table, lengths, q_starts=None, pref
       max_length: at least the largest of lengths (None: what the table can hold); goes into how the work is split
       scale: None for 1 / sqrt(head_dim)
     """
+    if stream is None:
+        done = _native().paged(q, k_pages, v_pages, table, lengths, q_starts, prefix_table, prefix_length, max_q, max_length, scale, out, lse,
+                               want_lse, workspace)
+        if done is not None:
+            if type(done) is int:
+                raise WhtAttentionError(done, "wht_attention_paged")
+            return done
     torch = _torch()
     cache = _cache(k_pages, v_pages)
     code = _code(k_pages, torch)
@@ -205,7 +261,7 @@ def wht_attention_paged(q, k_pages, v_pages, table, lengths, q_starts=None, pref
     T, q_heads, head_dim = q.shape
     batch = _batch(table, lengths, q_starts, T, k_pages.device, torch)
     if out is None:
-        out = torch.empty((T, q_heads, head_dim), dtype=q.dtype, device=q.device)
+        out = _empty((T, q_heads, head_dim), q.dtype, q.device, stream, torch)
     outr = _rows(out, "out", k_pages, q_heads)
     if out.shape[0] != T:
         raise ValueError("out and q must have the same number of rows")
@@ -213,7 +269,7 @@ def wht_attention_paged(q, k_pages, v_pages, table, lengths, q_starts=None, pref
         if not lse.is_cuda or lse.dtype != torch.float32 or lse.shape != (T, q_heads) or not lse.is_contiguous() or lse.device != q.device:
             raise ValueError("lse must be a contiguous float32 [T, q_heads] tensor on q's device")
     elif want_lse:
-        lse = torch.empty((T, q_heads), dtype=torch.float32, device=q.device)
+        lse = _empty((T, q_heads), torch.float32, q.device, stream, torch)
     prefix_length = int(prefix_length)
     if prefix_length > 0:
         need = -(-prefix_length // k_pages.shape[2])
@@ -229,7 +285,7 @@ def wht_attention_paged(q, k_pages, v_pages, table, lengths, q_starts=None, pref
     if T > 0:
         need = wht_attention_workspace_bytes(T, table.shape[0], q_heads, k_pages.shape[1], head_dim, max_q, max_length, prefix_length, code)
         if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+            workspace = _empty(need, torch.uint8, q.device, stream, torch) if need else None
         elif not workspace.is_cuda or not workspace.is_contiguous() or workspace.device != q.device:
             raise ValueError("workspace must be a contiguous GPU tensor on q's device")
         with _DeviceGuard(torch, q.device):

@@ -1,8 +1,8 @@
 """Compile the HIP libraries for gfx950 -- csrc/wht_affine.hip into libwht_affine.so, csrc/wht_attention.hip into
-libwht_attention.so -- and the tensor calls' marshalling (csrc/torch_marshal.cpp) into the extension module
-_torch_marshal.so, in-tree.
+libwht_attention.so -- and the tensor calls' marshalling (csrc/torch_marshal.cpp, csrc/attention_marshal.cpp)
+into the extension modules _torch_marshal.so and _attention_marshal.so, in-tree.
 
-hipcc cross-compiles without a GPU; the extension module takes the host compiler and torch's headers.
+hipcc cross-compiles without a GPU; the extension modules take the host compiler and torch's headers.
 Run as `python -m paper_2603_08343_amd.build`.
 """
 import importlib.metadata
@@ -34,6 +34,8 @@ ROUTE_LIB = os.path.join(HERE, "libwht_route.so")
 # the paged cache and its attention, in a library of their own
 ATTENTION_SRC = os.path.join(HERE, "csrc", "wht_attention.hip")
 ATTENTION_LIB = os.path.join(HERE, "libwht_attention.so")
+ATTENTION_MARSHAL_SRC = os.path.join(HERE, "csrc", "attention_marshal.cpp")
+ATTENTION_MARSHAL_LIB = os.path.join(HERE, "_attention_marshal.so")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -54,20 +56,21 @@ SOURCES = [SRC, HEADER] + [os.path.join(HERE, "csrc", f) for f in ("wht_device.h
 def build(verbose: bool = False, extra=()) -> str:
     _compile(COPY_SRC, COPY_LIB, verbose, extra)
     _compile(SRC, POISON_LIB, verbose, (*extra, "-DWHT_POISON_LDS"))
-    _compile_marshal(verbose)
+    _compile_marshal(MARSHAL_SRC, MARSHAL_LIB, verbose)
+    _compile_marshal(ATTENTION_MARSHAL_SRC, ATTENTION_MARSHAL_LIB, verbose)
     _compile_route(verbose)
     _compile(ATTENTION_SRC, ATTENTION_LIB, verbose, extra)
     return _compile(SRC, LIB, verbose, extra)
 
 
-def _compile_marshal(verbose: bool) -> None:
+def _compile_marshal(src: str, lib: str, verbose: bool) -> None:
     torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)
     lib_dir = os.path.join(torch_dir, "lib")
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
            "-isystem", os.path.join(torch_dir, "include"),
            "-isystem", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
            f'-DWHT_TORCH_VERSION="{importlib.metadata.version("torch")}"',
-           "-o", MARSHAL_LIB, MARSHAL_SRC, "-L" + lib_dir, "-ltorch_python", "-ltorch_hip", "-ltorch_cpu", "-lc10"]
+           "-o", lib, src, "-L" + lib_dir, "-ltorch_python", "-ltorch_hip", "-ltorch_cpu", "-lc10"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
@@ -98,13 +101,15 @@ def _compile(src: str, lib: str, verbose: bool, extra=()) -> str:
 def ensure_built(verbose: bool = False) -> str:
     """For harnesses (tests, smoke check, benchmark): compile only if nothing has been built yet.
     The binding itself never builds: a missing library is an error there."""
-    if not all(os.path.exists(lib) for lib in (LIB, COPY_LIB, POISON_LIB, MARSHAL_LIB, ROUTE_LIB, ATTENTION_LIB)):
+    if not all(os.path.exists(lib) for lib in (LIB, COPY_LIB, POISON_LIB, MARSHAL_LIB, ROUTE_LIB, ATTENTION_LIB, ATTENTION_MARSHAL_LIB)):
         build(verbose=verbose)
     elif any(os.path.getmtime(f) > os.path.getmtime(MARSHAL_LIB) for f in (MARSHAL_SRC, HEADER)):
         raise RuntimeError(f"{MARSHAL_LIB} is older than its source: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > os.path.getmtime(ROUTE_LIB)
              for f in (ROUTE_SRC, os.path.join(HERE, "csrc", "wht_route.h"), os.path.join(HERE, "csrc", "wht_validate.h"), HEADER)):
         raise RuntimeError(f"{ROUTE_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
+    elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_MARSHAL_LIB) for f in (ATTENTION_MARSHAL_SRC, ATTENTION_HEADER, HEADER)):
+        raise RuntimeError(f"{ATTENTION_MARSHAL_LIB} is older than its source: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_LIB) for f in ATTENTION_SOURCES):
         raise RuntimeError(f"{ATTENTION_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > min(os.path.getmtime(LIB), os.path.getmtime(POISON_LIB))

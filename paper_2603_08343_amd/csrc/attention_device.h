@@ -480,21 +480,35 @@ __device__ __forceinline__ void hide(f32x16& s, int key0, int limit, const Atten
 }
 
 // ------------------------------------------------------------------------------------------------
-// Few rows (decoding): memory-bound.  The four waves of a workgroup hold the same rows and take 32 of every 128 keys each, through
-// LDS slots of their own, so that no barrier stands in the loop; V of a block is in flight while its scores are formed, K of
-// the next one while V is used.  All (sequence, head) items' units of 128 keys form one line that the workgroups of the grid share evenly,
-// whatever the sequences' lengths: a workgroup's share begins and ends anywhere in an item.  Every piece of an item leaves a slot of
-// partial results, numbered item + workgroup (each step along the line raises one of the two), which join_kernel puts together.
+// Few rows (decoding): memory-bound.  Every wave works by itself, through LDS slots of its own, without a barrier: V of a block of 32 keys is in flight
+// while its scores are formed, K of the next one while V is used.  All (sequence, head) items' blocks form one line that the grid's
+// waves share evenly, whatever the sequences' lengths: a wave's share begins and ends anywhere in an item.  Every piece of an item leaves a
+// slot of partial results, numbered item + worker (each step along the line raises one of the two), which join_kernel puts together.
 
 template <class T, int D, bool MULTI>
 struct FewRange {
     using H = Head<T, D>;
     static constexpr int kLoads = H::kChunks / 2;                   // of one wave for 32 rows
 
-    static __device__ __forceinline__ void addresses(int64_t (&off)[kLoads], const AttentionArgs& a, const PageList& list, int first, int key0, int keys) {
+    // Where a lane's 16 bytes of each load come from, relative to the cache's start; -1 where there is no key.  `page`: lane i holds the number of the
+    // page first + i of the table (-1: none).
+    static __device__ __forceinline__ void addresses(int64_t (&off)[kLoads], const AttentionArgs& a, int page, int first, int key0, int end) {
         const int lane = threadIdx.x & 63;
+        if (a.page_shift >= 5) {                                    // the 32 keys are in one page
+            const int at = __builtin_amdgcn_readlane(page, (key0 >> a.page_shift) - first);
+            const uint64_t base = (uint64_t)(unsigned)at * a.page_stride + (unsigned)(key0 & ((1 << a.page_shift) - 1)) * a.token_stride;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) off[i] = key_offset(a, list, first, key0 + (i * 64 + lane) / H::kChunks, keys);
+            for (int i = 0; i < kLoads; ++i) {
+                const int r = (i * 64 + lane) / H::kChunks;
+                off[i] = at >= 0 && key0 + r < end ? (int64_t)(base + (unsigned)r * a.token_stride) : -1;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int key = key0 + (i * 64 + lane) / H::kChunks, at = __shfl(page, (key >> a.page_shift) - first);
+                off[i] = at >= 0 && key < end ? (int64_t)((uint64_t)(unsigned)at * a.page_stride + (unsigned)(key & ((1 << a.page_shift) - 1)) * a.token_stride) : -1;
+            }
+        }
     }
     template <bool V>
     static __device__ __forceinline__ void issue(const int64_t (&off)[kLoads], const unsigned char* base, unsigned to) {
@@ -508,70 +522,77 @@ struct FewRange {
         }
     }
 
-    // units [u0, u1) of `table`'s `keys` tokens; limit: how many of them this lane's row sees, all_see: how many every row sees
-    static __device__ __forceinline__ void run(const AttentionArgs& a, PageList& list, const int* table, int u0, int u1, int keys, int limit, int all_see,
+    // blocks [n0, n1) of `table`'s tokens, of which there are `keys`; limit: how many of them this lane's row sees, all_see: how many every row sees
+    static __device__ __forceinline__ void run(const AttentionArgs& a, const int* table, int n0, int n1, int keys, int limit, int all_see,
                                                const unsigned char* kbase, const unsigned char* vbase, const unsigned char* buf,
                                                const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd, RowState<H>& st) {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int lane = threadIdx.x & 63;
         const unsigned char *kbuf = buf, *vbuf = buf + 32 * H::kRowBytes;
         const unsigned kto = __builtin_amdgcn_readfirstlane(lds_address(kbuf)), vto = __builtin_amdgcn_readfirstlane(lds_address(vbuf));
-        const int per_list = (kListed << a.page_shift) / kUnitKeys;
-        for (int lo = u0; lo < u1; lo += per_list) {
-            const int hi = min(u1, lo + per_list), end = min(hi * kUnitKeys, keys), first = (lo * kUnitKeys) >> a.page_shift;
-            list_pages(list, table + first, 0, ((end - 1) >> a.page_shift) - first + 1, a.pages);
-            const bool bad = __builtin_amdgcn_readfirstlane(list.bad) != 0;
-            int key0 = lo * kUnitKeys + wave * 32;
-            if (key0 >= end) continue;
+        const int last = min(n1 * kBlockKeys, keys);
+        int key0 = n0 * kBlockKeys;
+        while (key0 < last) {
+            // 64 pages at a time, one per lane
+            const int first = key0 >> a.page_shift, end = min((int64_t)last, (int64_t)(first + 64) << a.page_shift);
+            int page = -1;
+            const bool listed = ((int64_t)(first + lane) << a.page_shift) < end;
+            if (listed) page = table[first + lane];
+            if (page >= a.pages) page = -1;
+            const bool bad = __any(listed && page < 0);
             int64_t off[kLoads];
-            addresses(off, a, list, first, key0, keys);
+            addresses(off, a, page, first, key0, end);
             issue<false>(off, kbase, kto);
             issue<true>(off, vbase, vto);
             while (true) {
-                const int next = key0 + kUnitKeys;
+                const int next = key0 + kBlockKeys;
                 const bool more = next < end;
                 wait_loads<kLoads>();
                 f32x16 s[1] = {scores<T, D>(kbuf, q)};
                 if (more) {
-                    addresses(off, a, list, first, next, keys);
+                    addresses(off, a, page, first, next, end);
                     issue<false>(off, kbase, kto);
                 }
-                if (bad || key0 + 32 > all_see) hide(s[0], key0, limit, a, list, first);
+                if (bad || key0 + kBlockKeys > all_see) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = key0 + key_of(i), at = bad ? __shfl(page, (key >> a.page_shift) - first) : 0;
+                        s[0][i] = key < limit && at >= 0 ? s[0][i] : WHT_NEG_INF;
+                    }
+                }
                 weigh<H, 1>(s, a.scale, st);
                 if (more) wait_loads<kLoads>();
                 else wait_loads<0>();
                 accumulate<T, D, MULTI>(vbuf, s[0], limit - key0, odd, st);
+                key0 = next;
                 if (!more) break;
                 issue<true>(off, vbase, vto);
-                key0 = next;
             }
+            reads_done();
         }
     }
 };
 
-__device__ __forceinline__ int item_units(const AttentionArgs& a, int b) {
-    const int front = a.use_prefix ? ceil_div(a.prefix, kUnitKeys) : 0;
+__device__ __forceinline__ int item_blocks(const AttentionArgs& a, int b) {
+    const int front = a.use_prefix ? ceil_div(a.prefix, kBlockKeys) : 0;
     if (a.stacked) return front;
     const Sequence s = sequence(a.batch, b);
-    return s.queries > 0 ? front + ceil_div(s.length, kUnitKeys) : 0;
+    return s.queries > 0 ? front + ceil_div(s.length, kBlockKeys) : 0;
 }
 
 template <class T, int D, bool MULTI>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel(AttentionArgs a) {
     using H = Head<T, D>;
     constexpr int kWaveBytes = 2 * 32 * H::kRowBytes;
-    static_assert(kWaveBytes >= 32 * D * 4, "a wave's outputs are handed over where its keys stood");
     __shared__ __align__(16) unsigned char buf[4 * kWaveBytes];
-    __shared__ PageList list;
-    __shared__ FirstOdd<D> odd[4];
-    __shared__ float sums[4][32][2];
-    __shared__ int scan[4], found[2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ FirstOdd<D> odd[MULTI ? 4 : 1];
+    __shared__ int scan[4], found[4][2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int B = a.stacked ? 1 : a.batch.B;
 
-    // each thread's run of sequences, the runs' prefix sums, and the sequence in which this workgroup's share begins
+    // each thread's run of sequences, the runs' prefix sums, and the sequences in which the waves' shares begin
     const int run = ceil_div(B, 256), b0 = min(B, tid * run), b1 = min(B, b0 + run);
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += item_units(a, b);
+    for (int b = b0; b < b1; ++b) mine += item_blocks(a, b);
     int upto = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -585,26 +606,30 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel
     for (int w = 0; w < 4; ++w) { if (w < wave) before += scan[w]; all += scan[w]; }
     if (blockIdx.x == 0 && !a.stacked) {
         int c = before;
-        for (int b = b0; b < b1; ++b) { a.cum[b] = c; c += item_units(a, b); }
+        for (int b = b0; b < b1; ++b) { a.cum[b] = c; c += item_blocks(a, b); }
         if (tid == 255) a.cum[B] = all;
     }
-    const int total = all * a.heads, per = line_share(total, (int)gridDim.x);
-    int u = blockIdx.x * per;
-    const int end = min(total, u + per);
-    if (u >= end) return;
-    if (mine > 0 && u >= before * a.heads && u < (before + mine) * a.heads) {
-        int b = b0, c = before;
-        for (int n; u >= (c + (n = item_units(a, b))) * a.heads; ++b) c += n;
-        found[0] = b;
-        found[1] = c;
+    const int total = all * a.heads, per = line_share(total, a.rows_cap);
+    for (int w = 0; w < 4; ++w) {
+        const int u = min(total, (int)(blockIdx.x * 4 + w) * per);
+        if (mine > 0 && u >= before * a.heads && u < (before + mine) * a.heads) {
+            int b = b0, c = before;
+            for (int n; u >= (c + (n = item_blocks(a, b))) * a.heads; ++b) c += n;
+            found[w][0] = b;
+            found[w][1] = c;
+        }
     }
     __syncthreads();
-    int b = __builtin_amdgcn_readfirstlane(found[0]), cum = __builtin_amdgcn_readfirstlane(found[1]);
+    const int worker = blockIdx.x * 4 + wave;
+    int u = min(total, worker * per);
+    const int end = min(total, u + per);
+    if (u >= end) return;
+    int b = __builtin_amdgcn_readfirstlane(found[wave][0]), cum = __builtin_amdgcn_readfirstlane(found[wave][1]);
 
     while (u < end) {
-        const int n = item_units(a, b);
+        const int n = item_blocks(a, b);
         if (u >= (cum + n) * a.heads) { cum += n; ++b; continue; }
-        const int within = u - cum * a.heads, head = within / n, u0 = within - head * n, u1 = min(n, u0 + (end - u));
+        const int within = u - cum * a.heads, head = within / n, n0 = within - head * n, n1 = min(n, n0 + (end - u));
         const Sequence s = a.stacked ? Sequence{0, a.batch.T, 0} : sequence(a.batch, b);
         const int rows = min(s.queries * a.G, a.rows_cap), row = lane & 31;
         const int token = row / a.G, qh = head * a.G + row % a.G;
@@ -612,51 +637,26 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel
         load_row<T, D>(a.q + (s.first + token) * a.q_ts + qh * a.q_hs, row < rows, q);
         RowState<H> st;
         st.clear();
-        const unsigned char *kbase = a.k + head * a.head_stride, *vbase = a.v + head * a.head_stride;
-        const int front = a.use_prefix ? ceil_div(a.prefix, kUnitKeys) : 0;
-        if (u0 < front) FewRange<T, D, MULTI>::run(a, list, a.prefix_table, u0, min(u1, front), a.prefix, a.prefix, a.prefix, kbase, vbase, buf + wave * kWaveBytes, q, odd[wave], st);
-        if (u1 > front && !a.stacked) {
+        const unsigned char *kbase = a.k + head * a.head_stride, *vbase = a.v + head * a.head_stride, *own = buf + wave * kWaveBytes;
+        FirstOdd<D>& first = odd[MULTI ? wave : 0];
+        const int front = a.use_prefix ? ceil_div(a.prefix, kBlockKeys) : 0;
+        if (n0 < front) FewRange<T, D, MULTI>::run(a, a.prefix_table, n0, min(n1, front), a.prefix, a.prefix, a.prefix, kbase, vbase, own, q, first, st);
+        if (n1 > front && !a.stacked) {
             const int limit = min(max(s.length - s.queries + token + 1, 0), s.length), all_see = min(max(s.length - s.queries + 1, 0), s.length);
             const int keys = min(max(s.length - s.queries + min(s.queries, a.max_q), 0), s.length);       // what the last of the rows sees
-            FewRange<T, D, MULTI>::run(a, list, a.batch.table + b * a.batch.table_stride, max(u0 - front, 0), u1 - front, keys, limit, all_see, kbase, vbase,
-                                buf + wave * kWaveBytes, q, odd[wave], st);
+            FewRange<T, D, MULTI>::run(a, a.batch.table + b * a.batch.table_stride, max(n0 - front, 0), n1 - front, keys, limit, all_see, kbase, vbase, own, q, first, st);
         }
-        // the four waves' results of the piece, together
         st.l += other_half(st.l);
-        if (lane < 32) { sums[wave][row][0] = st.m; sums[wave][row][1] = st.l; }
-        __syncthreads();
-        float m = WHT_NEG_INF, l = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) m = fmaxf(m, sums[w][row][0]);
-        const float base = m == WHT_NEG_INF ? 0.0f : m, f = __builtin_amdgcn_exp2f(st.m - base);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) l += sums[w][row][1] * __builtin_amdgcn_exp2f(sums[w][row][0] - base);
-        float* own = reinterpret_cast<float*>(buf + wave * kWaveBytes);
         if (row < rows) {
+            const int64_t at = (int64_t)((a.stacked ? 0 : b) * a.heads + head + worker) * a.rows_cap + row;
+            if (lane < 32) *reinterpret_cast<f32x2*>(a.sums + at * 2) = f32x2{st.m, st.l};
 #pragma unroll
             for (int d = 0; d < H::kBlocks; ++d)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f32x4 x;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = st.o[d][4 * i + e] * f;
-                    *reinterpret_cast<f32x4*>(own + row * D + d * 32 + i * 8 + (lane >> 5) * 4) = x;
-                }
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<f32x4*>(a.part + at * D + d * 32 + i * 8 + (lane >> 5) * 4) = f32x4{st.o[d][4 * i], st.o[d][4 * i + 1], st.o[d][4 * i + 2], st.o[d][4 * i + 3]};
         }
-        const int64_t slot = (int64_t)((a.stacked ? 0 : b) * a.heads + head + blockIdx.x) * a.rows_cap;
-        if (wave == 0 && lane < rows) {
-            a.sums[(slot + lane) * 2] = m;
-            a.sums[(slot + lane) * 2 + 1] = l;
-        }
-        __syncthreads();
-        for (int i = tid; i < rows * (D / 4); i += 256) {
-            f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int w = 0; w < 4; ++w) x += *reinterpret_cast<const f32x4*>(buf + w * kWaveBytes + i * 16);
-            *reinterpret_cast<f32x4*>(a.part + slot * D + i * 4) = x;
-        }
-        __syncthreads();
-        u += u1 - u0;
+        u += n1 - n0;
     }
 }
 
@@ -819,7 +819,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void many_rows_kerne
 }
 
 // ------------------------------------------------------------------------------------------------
-// Joins the partial results of a row: out = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p.  A wave per row.
+// Joins the partial results of a row: out = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p.  WAVES waves share a row's pieces; D / 4 lanes take a
+// piece's outputs, 16 bytes each, so that a wave reads two pieces (four of 64 wide) at a time.
 
 struct JoinArgs {
     Batch batch;
@@ -828,7 +829,7 @@ struct JoinArgs {
     const float *front_part, *front_sums, *own_part, *own_sums;
     const int* cum;
     int64_t out_ts, out_hs;
-    int q_heads, heads, G, max_q, prefix, grid;         // grid: workgroups of the few-rows kernels
+    int q_heads, heads, G, max_q, prefix;
     int front, front_few, front_splits;                 // front: there is one
     int own_few, own_splits, own_cap, own_prefix;       // own_prefix: the own range begins with the prefix
 };
@@ -836,20 +837,23 @@ struct JoinArgs {
 struct Parts { const float *part, *sums; int64_t at, step; int n; };        // rows at, at + step, ...
 
 // The pieces of an item that covers units [u0, u0 + n) of a line of `total`.
-__device__ __forceinline__ Parts slots(const float* part, const float* sums, int item, int u0, int n, int total, int grid, int cap, int row) {
-    const Slots p = item_slots(item, u0, n, total, grid);
+__device__ __forceinline__ Parts slots(const float* part, const float* sums, int item, int u0, int n, int total, int cap, int row) {
+    const Slots p = item_slots(item, u0, n, total, cap);
     return {part, sums, p.first * cap + row, cap, p.count};
 }
 
-template <class T, int D>
-__global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+template <class T, int D, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(JoinArgs a) {
+    constexpr int kLanes = D / 4, kAtOnce = 64 / kLanes, kUnroll = 4;
+    struct Share { float m, l; f32x4 o[kLanes]; };
+    __shared__ Share shares[WAVES];
+    const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t r = WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     if (r >= (int64_t)a.batch.T * a.q_heads) return;
     const int t = (int)(r / a.q_heads), qh = (int)(r % a.q_heads), head = qh / a.G, g = qh % a.G;
     const int b = __builtin_amdgcn_readfirstlane(sequence_of(a.batch, t));
     float value = 0.0f, m = WHT_NEG_INF, l = 0.0f;
-    f32x2 o = {0.0f, 0.0f};
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     if (b >= 0) {
         const Sequence s = sequence(a.batch, b);
         const int j = t - s.first;
@@ -857,23 +861,27 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
         else {
             Parts parts[2] = {{nullptr, nullptr, 0, 0, 0}, {nullptr, nullptr, 0, 0, 0}};
             if (a.front) {
-                const int units = ceil_div(a.prefix, kUnitKeys);
-                if (a.front_few) parts[0] = slots(a.front_part, a.front_sums, head, head * units, units, a.heads * units, a.grid, a.batch.T * a.G, t * a.G + g);
+                const int units = ceil_div(a.prefix, kBlockKeys);
+                if (a.front_few) parts[0] = slots(a.front_part, a.front_sums, head, head * units, units, a.heads * units, a.batch.T * a.G, t * a.G + g);
                 else parts[0] = {a.front_part, a.front_sums, r, (int64_t)a.batch.T * a.q_heads, a.front_splits};
             }
             if (a.own_few) {
-                const int units = (a.own_prefix ? ceil_div(a.prefix, kUnitKeys) : 0) + ceil_div(s.length, kUnitKeys);
-                parts[1] = slots(a.own_part, a.own_sums, b * a.heads + head, a.cum[b] * a.heads + head * units, units, a.cum[a.batch.B] * a.heads, a.grid, a.own_cap, j * a.G + g);
+                const int units = (a.own_prefix ? ceil_div(a.prefix, kBlockKeys) : 0) + ceil_div(s.length, kBlockKeys);
+                parts[1] = slots(a.own_part, a.own_sums, b * a.heads + head, a.cum[b] * a.heads + head * units, units, a.cum[a.batch.B] * a.heads, a.own_cap, j * a.G + g);
             } else parts[1] = {a.own_part, a.own_sums, r, (int64_t)a.batch.T * a.q_heads, a.own_splits};
+            const int group = lane / kLanes, col = (lane % kLanes) * 4;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const Parts& p = parts[k];
-                for (int lo = 0; lo < p.n; lo += 64) {
-                    const int n = min(64, p.n - lo);
+                // the wave takes every WAVES-th run of 64 pieces, or an even share where there are fewer
+                const int run = min(64, ceil_div(p.n, WAVES));
+                for (int lo = wave * run; lo < p.n; lo += WAVES * run) {
+                    const int n = min(run, p.n - lo);
                     float pm = WHT_NEG_INF, pl = 0.0f;
                     if (lane < n) {
-                        pm = p.sums[(p.at + (lo + lane) * p.step) * 2];
-                        pl = p.sums[(p.at + (lo + lane) * p.step) * 2 + 1];
+                        const f32x2 x = *reinterpret_cast<const f32x2*>(p.sums + (p.at + (lo + lane) * p.step) * 2);
+                        pm = x[0];
+                        pl = x[1];
                     }
                     float most = pm;
 #pragma unroll
@@ -886,21 +894,46 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
                     l = l * f + sum;
                     o *= f;
                     m = now;
-                    for (int i = 0; i < n; ++i) {
-                        const float wi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), i));
-                        if (lane < D / 2) o += wi * *reinterpret_cast<const f32x2*>(p.part + (p.at + (lo + i) * p.step) * D + 2 * lane);
+                    for (int i = 0; i < n; i += kAtOnce * kUnroll) {
+                        f32x4 x[kUnroll];
+                        float wi[kUnroll];
+#pragma unroll
+                        for (int e = 0; e < kUnroll; ++e) {
+                            const int at = i + e * kAtOnce + group;
+                            const bool there = group < kAtOnce && at < n;
+                            wi[e] = __shfl(w, there ? at : 0);
+                            x[e] = there ? *reinterpret_cast<const f32x4*>(p.part + (p.at + (lo + at) * p.step) * D + col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                        }
+#pragma unroll
+                        for (int e = 0; e < kUnroll; ++e) o += wi[e] * x[e];
                     }
                 }
             }
+            const f32x4 mine = o;
+#pragma unroll
+            for (int e = 1; e < kAtOnce; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] += __shfl(mine[i], lane + e * kLanes);      // the first group's lanes hold the sum
+        }
+    }
+    if constexpr (WAVES > 1) {
+        if (lane < kLanes) shares[wave].o[lane] = o;
+        if (lane == 0) { shares[wave].m = m; shares[wave].l = l; }
+        __syncthreads();
+        if (wave > 0) return;
+        m = WHT_NEG_INF;
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, shares[w].m);
+        const float base = m == WHT_NEG_INF ? 0.0f : m;
+        l = 0.0f;
+        o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = __builtin_amdgcn_exp2f(shares[w].m - base);
+            l += shares[w].l * f;
+            o += f * shares[w].o[lane % kLanes];
         }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    if (lane < D / 2) {
-        unsigned char* to = a.out + t * a.out_ts + qh * a.out_hs + 2 * lane * sizeof(T);
-        const f32x2 x = o * inv + value;
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x2*>(to) = x;
-        else *reinterpret_cast<bf16x2*>(to) = bf16x2{(bf16)x[0], (bf16)x[1]};
-    }
+    if (lane < kLanes) store4<T>(a.out + t * a.out_ts + qh * a.out_hs + lane * 4 * sizeof(T), o * inv + value);
     if (a.lse && lane == 0) a.lse[r] = l == 0.0f ? WHT_NEG_INF : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 

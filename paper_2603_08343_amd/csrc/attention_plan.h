@@ -19,11 +19,12 @@ WHT_HD int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // A row is one query of one head.  Rows that read the same keys -- G = q_heads / heads query heads, all new tokens of the
 // sequence -- are taken together as the columns of one matrix product with the keys.
-constexpr int kFewRows = 32;        // few-rows kernel: one tile of rows, the waves share the keys out
+constexpr int kFewRows = 32;        // few-rows kernel: one tile of rows, every wave takes keys of its own
 constexpr int kTileRows = 128;      // many-rows kernel: 32 rows per wave, all waves take the same keys
-constexpr int kUnitKeys = 128;      // keys of one step of a workgroup in the few-rows kernel: 32 per wave
-constexpr int kStepKeys = 64;       // the same in the many-rows kernel
+constexpr int kBlockKeys = 32;      // keys of one step of a wave in the few-rows kernel
+constexpr int kStepKeys = 64;       // keys of one step of a workgroup in the many-rows kernel
 constexpr int kWorkgroups = 512;    // two per compute unit
+constexpr int kWorkers = 4 * kWorkgroups;       // waves of the few-rows kernel's grid
 
 enum class Range { Own, Prefix, Both };
 
@@ -56,13 +57,13 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
     p.front_few = T * G <= kFewRows;
     p.front_splits = p.own_splits = 1;
     if (p.front) {
-        if (p.front_few) p.front_rows = (size_t)(heads + kWorkgroups) * (size_t)(T * G);
+        if (p.front_few) p.front_rows = (size_t)(heads + kWorkers) * (size_t)(T * G);
         else {
             p.front_splits = splits_for(ceil_div64(T * G, kTileRows) * heads, prefix);
             p.front_rows = (size_t)p.front_splits * (size_t)(T * q_heads);
         }
     }
-    if (p.own_few) p.own_rows = ((size_t)B * heads + kWorkgroups) * (size_t)(max_q * G);
+    if (p.own_few) p.own_rows = ((size_t)B * heads + kWorkers) * (size_t)(max_q * G);
     else {
         p.own_splits = splits_for(ceil_div64((int64_t)max_q * G, kTileRows) * heads * B, max_length + prefix);
         if (p.own_splits > 1) p.own_rows = (size_t)p.own_splits * (size_t)(T * q_heads);
@@ -79,13 +80,17 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
     return p;
 }
 
-// The few-rows kernel's line: the units of all items one after the other, `per` of them to a workgroup.  The pieces of an item of n
-// units from u0 on lie in the slots item + w of the workgroups w that it meets: first .. first + count - 1.
+// The few-rows kernel's line: the blocks of all items one after the other, an equal share of them to a worker (a wave).  The pieces of an item
+// of n blocks from u0 on lie in the slots item + w of the workers w that it meets: first .. first + count - 1.  A piece writes `rows`
+// rows of results, 4 bytes an element, for the keys and values it reads: a share is a block for every eight rows at least.
 struct Slots { int64_t first; int count; };
-WHT_HD int line_share(int total, int workgroups) { return ceil_div(total, workgroups); }
-WHT_HD Slots item_slots(int item, int u0, int n, int total, int workgroups) {
+WHT_HD int line_share(int total, int rows) {
+    const int even = ceil_div(total, kWorkers), least = ceil_div(rows, 8);
+    return even > least ? even : least;
+}
+WHT_HD Slots item_slots(int item, int u0, int n, int total, int rows) {
     if (n == 0) return {0, 0};
-    const int per = line_share(total, workgroups), w0 = u0 / per, w1 = (u0 + n - 1) / per;
+    const int per = line_share(total, rows), w0 = u0 / per, w1 = (u0 + n - 1) / per;
     return {(int64_t)item + w0, w1 - w0 + 1};
 }
 

@@ -15,15 +15,15 @@ using namespace wht;
 
 #define CHECK(c) do { if (!(c)) { printf("FAILED %s:%d: %s\n", __FILE__, __LINE__, #c); exit(1); } } while (0)
 
-// Walks the line as the workgroups do, and compares what each item leaves with what item_slots says.
-static void walk(const std::vector<int>& lengths, int heads, int front) {
-    const int B = (int)lengths.size(), W = kWorkgroups;
+// Walks the line as the workers do, and compares what each item leaves with what item_slots says.
+static void walk(const std::vector<int>& lengths, int heads, int front, int rows) {
+    const int B = (int)lengths.size(), W = kWorkers;
     std::vector<int> units(B), cum(B + 1, 0);
     for (int b = 0; b < B; ++b) {
-        units[b] = ceil_div(front, kUnitKeys) + ceil_div(lengths[b], kUnitKeys);
+        units[b] = ceil_div(front, kBlockKeys) + ceil_div(lengths[b], kBlockKeys);
         cum[b + 1] = cum[b] + units[b];
     }
-    const int total = cum[B] * heads, per = line_share(total, W);
+    const int total = cum[B] * heads, per = line_share(total, rows);
     std::map<int, std::vector<int64_t>> of;             // item -> slots, in order
     std::set<int64_t> used;
     int covered = 0;
@@ -44,7 +44,7 @@ static void walk(const std::vector<int>& lengths, int heads, int front) {
     CHECK(covered == total);
     for (int b = 0; b < B; ++b)
         for (int h = 0; h < heads; ++h) {
-            const Slots s = item_slots(b * heads + h, cum[b] * heads + h * units[b], units[b], total, W);
+            const Slots s = item_slots(b * heads + h, cum[b] * heads + h * units[b], units[b], total, rows);
             const auto& got = of[b * heads + h];
             CHECK(s.count == (int)got.size());
             for (int i = 0; i < s.count; ++i) CHECK(got[i] == s.first + i);
@@ -60,7 +60,7 @@ static void plans() {
         const AttentionPlan p = plan_attention(T, B, heads * G, heads, dim, max_q, most, prefix);
         CHECK(p.own_few == (max_q * G <= kFewRows));
         CHECK(p.front_splits >= 1 && p.own_splits >= 1 && p.front_splits <= kWorkgroups && p.own_splits <= kWorkgroups);
-        if (p.own_few) CHECK(p.own_rows >= ((size_t)B * heads + kWorkgroups) * (size_t)(max_q * G));
+        if (p.own_few) CHECK(p.own_rows >= ((size_t)B * heads + kWorkers) * (size_t)(max_q * G));
         if (p.front && !p.front_few) CHECK(p.front_rows == (size_t)p.front_splits * (size_t)T * (size_t)(heads * G));
         if (!p.combine) CHECK(!p.front && !p.own_few && p.own_rows == 0);
         const size_t at[] = {p.front_at, p.own_at, p.front_sums_at, p.own_sums_at, p.cum_at, p.bytes};
@@ -139,11 +139,11 @@ int main() {
         std::vector<int> lengths(rng() % 200);
         const int most = 1 << (rng() % 16);
         for (int& n : lengths) n = (int)(rng() % (unsigned)most) * (rng() % 5 != 0);
-        walk(lengths, 1 + (int)(rng() % 40), i % 3 ? 0 : (int)(rng() % 5000));
+        walk(lengths, 1 + (int)(rng() % 40), i % 3 ? 0 : (int)(rng() % 5000), 1 + (int)(rng() % 32));
     }
-    walk({}, 8, 0);
-    walk({0, 0}, 8, 0);
-    walk({1}, 1, 0);
+    walk({}, 8, 0, 4);
+    walk({0, 0}, 8, 0, 4);
+    walk({1}, 1, 0, 1);
     plans();
     statuses();
     printf("attention_selftest: ok\n");

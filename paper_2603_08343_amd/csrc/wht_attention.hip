@@ -17,6 +17,9 @@ static int with_type(int dtype, int head_dim, F&& f) {
 
 static int launched() { return hipGetLastError() == hipSuccess ? WHT_OK : WHT_ERR_LAUNCH; }
 
+// Rows up to which 16, or 4, waves share a row's pieces: where few rows have to fill the chip.
+constexpr int64_t kJoinRowsWide = 256, kJoinRows = 2048;
+
 static int page_shift(const wht_attention_cache_t* c) { return __builtin_ctz((unsigned)c->page_size); }
 
 static Batch batch_of(const wht_attention_batch_t* b, int64_t T, int64_t most) {
@@ -104,11 +107,14 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     j.batch = a.batch; j.out = a.out; j.lse = lse; j.out_ts = a.out_ts; j.out_hs = a.out_hs;
     j.front_part = reinterpret_cast<float*>(ws + p.front_at); j.front_sums = reinterpret_cast<float*>(ws + p.front_sums_at);
     j.own_part = a.part; j.own_sums = a.sums; j.cum = a.cum;
-    j.q_heads = q_heads; j.heads = a.heads; j.G = a.G; j.max_q = max_q; j.prefix = a.prefix; j.grid = kWorkgroups;
+    j.q_heads = q_heads; j.heads = a.heads; j.G = a.G; j.max_q = max_q; j.prefix = a.prefix;
     j.front = p.front; j.front_few = p.front_few; j.front_splits = p.front_splits;
     j.own_few = p.own_few; j.own_splits = p.own_splits; j.own_cap = a.rows_cap; j.own_prefix = a.use_prefix;
     return with_type(dtype, c->head_dim, [&](auto t, auto d) {
-        hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value>), dim3((unsigned)ceil_div64(T * q_heads, 4)), dim3(256), 0, stream, j);
+        const int64_t rows = T * q_heads;
+        if (rows <= kJoinRowsWide) hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 16>), dim3((unsigned)rows), dim3(1024), 0, stream, j);
+        else if (rows <= kJoinRows) hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 4>), dim3((unsigned)rows), dim3(256), 0, stream, j);
+        else hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 1>), dim3((unsigned)ceil_div64(rows, 4)), dim3(256), 0, stream, j);
         return launched();
     });
 }

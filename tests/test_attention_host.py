@@ -98,3 +98,15 @@ def test_an_older_library_is_refused(source, monkeypatch):
     monkeypatch.setattr(os.path, "getmtime", lambda f: real(source) - 1.0 if f == build.ATTENTION_LIB else real(f))
     with pytest.raises(RuntimeError, match="older than its source"):
         build.ensure_built()
+
+
+def test_without_the_extension_module_calls_are_declined_after_one_warning(monkeypatch, recwarn):
+    import sys
+    monkeypatch.setitem(sys.modules, "paper_2603_08343_amd._attention_marshal", None)
+    monkeypatch.delattr(wht, "_attention_marshal", raising=False)
+    monkeypatch.setattr(attention, "_native_module", None)
+    monkeypatch.setattr(attention, "_torch", lambda: torch)              # as if a GPU had been seen
+    for _ in range(2):
+        native = attention._native()
+        assert native.append(*[None] * 12) is None and native.paged(*[None] * 15) is None
+    assert [w.category for w in recwarn] == [RuntimeWarning]

@@ -406,3 +406,47 @@ def test_refusals():
     kept = c["k_pages"].clone()
     append(ValueError, "without q_starts", k=torch.cat((c["k"], c["k"])), v=torch.cat((c["v"], c["v"])), q=None)
     assert torch.equal(kept, c["k_pages"])
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_native_marshalling_and_python_give_the_same(monkeypatch, interleaved):
+    """The extension module takes the plain calls, and without it attention.py's own code does the same."""
+    wht = _wht()
+    from paper_2603_08343_amd import attention
+    c = check.make(3, [2, 1, 3], [40, 1, 35], (4, 2, 128), 16, 20, seed=27)
+    d = check.make(3, [1, 1, 1], [40, 1, 0], (4, 2, 64), 16, 20, F32, "token", seed=28)
+    rope = [wht.wht_attention_rope_table(64, n, device="cuda:0") for n in (128, 32)]
+
+    def calls():
+        got = []
+        for x, r, starts in ((c, rope[0], c["starts"]), (d, rope[1], None)):
+            kp, vp = x["k_pages"].clone(), x["v_pages"].clone()
+            got.append(wht.wht_attention_append(x["q"], x["k"], x["v"], kp, vp, x["table"], x["lengths"], r, starts, 20, interleaved))
+            assert wht.wht_attention_append(None, x["k"], x["v"], kp, vp, x["table"], x["lengths"], None, starts) is None
+            got += [kp, vp, _paged(x, lse=False), *_paged(x), *_paged(x, scale=0.25, max_length=None, out=torch.empty_like(x["q"]))]
+            got.append(_paged({**x, "prefix": 0, "prefix_table": None}, lse=False, starts=starts is not None, max_q=None))
+        return got
+
+    native = attention._native()
+    assert native is not attention._NoNative
+    taken = []
+
+    class Counting:
+        @staticmethod
+        def append(*args):
+            taken.append(native.append(*args))
+            return taken[-1]
+
+        @staticmethod
+        def paged(*args):
+            taken.append(native.paged(*args))
+            return taken[-1]
+
+    monkeypatch.setattr(attention, "_native_module", Counting)
+    ours = calls()
+    assert len(taken) == 12 and all(x is not None for x in taken)
+    monkeypatch.setattr(attention, "_native_module", attention._NoNative)
+    assert all(torch.equal(a, b) for a, b in zip(ours, calls()))
+    monkeypatch.setattr(attention, "_native_module", native)
+    with pytest.raises(wht.WhtAttentionError, match="status 2"):
+        _paged(c, scale=-1.0)
