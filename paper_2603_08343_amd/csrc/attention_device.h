@@ -199,8 +199,9 @@ struct AttentionArgs {
     unsigned page_stride, token_stride;             // bytes
     int q_heads, heads, G, pages, page_shift, prefix, max_q;
     int splits, tiles, rows_cap;                    // rows_cap: rows of one slot of partial results
-    int stacked;                                    // rows of all sequences against the prefix alone
+    int stacked;                                    // many rows: those of all sequences, against the prefix alone
     int use_prefix;                                 // the range begins with the prefix
+    int front_item;                                 // few rows: the rows of all sequences against the prefix are one more sequence on the line
     float scale;                                    // scale * log2(e)
 };
 
@@ -573,21 +574,32 @@ struct FewRange {
 };
 
 __device__ __forceinline__ int item_blocks(const AttentionArgs& a, int b) {
+    if (b >= a.batch.B) return ceil_div(a.prefix, kBlockKeys);      // the front
     const int front = a.use_prefix ? ceil_div(a.prefix, kBlockKeys) : 0;
-    if (a.stacked) return front;
     const Sequence s = sequence(a.batch, b);
     return s.queries > 0 ? front + ceil_div(s.length, kBlockKeys) : 0;
 }
 
+// What a workgroup of either kernel has in LDS.
+template <class T, int D>
+struct Shared {
+    __align__(16) unsigned char buf[256 * Head<T, D>::kRowBytes];   // few rows: 32 keys and values of each wave; many: two steps' 64
+    FirstOdd<D> odd[4];
+    union {
+        PageList list;
+        struct { int scan[4], found[4][2]; };
+    };
+};
+
 template <class T, int D, bool MULTI>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel(AttentionArgs a) {
+__device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shared<T, D>& shared) {
     using H = Head<T, D>;
     constexpr int kWaveBytes = 2 * 32 * H::kRowBytes;
-    __shared__ __align__(16) unsigned char buf[4 * kWaveBytes];
-    __shared__ FirstOdd<D> odd[MULTI ? 4 : 1];
-    __shared__ int scan[4], found[4][2];
+    auto& buf = shared.buf;
+    auto& scan = shared.scan;
+    auto& found = shared.found;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int B = a.stacked ? 1 : a.batch.B;
+    const int B = a.batch.B + a.front_item;
 
     // each thread's run of sequences, the runs' prefix sums, and the sequences in which the waves' shares begin
     const int run = ceil_div(B, 256), b0 = min(B, tid * run), b1 = min(B, b0 + run);
@@ -604,14 +616,14 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel
     int before = upto - mine, all = 0;
 #pragma unroll
     for (int w = 0; w < 4; ++w) { if (w < wave) before += scan[w]; all += scan[w]; }
-    if (blockIdx.x == 0 && !a.stacked) {
+    if (block == 0) {
         int c = before;
         for (int b = b0; b < b1; ++b) { a.cum[b] = c; c += item_blocks(a, b); }
         if (tid == 255) a.cum[B] = all;
     }
     const int total = all * a.heads, per = line_share(total, a.rows_cap);
     for (int w = 0; w < 4; ++w) {
-        const int u = min(total, (int)(blockIdx.x * 4 + w) * per);
+        const int u = min(total, (block * 4 + w) * per);
         if (mine > 0 && u >= before * a.heads && u < (before + mine) * a.heads) {
             int b = b0, c = before;
             for (int n; u >= (c + (n = item_blocks(a, b))) * a.heads; ++b) c += n;
@@ -620,7 +632,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel
         }
     }
     __syncthreads();
-    const int worker = blockIdx.x * 4 + wave;
+    const int worker = block * 4 + wave;
     int u = min(total, worker * per);
     const int end = min(total, u + per);
     if (u >= end) return;
@@ -630,7 +642,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel
         const int n = item_blocks(a, b);
         if (u >= (cum + n) * a.heads) { cum += n; ++b; continue; }
         const int within = u - cum * a.heads, head = within / n, n0 = within - head * n, n1 = min(n, n0 + (end - u));
-        const Sequence s = a.stacked ? Sequence{0, a.batch.T, 0} : sequence(a.batch, b);
+        const bool stacked = b >= a.batch.B;
+        const Sequence s = stacked ? Sequence{0, a.batch.T, 0} : sequence(a.batch, b);
         const int rows = min(s.queries * a.G, a.rows_cap), row = lane & 31;
         const int token = row / a.G, qh = head * a.G + row % a.G;
         u32x4 q[H::kSteps];
@@ -638,17 +651,17 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel
         RowState<H> st;
         st.clear();
         const unsigned char *kbase = a.k + head * a.head_stride, *vbase = a.v + head * a.head_stride, *own = buf + wave * kWaveBytes;
-        FirstOdd<D>& first = odd[MULTI ? wave : 0];
-        const int front = a.use_prefix ? ceil_div(a.prefix, kBlockKeys) : 0;
+        FirstOdd<D>& first = shared.odd[wave];
+        const int front = a.use_prefix || stacked ? ceil_div(a.prefix, kBlockKeys) : 0;
         if (n0 < front) FewRange<T, D, MULTI>::run(a, a.prefix_table, n0, min(n1, front), a.prefix, a.prefix, a.prefix, kbase, vbase, own, q, first, st);
-        if (n1 > front && !a.stacked) {
+        if (n1 > front && !stacked) {
             const int limit = min(max(s.length - s.queries + token + 1, 0), s.length), all_see = min(max(s.length - s.queries + 1, 0), s.length);
             const int keys = min(max(s.length - s.queries + min(s.queries, a.max_q), 0), s.length);       // what the last of the rows sees
             FewRange<T, D, MULTI>::run(a, a.batch.table + b * a.batch.table_stride, max(n0 - front, 0), n1 - front, keys, limit, all_see, kbase, vbase, own, q, first, st);
         }
         st.l += other_half(st.l);
         if (row < rows) {
-            const int64_t at = (int64_t)((a.stacked ? 0 : b) * a.heads + head + worker) * a.rows_cap + row;
+            const int64_t at = (int64_t)(b * a.heads + head + worker) * a.rows_cap + row;
             if (lane < 32) *reinterpret_cast<f32x2*>(a.sums + at * 2) = f32x2{st.m, st.l};
 #pragma unroll
             for (int d = 0; d < H::kBlocks; ++d)
@@ -755,17 +768,17 @@ __device__ __forceinline__ void fill_rows(const AttentionArgs& a, int group) {
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void many_rows_kernel(AttentionArgs a) {
+__device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Shared<T, D>& shared) {
     using H = Head<T, D>;
     using R = ManyRange<T, D>;
-    __shared__ __align__(16) unsigned char buf[4 * R::kTileBytes];
-    __shared__ PageList list;
-    __shared__ FirstOdd<D> odd[4];
+    auto& buf = shared.buf;
+    auto& list = shared.list;
+    auto& odd = shared.odd;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int B = a.stacked ? 1 : a.batch.B;
     // Workgroups go to the 8 dies in turn: a die takes whole groups (a sequence's head and share of its keys), so that their keys are in its L2
     // once, tile after tile, the tiles that see most first.
-    const int groups = B * a.heads * a.splits, x = blockIdx.x & 7, y = blockIdx.x >> 3;
+    const int groups = B * a.heads * a.splits, x = block & 7, y = block >> 3;
     const int group = x + 8 * (y / a.tiles), tile = a.tiles - 1 - y % a.tiles;
     if (group >= groups) {
         // the grid's last workgroups, one per die
@@ -819,6 +832,26 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void many_rows_kerne
 }
 
 // ------------------------------------------------------------------------------------------------
+// The kernels.  Where rows of all sequences meet the prefix (compute-bound) and each sequence's few rows its own keys (memory-bound), one launch does
+// both, so that a compute unit holds a workgroup of each.
+
+template <class T, int D>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void many_rows_kernel(AttentionArgs a) {
+    __shared__ Shared<T, D> shared;
+    many_rows<T, D>(a, blockIdx.x, shared);
+}
+
+template <class T, int D, bool MULTI, bool FRONT>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel(AttentionArgs a, AttentionArgs front, int front_blocks) {
+    __shared__ Shared<T, D> shared;
+    if constexpr (FRONT) {
+        const int block = blockIdx.x;
+        if (block < front_blocks) many_rows<T, D>(front, block, shared);
+        else few_rows<T, D, MULTI>(a, block - front_blocks, shared);
+    } else few_rows<T, D, MULTI>(a, blockIdx.x, shared);
+}
+
+// ------------------------------------------------------------------------------------------------
 // Joins the partial results of a row: out = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p.  WAVES waves share a row's pieces; D / 4 lanes take a
 // piece's outputs, 16 bytes each, so that a wave reads two pieces (four of 64 wide) at a time.
 
@@ -860,14 +893,15 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Joi
         if (j < 0 || j >= s.queries || j >= a.max_q) value = l = __builtin_nanf("");
         else {
             Parts parts[2] = {{nullptr, nullptr, 0, 0, 0}, {nullptr, nullptr, 0, 0, 0}};
+            const int total = a.own_few ? a.cum[a.batch.B + (a.front && a.front_few)] * a.heads : 0;
             if (a.front) {
                 const int units = ceil_div(a.prefix, kBlockKeys);
-                if (a.front_few) parts[0] = slots(a.front_part, a.front_sums, head, head * units, units, a.heads * units, a.batch.T * a.G, t * a.G + g);
+                if (a.front_few) parts[0] = slots(a.own_part, a.own_sums, a.batch.B * a.heads + head, a.cum[a.batch.B] * a.heads + head * units, units, total, a.own_cap, t * a.G + g);
                 else parts[0] = {a.front_part, a.front_sums, r, (int64_t)a.batch.T * a.q_heads, a.front_splits};
             }
             if (a.own_few) {
                 const int units = (a.own_prefix ? ceil_div(a.prefix, kBlockKeys) : 0) + ceil_div(s.length, kBlockKeys);
-                parts[1] = slots(a.own_part, a.own_sums, b * a.heads + head, a.cum[b] * a.heads + head * units, units, a.cum[a.batch.B] * a.heads, a.own_cap, j * a.G + g);
+                parts[1] = slots(a.own_part, a.own_sums, b * a.heads + head, a.cum[b] * a.heads + head * units, units, total, a.own_cap, j * a.G + g);
             } else parts[1] = {a.own_part, a.own_sums, r, (int64_t)a.batch.T * a.q_heads, a.own_splits};
             const int group = lane / kLanes, col = (lane % kLanes) * 4;
 #pragma unroll

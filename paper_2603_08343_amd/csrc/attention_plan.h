@@ -29,18 +29,20 @@ constexpr int kWorkers = 4 * kWorkgroups;       // waves of the few-rows kernel'
 enum class Range { Own, Prefix, Both };
 
 // What one call launches.  `front`: the rows of all sequences against the prefix; `own`: each sequence's rows against its own
-// keys -- or, where there is no front, against prefix and own keys as one range.
+// keys -- or, where there is no front, against prefix and own keys as one range.  A front of few rows is one more sequence on the
+// few-rows kernel's line; one of many rows shares the launch with it, with a workgroup for every compute unit.
 struct AttentionPlan {
     bool front, front_few, own_few;
     int front_splits, own_splits;           // many-rows kernel: workgroups that share a tile's keys
     bool combine;
+    int32_t own_cap;                        // rows of one slot of the few-rows kernel's partial results
     size_t front_rows, own_rows;            // rows of partial results
     size_t front_at, own_at, front_sums_at, own_sums_at, cum_at, bytes;     // byte offsets in the workspace
 };
 
-inline int splits_for(int64_t tiles, int64_t keys) {
-    // enough workgroups for every compute unit, at least 256 keys each
-    int64_t s = tiles > 0 ? kWorkgroups / tiles : 1;
+inline int splits_for(int64_t tiles, int64_t keys, int workgroups) {
+    // at least 256 keys each
+    int64_t s = tiles > 0 ? workgroups / tiles : 1;
     const int64_t most = ceil_div64(keys, 256);
     if (s > most) s = most;
     return s < 1 ? 1 : (int)s;
@@ -57,15 +59,15 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
     p.front_few = T * G <= kFewRows;
     p.front_splits = p.own_splits = 1;
     if (p.front) {
-        if (p.front_few) p.front_rows = (size_t)(heads + kWorkers) * (size_t)(T * G);
-        else {
-            p.front_splits = splits_for(ceil_div64(T * G, kTileRows) * heads, prefix);
+        if (!p.front_few) {
+            p.front_splits = splits_for(ceil_div64(T * G, kTileRows) * heads, prefix, kWorkgroups / 2);
             p.front_rows = (size_t)p.front_splits * (size_t)(T * q_heads);
         }
     }
-    if (p.own_few) p.own_rows = ((size_t)B * heads + kWorkers) * (size_t)(max_q * G);
+    p.own_cap = p.front && p.front_few ? (int32_t)(T * G) : max_q * (int32_t)G;
+    if (p.own_few) p.own_rows = (((size_t)B + 1) * heads + kWorkers) * (size_t)p.own_cap;
     else {
-        p.own_splits = splits_for(ceil_div64((int64_t)max_q * G, kTileRows) * heads * B, max_length + prefix);
+        p.own_splits = splits_for(ceil_div64((int64_t)max_q * G, kTileRows) * heads * B, max_length + prefix, kWorkgroups);
         if (p.own_splits > 1) p.own_rows = (size_t)p.own_splits * (size_t)(T * q_heads);
     }
     p.combine = p.front || p.own_few || p.own_splits > 1;
@@ -75,7 +77,7 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
     p.own_at = take(p.own_rows * head_dim * 4);
     p.front_sums_at = take(p.front_rows * 8);
     p.own_sums_at = take(p.own_rows * 8);
-    p.cum_at = take(p.own_few ? ((size_t)B + 1) * 4 : 0);
+    p.cum_at = take(p.own_few ? ((size_t)B + 2) * 4 : 0);
     p.bytes = at;
     return p;
 }

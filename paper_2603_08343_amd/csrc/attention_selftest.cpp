@@ -60,11 +60,12 @@ static void plans() {
         const AttentionPlan p = plan_attention(T, B, heads * G, heads, dim, max_q, most, prefix);
         CHECK(p.own_few == (max_q * G <= kFewRows));
         CHECK(p.front_splits >= 1 && p.own_splits >= 1 && p.front_splits <= kWorkgroups && p.own_splits <= kWorkgroups);
-        if (p.own_few) CHECK(p.own_rows >= ((size_t)B * heads + kWorkers) * (size_t)(max_q * G));
+        if (p.own_few) CHECK(p.own_rows == (((size_t)B + 1) * heads + kWorkers) * (size_t)p.own_cap && p.own_cap >= max_q * G);
+        if (p.front && p.front_few) CHECK(p.own_cap == T * G && p.own_cap <= kFewRows);
         if (p.front && !p.front_few) CHECK(p.front_rows == (size_t)p.front_splits * (size_t)T * (size_t)(heads * G));
         if (!p.combine) CHECK(!p.front && !p.own_few && p.own_rows == 0);
         const size_t at[] = {p.front_at, p.own_at, p.front_sums_at, p.own_sums_at, p.cum_at, p.bytes};
-        const size_t need[] = {p.front_rows * dim * 4, p.own_rows * dim * 4, p.front_rows * 8, p.own_rows * 8, p.own_few ? ((size_t)B + 1) * 4 : 0};
+        const size_t need[] = {p.front_rows * dim * 4, p.own_rows * dim * 4, p.front_rows * 8, p.own_rows * 8, p.own_few ? ((size_t)B + 2) * 4 : 0};
         for (int k = 0; k < 5; ++k) CHECK(at[k] % 256 == 0 && at[k] + need[k] <= at[k + 1]);
     }
 }

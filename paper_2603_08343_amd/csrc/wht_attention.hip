@@ -73,34 +73,36 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     a.scale = (float)((double)scale * 1.4426950408889634074);
     const int64_t tiles_all = ceil_div64(T * a.G, kTileRows), tiles_one = ceil_div64((max_q < T ? max_q : T) * a.G, kTileRows);
 
-    auto many = [&](const AttentionArgs& m, int64_t groups) {
-        const int64_t grid = (ceil_div64(groups, 8) + 1) * 8 * m.tiles;             // the last 8: rows that no tile covers
-        if (grid > (int64_t)INT32_MAX) return (int)WHT_ERR_BAD_DIM;
-        return with_type(dtype, c->head_dim, [&](auto t, auto d) {
-            hipLaunchKernelGGL((many_rows_kernel<decltype(t), decltype(d)::value>), dim3((unsigned)((ceil_div64(groups, 8) * m.tiles + 1) * 8)), dim3(256), 0, stream, m);
-            return launched();
-        });
-    };
-    auto few = [&](const AttentionArgs& m) {
-        return with_type(dtype, c->head_dim, [&](auto t, auto d) {
-            // rows of one token each, or against the prefix, all see the same keys
-            if (m.stacked || max_q == 1) hipLaunchKernelGGL((few_rows_kernel<decltype(t), decltype(d)::value, false>), dim3(kWorkgroups), dim3(256), 0, stream, m);
-            else hipLaunchKernelGGL((few_rows_kernel<decltype(t), decltype(d)::value, true>), dim3(kWorkgroups), dim3(256), 0, stream, m);
-            return launched();
-        });
-    };
-
-    if (p.front) {
-        AttentionArgs f = a;
-        f.stacked = 1; f.use_prefix = 1; f.splits = p.front_splits; f.tiles = (int)tiles_all; f.rows_cap = (int)(T * a.G);
+    const auto many_blocks = [](const AttentionArgs& m, int64_t groups) { return (ceil_div64(groups, 8) * m.tiles + 1) * 8; };   // the last 8: rows that no tile covers
+    AttentionArgs f = a;
+    int64_t front_blocks = 0;
+    if (p.front && !p.front_few) {
+        f.stacked = 1; f.use_prefix = 1; f.splits = p.front_splits; f.tiles = (int)tiles_all;
         f.part = reinterpret_cast<float*>(ws + p.front_at); f.sums = reinterpret_cast<float*>(ws + p.front_sums_at);
-        if (int rc = p.front_few ? few(f) : many(f, (int64_t)c->heads * f.splits)) return rc;
+        front_blocks = many_blocks(f, (int64_t)c->heads * f.splits);
     }
     a.use_prefix = !p.front && prefix > 0;
-    a.splits = p.own_splits; a.tiles = (int)tiles_one; a.rows_cap = max_q * a.G;
+    a.front_item = p.front && p.front_few;
+    a.splits = p.own_splits; a.tiles = (int)tiles_one; a.rows_cap = p.own_cap;
     a.part = reinterpret_cast<float*>(ws + p.own_at); a.sums = reinterpret_cast<float*>(ws + p.own_sums_at);
     a.cum = reinterpret_cast<int*>(ws + p.cum_at);
-    if (int rc = p.own_few ? few(a) : many(a, (int64_t)b->B * c->heads * a.splits)) return rc;
+    const int64_t own_blocks = p.own_few ? kWorkgroups : many_blocks(a, (int64_t)b->B * c->heads * a.splits);
+    if (front_blocks + own_blocks > INT32_MAX) return WHT_ERR_BAD_DIM;
+    const int rc = with_type(dtype, c->head_dim, [&](auto t, auto d) {
+        using E = decltype(t);
+        constexpr int D = decltype(d)::value;
+        const dim3 grid((unsigned)(front_blocks + own_blocks)), block(256);
+        if (!p.own_few) hipLaunchKernelGGL((many_rows_kernel<E, D>), grid, block, 0, stream, a);
+        else if (max_q == 1) {                                      // a sequence's rows all see the same keys
+            if (front_blocks) hipLaunchKernelGGL((few_rows_kernel<E, D, false, true>), grid, block, 0, stream, a, f, (int)front_blocks);
+            else hipLaunchKernelGGL((few_rows_kernel<E, D, false, false>), grid, block, 0, stream, a, f, 0);
+        } else {
+            if (front_blocks) hipLaunchKernelGGL((few_rows_kernel<E, D, true, true>), grid, block, 0, stream, a, f, (int)front_blocks);
+            else hipLaunchKernelGGL((few_rows_kernel<E, D, true, false>), grid, block, 0, stream, a, f, 0);
+        }
+        return launched();
+    });
+    if (rc) return rc;
     if (!p.combine) return WHT_OK;
 
     JoinArgs j{};
