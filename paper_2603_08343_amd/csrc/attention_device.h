@@ -256,8 +256,11 @@ struct RowState {
     }
 };
 
+// The value that the lane 32 away holds.
 __device__ __forceinline__ float other_half(float x) {
-    return __shfl_xor(x, 32);
+    const unsigned u = __float_as_uint(x);
+    const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float((threadIdx.x & 32) ? both[0] : both[1]);
 }
 
 __device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
@@ -267,6 +270,10 @@ __device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigne
 // have returned (lgkmcnt).
 __device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned to) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(to) : "memory");
+}
+// The same from a place that all lanes share, `off` bytes on.
+__device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned off, unsigned to) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(from), "s"(to) : "memory");
 }
 template <int PENDING> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PENDING) : "memory"); }
 __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
@@ -279,17 +286,41 @@ __device__ __forceinline__ void workgroup_barrier() {
 // Loaded in place of keys that are not there.
 static __device__ __align__(16) unsigned char zero_chunk[16];
 
-// S^T of 32 keys (rows `row` = lane % 32 of the LDS block) and the wave's rows.
+// LDS addresses.  Where a row's chunks are a power of two, a place is the row's first one with the chunk's bits flipped in: one register and an
+// exclusive or for each, which is less than the registers that all of them would take (fresh() keeps the compiler from doing that).
+__device__ __forceinline__ unsigned fresh(unsigned x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+template <class V>
+__device__ __forceinline__ V lds_read(unsigned at) { return *(const __attribute__((address_space(3))) V*)(uintptr_t)at; }
+
 template <class T, int D>
-__device__ __forceinline__ f32x16 scores(const unsigned char* kbuf, const u32x4 (&q)[Head<T, D>::kSteps]) {
+struct KeyReads {                                                   // a lane reads chunks h, 2 + h, 4 + h, ... of row lane % 32
     using H = Head<T, D>;
-    const int lane = threadIdx.x & 63, row = lane & 31, h = lane >> 5;
+    static constexpr bool kFlip = (H::kChunks & (H::kChunks - 1)) == 0;
+    static __device__ __forceinline__ unsigned first(unsigned buf) {
+        const int lane = threadIdx.x & 63, row = lane & 31, h = lane >> 5;
+        return kFlip ? buf + row * H::kRowBytes + H::k_place(row, h) * 16 : buf + row * H::kRowBytes;
+    }
+    static __device__ __forceinline__ unsigned chunk(unsigned first, int c) {
+        const int lane = threadIdx.x & 63, row = lane & 31, h = lane >> 5;
+        return kFlip ? first ^ (c * 32) : first + H::k_place(row, 2 * c + h) * 16;
+    }
+};
+
+// S^T of 32 keys in LDS at `buf` (16-byte aligned rows) and the wave's rows.
+template <class T, int D>
+__device__ __forceinline__ f32x16 scores(unsigned buf, const u32x4 (&q)[Head<T, D>::kSteps]) {
+    using H = Head<T, D>;
+    using R = KeyReads<T, D>;
+    const unsigned first = R::first(buf);
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
     for (int c = 0; c < H::kSteps; ++c) {
-        const u32x4 k = *reinterpret_cast<const u32x4*>(kbuf + row * H::kRowBytes + H::k_place(row, 2 * c + h) * 16);
+        const u32x4 k = lds_read<u32x4>(R::chunk(first, c));
         if constexpr (!H::kF32) {
             s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[c]), s, 0, 0, 0);
         } else {
@@ -304,19 +335,22 @@ __device__ __forceinline__ f32x16 scores(const unsigned char* kbuf, const u32x4 
 // Key, of 32, whose score a lane's register i holds.
 __device__ __forceinline__ int key_of(int i) { return (i >> 2) * 8 + ((threadIdx.x >> 5) & 1) * 4 + (i & 3); }
 
-// Running maximum and sum over NS blocks of scores, which become weights.
+// The base of a row's weights follows its maximum, but not step by step: the sums are multiplied over only when the maximum has grown by more than a
+// factor of 2^kSlack (a wave's 32 rows would otherwise have one with a new maximum in most steps).  Weights are up to 2^kSlack then, which
+// float32 sums hold as exactly, and bfloat16 rounds relative to the value.
+constexpr float kSlack = 8.0f;
+
 template <class H, int NS>
-__device__ __forceinline__ void weigh(f32x16 (&s)[NS], float scale, RowState<H>& st) {
+__device__ __forceinline__ void rebase(const f32x16 (&s)[NS], float scale, RowState<H>& st) {
     float mx = s[0][0];
 #pragma unroll
     for (int n = 0; n < NS; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
-    mx = fmaxf(mx, other_half(mx));
-    const float now = fmaxf(st.m, mx * scale);
-    const float base = now == WHT_NEG_INF ? 0.0f : now;             // nothing seen yet: weights of zero
-    if (__any(now > st.m)) {
-        const float f = __builtin_amdgcn_exp2f(st.m - base);
+    mx = fmaxf(mx, other_half(mx)) * scale;
+    if (__any(mx > st.m + kSlack || (st.m == WHT_NEG_INF && mx > WHT_NEG_INF))) {
+        const float now = fmaxf(st.m, mx);
+        const float f = __builtin_amdgcn_exp2f(st.m - (now == WHT_NEG_INF ? 0.0f : now));
         st.l *= f;
 #pragma unroll
         for (int d = 0; d < H::kBlocks; ++d)
@@ -324,15 +358,19 @@ __device__ __forceinline__ void weigh(f32x16 (&s)[NS], float scale, RowState<H>&
             for (int i = 0; i < 16; ++i) st.o[d][i] *= f;
         st.m = now;
     }
-    float sum = 0.0f;
+}
+
+// Scores become weights, and their sum.
+template <class H>
+__device__ __forceinline__ void weigh(f32x16& s, float scale, RowState<H>& st) {
+    const float base = st.m == WHT_NEG_INF ? 0.0f : st.m;           // nothing seen yet: weights of zero
+    float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            s[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], scale, -base));
-            sum += s[n][i];
-        }
-    st.l += sum;
+    for (int i = 0; i < 16; ++i) {
+        s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -base));
+        sum[i & 1] += s[i];
+    }
+    st.l += sum[0] + sum[1];
 }
 
 // Values that are not finite, as zeros.
@@ -352,14 +390,17 @@ __device__ __forceinline__ float finite(float v, bool& found) {
     return odd ? 0.0f : v;
 }
 
-// o += (V^T P^T) over 32 keys, for the 32 columns of V from 32 d on.
+// o += (V^T P^T) over 32 keys in LDS at `buf`, for the 32 columns of V from 32 d on.
 template <class T, int D, bool GUARD>
-__device__ __forceinline__ void block_product(const unsigned char* vbuf, int d, const f32x16& p, f32x16& o, bool& found) {
+__device__ __forceinline__ void block_product(unsigned buf, int d, const f32x16& p, f32x16& o, bool& found) {
     using H = Head<T, D>;
     const int lane = threadIdx.x & 63;
+    constexpr bool kFlip = (H::kChunks & (H::kChunks - 1)) == 0;
     if constexpr (!H::kF32) {
         // a transposing read gives lane i of 16 the i-th of 16 columns, four rows of it, that the 16 lanes address as 4 x 4 pieces of 8 bytes
-        const int g = lane >> 4, in = lane & 15, row = (g >> 1) * 4 + (in >> 2);
+        const int g = lane >> 4, in = lane & 15, row = (g >> 1) * 4 + (in >> 2), c = (g & 1) * 2 + ((in & 3) >> 1);
+        const unsigned at = kFlip ? (buf + row * H::kRowBytes + H::v_place(row, c) * 16 + (in & 1) * 8) ^ (d * 64)
+                                  : buf + row * H::kRowBytes + H::v_place(row, d * 4 + c) * 16 + (in & 1) * 8;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             bf16x8 v, w;
@@ -367,9 +408,7 @@ __device__ __forceinline__ void block_product(const unsigned char* vbuf, int d, 
             for (int i = 0; i < 8; ++i) w[i] = (bf16)p[ks * 8 + i];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int r = ks * 16 + e * 8 + row;
-                const unsigned char* at = vbuf + r * H::kRowBytes + H::v_place(r, d * 4 + (g & 1) * 2 + ((in & 3) >> 1)) * 16 + (in & 1) * 8;
-                const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)lds_address(at));
+                const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)(at + (ks * 16 + e * 8) * H::kRowBytes));
                 const bf16x4 y = __builtin_bit_cast(bf16x4, x);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[e * 4 + i] = y[i];
@@ -378,11 +417,12 @@ __device__ __forceinline__ void block_product(const unsigned char* vbuf, int d, 
             o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, o, 0, 0, 0);
         }
     } else {
-        const int col = lane & 31;
+        const int col = lane & 31, h4 = (lane >> 5) * 4;
+        const unsigned at = kFlip ? (buf + h4 * H::kRowBytes + H::v_place(h4, col >> 2) * 16 + (col & 3) * 4) ^ (d * 128)
+                                  : buf + h4 * H::kRowBytes + H::v_place(h4, d * 8 + (col >> 2)) * 16 + (col & 3) * 4;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int r = key_of(i);
-            float v = *reinterpret_cast<const float*>(vbuf + r * H::kRowBytes + H::v_place(r, d * 8 + (col >> 2)) * 16 + (col & 3) * 4);
+            float v = lds_read<float>(at + ((i >> 2) * 8 + (i & 3)) * H::kRowBytes);
             if constexpr (GUARD) v = finite(v, found);
             o = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], o, 0, 0, 0);
         }
@@ -393,14 +433,14 @@ __device__ __forceinline__ void block_product(const unsigned char* vbuf, int d, 
 template <int D> struct FirstOdd { int above[D], below[D]; };
 
 template <class T, int D>
-__device__ __forceinline__ void add_odd(const unsigned char* vbuf, int seen, FirstOdd<D>& first, RowState<Head<T, D>>& st) {
+__device__ __forceinline__ void add_odd(unsigned buf, int seen, FirstOdd<D>& first, RowState<Head<T, D>>& st) {
     using H = Head<T, D>;
     const int lane = threadIdx.x & 63;
     for (int c = lane; c < D; c += 64) {
         int above = 32, below = 32;
 #pragma unroll 1
         for (int k = 31; k >= 0; --k) {
-            const float v = (float)*reinterpret_cast<const T*>(vbuf + k * H::kRowBytes + H::v_place(k, c * (int)sizeof(T) / 16) * 16 + c * (int)sizeof(T) % 16);
+            const float v = (float)lds_read<T>(buf + k * H::kRowBytes + H::v_place(k, c * (int)sizeof(T) / 16) * 16 + c * (int)sizeof(T) % 16);
             if (!(fabsf(v) < __builtin_inff())) {
                 if (v != WHT_NEG_INF) above = k;
                 if (v != -WHT_NEG_INF) below = k;
@@ -425,12 +465,12 @@ __device__ __forceinline__ void add_odd(const unsigned char* vbuf, int seen, Fir
 // the tile see different keys (GUARD; a row sees the first `seen` of the 32), values that are not finite stay out of the product, and the
 // rows that see one get it by itself.
 template <class T, int D, bool GUARD>
-__device__ __forceinline__ void accumulate(const unsigned char* vbuf, const f32x16& p, int seen, FirstOdd<D>& first, RowState<Head<T, D>>& st) {
+__device__ __forceinline__ void accumulate(unsigned buf, const f32x16& p, int seen, FirstOdd<D>& first, RowState<Head<T, D>>& st) {
     bool found = false;
 #pragma unroll
-    for (int d = 0; d < Head<T, D>::kBlocks; ++d) block_product<T, D, GUARD>(vbuf, d, p, st.o[d], found);
+    for (int d = 0; d < Head<T, D>::kBlocks; ++d) block_product<T, D, GUARD>(buf, d, p, st.o[d], found);
     if constexpr (GUARD)
-        if (__any(found)) add_odd<T, D>(vbuf, seen, first, st);
+        if (__any(found)) add_odd<T, D>(buf, seen, first, st);
 }
 
 // A row of q, as the B operand of the first product; zeros where there is no row.
@@ -525,11 +565,10 @@ struct FewRange {
 
     // blocks [n0, n1) of `table`'s tokens, of which there are `keys`; limit: how many of them this lane's row sees, all_see: how many every row sees
     static __device__ __forceinline__ void run(const AttentionArgs& a, const int* table, int n0, int n1, int keys, int limit, int all_see,
-                                               const unsigned char* kbase, const unsigned char* vbase, const unsigned char* buf,
+                                               const unsigned char* kbase, const unsigned char* vbase, unsigned kbuf,
                                                const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd, RowState<H>& st) {
         const int lane = threadIdx.x & 63;
-        const unsigned char *kbuf = buf, *vbuf = buf + 32 * H::kRowBytes;
-        const unsigned kto = __builtin_amdgcn_readfirstlane(lds_address(kbuf)), vto = __builtin_amdgcn_readfirstlane(lds_address(vbuf));
+        const unsigned vbuf = kbuf + 32 * H::kRowBytes;
         const int last = min(n1 * kBlockKeys, keys);
         int key0 = n0 * kBlockKeys;
         while (key0 < last) {
@@ -542,8 +581,8 @@ struct FewRange {
             const bool bad = __any(listed && page < 0);
             int64_t off[kLoads];
             addresses(off, a, page, first, key0, end);
-            issue<false>(off, kbase, kto);
-            issue<true>(off, vbase, vto);
+            issue<false>(off, kbase, kbuf);
+            issue<true>(off, vbase, vbuf);
             while (true) {
                 const int next = key0 + kBlockKeys;
                 const bool more = next < end;
@@ -551,7 +590,7 @@ struct FewRange {
                 f32x16 s[1] = {scores<T, D>(kbuf, q)};
                 if (more) {
                     addresses(off, a, page, first, next, end);
-                    issue<false>(off, kbase, kto);
+                    issue<false>(off, kbase, kbuf);
                 }
                 if (bad || key0 + kBlockKeys > all_see) {
 #pragma unroll
@@ -560,13 +599,14 @@ struct FewRange {
                         s[0][i] = key < limit && at >= 0 ? s[0][i] : WHT_NEG_INF;
                     }
                 }
-                weigh<H, 1>(s, a.scale, st);
+                rebase<H, 1>(s, a.scale, st);
+                weigh(s[0], a.scale, st);
                 if (more) wait_loads<kLoads>();
                 else wait_loads<0>();
                 accumulate<T, D, MULTI>(vbuf, s[0], limit - key0, odd, st);
                 key0 = next;
                 if (!more) break;
-                issue<true>(off, vbase, vto);
+                issue<true>(off, vbase, vbuf);
             }
             reads_done();
         }
@@ -650,14 +690,18 @@ __device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shar
         load_row<T, D>(a.q + (s.first + token) * a.q_ts + qh * a.q_hs, row < rows, q);
         RowState<H> st;
         st.clear();
-        const unsigned char *kbase = a.k + head * a.head_stride, *vbase = a.v + head * a.head_stride, *own = buf + wave * kWaveBytes;
+        const unsigned char *kbase = a.k + head * a.head_stride, *vbase = a.v + head * a.head_stride;
+        const unsigned own = __builtin_amdgcn_readfirstlane(lds_address(buf)) + wave * kWaveBytes;
         FirstOdd<D>& first = shared.odd[wave];
         const int front = a.use_prefix || stacked ? ceil_div(a.prefix, kBlockKeys) : 0;
-        if (n0 < front) FewRange<T, D, MULTI>::run(a, a.prefix_table, n0, min(n1, front), a.prefix, a.prefix, a.prefix, kbase, vbase, own, q, first, st);
-        if (n1 > front && !stacked) {
-            const int limit = min(max(s.length - s.queries + token + 1, 0), s.length), all_see = min(max(s.length - s.queries + 1, 0), s.length);
-            const int keys = min(max(s.length - s.queries + min(s.queries, a.max_q), 0), s.length);       // what the last of the rows sees
-            FewRange<T, D, MULTI>::run(a, a.batch.table + b * a.batch.table_stride, max(n0 - front, 0), n1 - front, keys, limit, all_see, kbase, vbase, own, q, first, st);
+        const int limit = min(max(s.length - s.queries + token + 1, 0), s.length), all_see = min(max(s.length - s.queries + 1, 0), s.length);
+        const int keys = min(max(s.length - s.queries + min(s.queries, a.max_q), 0), s.length);           // what the last of the rows sees
+#pragma unroll 1
+        for (int part = 0; part < 2; ++part) {                      // the prefix, the sequence
+            const int lo = part ? max(n0 - front, 0) : n0, hi = part ? n1 - front : min(n1, front);
+            if (lo >= hi) continue;
+            FewRange<T, D, MULTI>::run(a, part ? a.batch.table + b * a.batch.table_stride : a.prefix_table, lo, hi, part ? keys : a.prefix, part ? limit : a.prefix,
+                                       part ? all_see : a.prefix, kbase, vbase, own, q, first, st);
         }
         st.l += other_half(st.l);
         if (row < rows) {
@@ -674,8 +718,9 @@ __device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shar
 }
 
 // ------------------------------------------------------------------------------------------------
-// Many rows: a workgroup takes 128 rows, 32 per wave, and all its waves the same 64 keys a step, which lie in LDS twice over: the next step's
-// are in flight during the products.
+// Many rows: a workgroup takes 128 rows, 32 per wave, and all its waves the same 64 keys a step; keys and values lie in LDS twice over, the
+// next steps' in flight.  Steps that every row sees all of run as a pipeline: the products with the next step's keys stand
+// beside this step's exponentials, so that the matrix units have work while the vector units do.
 
 template <class T, int D>
 struct ManyRange {
@@ -695,38 +740,107 @@ struct ManyRange {
         }
     }
 
-    // steps [t0, t1) of `table`'s `keys` tokens; limit: how many this lane's row sees; all_see, any_sees: every, any row of the wave
+    // The pipeline, over steps [lo, hi) of pages that are all there, of 16 tokens at least: a wave's 16 of the 64 keys are in one page, and a lane's
+    // place in it is the same every step.  LDS: keys of even, of odd steps, values of even, of odd steps.
+    static __device__ __forceinline__ void stream(const AttentionArgs& a, const PageList& list, int first, int lo, int hi, const unsigned char* kbase,
+                                                  const unsigned char* vbase, unsigned buf, const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd, RowState<H>& st) {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const unsigned to = buf + wave * kLoads * 1024;
+        unsigned koff[kLoads], voff[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int n = (wave * kLoads + i) * 64 + lane, r = n / H::kChunks, p = n % H::kChunks;
+            koff[i] = (unsigned)(r - wave * 16) * a.token_stride + H::k_chunk(r, p) * 16;
+            voff[i] = (unsigned)(r - wave * 16) * a.token_stride + H::v_chunk(r, p) * 16;
+        }
+        auto place = [&](int t) {
+            const int key = t * kStepKeys + wave * 16, page = __builtin_amdgcn_readfirstlane(list.page[(key >> a.page_shift) - first]);
+            return (uint64_t)(unsigned)page * a.page_stride + (unsigned)(key & ((1 << a.page_shift) - 1)) * a.token_stride;
+        };
+        auto load_k = [&](int t, uint64_t from) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) load_to_lds(kbase + from, koff[i], to + (t & 1) * kTileBytes + i * 1024);
+        };
+        auto load_v = [&](int t, uint64_t from) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) load_to_lds(vbase + from, voff[i], to + (2 + (t & 1)) * kTileBytes + i * 1024);
+        };
+        uint64_t now = place(lo), next = place(min(lo + 1, hi - 1));
+        load_k(lo, now);
+        load_v(lo, now);
+        if (lo + 1 < hi) { load_k(lo + 1, next); wait_loads<2 * kLoads>(); }
+        else wait_loads<kLoads>();
+        workgroup_barrier();
+        auto score = [&](int t, f32x16 (&s)[2]) {
+            const unsigned keys = fresh(buf + (t & 1) * kTileBytes);
+            s[0] = scores<T, D>(keys, q);
+            s[1] = scores<T, D>(keys + 32 * H::kRowBytes, q);
+        };
+        auto use = [&](int t, f32x16 (&s)[2]) {
+            const unsigned values = fresh(buf + (2 + (t & 1)) * kTileBytes);
+            weigh(s[0], a.scale, st);
+            weigh(s[1], a.scale, st);
+            accumulate<T, D, false>(values, s[0], 0, odd, st);
+            accumulate<T, D, false>(values + 32 * H::kRowBytes, s[1], 0, odd, st);
+        };
+        auto step = [&](int t, f32x16 (&s)[2], f32x16 (&ahead)[2]) {        // t + 1 < hi
+            wait_loads<0>();
+            workgroup_barrier();                                    // V of this step and K of the next have landed; what they replace next has been read
+            load_v(t + 1, next);
+            if (t + 2 < hi) { next = place(t + 2); load_k(t + 2, next); }
+            rebase<H, 2>(s, a.scale, st);
+            score(t + 1, ahead);
+            use(t, s);
+        };
+        f32x16 s[2], other[2];
+        score(lo, s);
+        int t = lo;
+        while (t + 1 < hi) {
+            step(t++, s, other);
+            if (t + 1 < hi) step(t++, other, s);
+            else { s[0] = other[0]; s[1] = other[1]; }
+        }
+        wait_loads<0>();
+        workgroup_barrier();
+        rebase<H, 2>(s, a.scale, st);
+        use(t, s);
+    }
+
+    // steps [t0, t1) of `table`'s `keys` tokens; limit: how many this lane's row sees; all_see: every row of the workgroup, any_sees: any row of the wave
     static __device__ __forceinline__ void run(const AttentionArgs& a, PageList& list, const int* table, int t0, int t1, int keys, int limit, int all_see, int any_sees,
-                                               const unsigned char* kbase, const unsigned char* vbase, const unsigned char* buf,
+                                               const unsigned char* kbase, const unsigned char* vbase, unsigned buf,
                                                const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd, RowState<H>& st) {
-        const unsigned at = __builtin_amdgcn_readfirstlane(lds_address(buf));
         const int per_list = (kListed << a.page_shift) / kStepKeys;
         for (int lo = t0; lo < t1; lo += per_list) {
             const int hi = min(t1, lo + per_list), end = min(hi * kStepKeys, keys), first = (lo * kStepKeys) >> a.page_shift;
             list_pages(list, table + first, 0, ((end - 1) >> a.page_shift) - first + 1, a.pages);
             const bool bad = __builtin_amdgcn_readfirstlane(list.bad) != 0;
-            issue(a, list, first, lo * kStepKeys, keys, kbase, vbase, at, at + kTileBytes);
-            for (int t = lo; t < hi; ++t) {
-                const int key0 = t * kStepKeys, side = (t - lo) & 1;
+            int from = lo;
+            if (!bad && a.page_shift >= 4 && min(hi, all_see / kStepKeys) > lo) {
+                from = min(hi, all_see / kStepKeys);
+                stream(a, list, first, lo, from, kbase, vbase, buf, q, odd, st);
+                if (from == hi) continue;
+                workgroup_barrier();                                // the pipeline's last reads are done
+            }
+            issue(a, list, first, from * kStepKeys, keys, kbase, vbase, buf, buf + kTileBytes);
+            for (int t = from; t < hi; ++t) {
+                const int key0 = t * kStepKeys, side = (t - from) & 1;
                 wait_loads<0>();
                 workgroup_barrier();                                // everyone's loads of this step have landed, everyone's reads of the last are done
-                const unsigned other = at + (side ^ 1) * 2 * kTileBytes;
+                const unsigned other = buf + (side ^ 1) * 2 * kTileBytes;
                 if (t + 1 < hi) issue(a, list, first, key0 + kStepKeys, keys, kbase, vbase, other, other + kTileBytes);
                 if (key0 < any_sees) {
-                    const unsigned char* kbuf = buf + side * 2 * kTileBytes;
-                    f32x16 s[2] = {scores<T, D>(kbuf, q), scores<T, D>(kbuf + 32 * H::kRowBytes, q)};
+                    const unsigned here = fresh(buf + side * 2 * kTileBytes);
+                    f32x16 s[2] = {scores<T, D>(here, q), scores<T, D>(here + 32 * H::kRowBytes, q)};
                     if (bad || key0 + kStepKeys > all_see) {
                         hide(s[0], key0, limit, a, list, first);
                         hide(s[1], key0 + 32, limit, a, list, first);
                     }
-                    weigh<H, 2>(s, a.scale, st);
-                    const unsigned char* vbuf = kbuf + kTileBytes;
-                    if (all_see < min(key0 + kStepKeys, keys)) {
-                        accumulate<T, D, true>(vbuf, s[0], limit - key0, odd, st);
-                        accumulate<T, D, true>(vbuf + 32 * H::kRowBytes, s[1], limit - key0 - 32, odd, st);
-                    } else {
-                        accumulate<T, D, false>(vbuf, s[0], 0, odd, st);
-                        accumulate<T, D, false>(vbuf + 32 * H::kRowBytes, s[1], 0, odd, st);
+                    rebase<H, 2>(s, a.scale, st);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        weigh(s[n], a.scale, st);
+                        accumulate<T, D, true>(here + kTileBytes + n * 32 * H::kRowBytes, s[n], limit - key0 - n * 32, odd, st);
                     }
                 }
             }
@@ -798,16 +912,21 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
     // own tokens that row r of the tile sees: length - queries + its token + 1
     auto sees = [&](int64_t r) { return a.stacked ? 0 : min(max(s.length - s.queries + (int)(min(r, rows - 1) / a.G) + 1, 0), s.length); };
     const int keys = sees(tile * kTileRows + kTileRows - 1);
-    const int limit = sees(row), all_see = sees(row0), any_sees = row0 < rows ? sees(row0 + 31) : 0;
+    const int limit = sees(row), all_see = sees((int64_t)tile * kTileRows), any_sees = row0 < rows ? sees(row0 + 31) : 0;
     const int front = a.use_prefix ? ceil_div(a.prefix, kStepKeys) : 0;
     const int total = front + ceil_div(keys, kStepKeys), per = ceil_div(total, a.splits);
     const int t0 = min(total, split * per), t1 = min(total, t0 + per);
     RowState<H> st;
     st.clear();
     const unsigned char *kbase = a.k + head * a.head_stride, *vbase = a.v + head * a.head_stride;
-    if (t0 < min(t1, front)) R::run(a, list, a.prefix_table, t0, min(t1, front), a.prefix, a.prefix, a.prefix, row0 < rows ? a.prefix : 0, kbase, vbase, buf, q, odd[wave], st);
-    if (max(t0, front) < t1)
-        R::run(a, list, a.batch.table + b * a.batch.table_stride, max(t0 - front, 0), t1 - front, keys, limit, all_see, any_sees, kbase, vbase, buf, q, odd[wave], st);
+    const unsigned at = __builtin_amdgcn_readfirstlane(lds_address(buf));
+#pragma unroll 1
+    for (int own = 0; own < 2; ++own) {                             // the prefix, the sequence
+        const int lo = own ? max(t0 - front, 0) : t0, hi = own ? t1 - front : min(t1, front);
+        if (lo >= hi) continue;
+        R::run(a, list, own ? a.batch.table + b * a.batch.table_stride : a.prefix_table, lo, hi, own ? keys : a.prefix, own ? limit : a.prefix,
+               own ? all_see : a.prefix, own ? any_sees : row0 < rows ? a.prefix : 0, kbase, vbase, at, q, odd[wave], st);
+    }
     if (!there) return;
     st.l += other_half(st.l);
     const int64_t t = s.first + token;
