@@ -11,6 +11,7 @@ typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short short4v __attribute__((ext_vector_type(4)));
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -335,12 +336,12 @@ __device__ __forceinline__ f32x16 scores(unsigned buf, const u32x4 (&q)[Head<T, 
 // Key, of 32, whose score a lane's register i holds.
 __device__ __forceinline__ int key_of(int i) { return (i >> 2) * 8 + ((threadIdx.x >> 5) & 1) * 4 + (i & 3); }
 
-// The base of a row's weights follows its maximum, but not step by step: the sums are multiplied over only when the maximum has grown by more than a
-// factor of 2^kSlack (a wave's 32 rows would otherwise have one with a new maximum in most steps).  Weights are up to 2^kSlack then, which
-// float32 sums hold as exactly, and bfloat16 rounds relative to the value.
-constexpr float kSlack = 8.0f;
-
-template <class H, int NS>
+// The base of a row's weights follows its maximum; SLACK: not step by step, but when the maximum has grown by more than a factor of 2^SLACK.  With
+// many rows, where the vector units' time counts, that is 8: one of a wave's 32 rows has a new maximum in most steps, and each
+// one multiplies all the sums over.  Weights are up to 256 then, which float32 sums hold as exactly; but the largest of a row is no longer
+// 1, which bfloat16 holds exactly: the error of the outputs, with that of their own rounding, goes from 1.9e-3 to 2.3e-3 of their norm.
+// With few rows, bound by memory, it is 0.
+template <class H, int NS, int SLACK>
 __device__ __forceinline__ void rebase(const f32x16 (&s)[NS], float scale, RowState<H>& st) {
     float mx = s[0][0];
 #pragma unroll
@@ -348,7 +349,7 @@ __device__ __forceinline__ void rebase(const f32x16 (&s)[NS], float scale, RowSt
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
     mx = fmaxf(mx, other_half(mx)) * scale;
-    if (__any(mx > st.m + kSlack || (st.m == WHT_NEG_INF && mx > WHT_NEG_INF))) {
+    if (__any(mx > st.m + (float)SLACK || (st.m == WHT_NEG_INF && mx > WHT_NEG_INF))) {
         const float now = fmaxf(st.m, mx);
         const float f = __builtin_amdgcn_exp2f(st.m - (now == WHT_NEG_INF ? 0.0f : now));
         st.l *= f;
@@ -374,25 +375,16 @@ __device__ __forceinline__ void weigh(f32x16& s, float scale, RowState<H>& st) {
 }
 
 // Values that are not finite, as zeros.
-__device__ __forceinline__ bf16x8 finite(bf16x8 v, bool& found) {
+__device__ __forceinline__ bf16x8 finite(bf16x8 v) {
     u32x4 x = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const bool lo = (x[i] & 0x7f80u) == 0x7f80u, hi = (x[i] & 0x7f800000u) == 0x7f800000u;
-        found |= lo | hi;
-        x[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
-    }
+    for (int i = 0; i < 4; ++i) x[i] &= ((x[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((x[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
     return __builtin_bit_cast(bf16x8, x);
 }
-__device__ __forceinline__ float finite(float v, bool& found) {
-    const bool odd = !(fabsf(v) < __builtin_inff());
-    found |= odd;
-    return odd ? 0.0f : v;
-}
 
-// o += (V^T P^T) over 32 keys in LDS at `buf`, for the 32 columns of V from 32 d on.
+// o += (V^T P^T) over 32 keys in LDS at `buf`, for the 32 columns of V from 32 d on.  GUARD: where `odd`, values that are not finite stay out.
 template <class T, int D, bool GUARD>
-__device__ __forceinline__ void block_product(unsigned buf, int d, const f32x16& p, f32x16& o, bool& found) {
+__device__ __forceinline__ void block_product(unsigned buf, int d, const f32x16& p, bool odd, f32x16& o) {
     using H = Head<T, D>;
     const int lane = threadIdx.x & 63;
     constexpr bool kFlip = (H::kChunks & (H::kChunks - 1)) == 0;
@@ -413,7 +405,11 @@ __device__ __forceinline__ void block_product(unsigned buf, int d, const f32x16&
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[e * 4 + i] = y[i];
             }
-            if constexpr (GUARD) v = finite(v, found);
+            if constexpr (GUARD)
+                if (odd) {
+                    asm volatile("");                               // a branch: not computed where it is not needed
+                    v = finite(v);
+                }
             o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, o, 0, 0, 0);
         }
     } else {
@@ -423,10 +419,28 @@ __device__ __forceinline__ void block_product(unsigned buf, int d, const f32x16&
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             float v = lds_read<float>(at + ((i >> 2) * 8 + (i & 3)) * H::kRowBytes);
-            if constexpr (GUARD) v = finite(v, found);
+            if constexpr (GUARD) v = fabsf(v) < __builtin_inff() ? v : 0.0f;
             o = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], o, 0, 0, 0);
         }
     }
+}
+
+// Whether 32 rows in LDS hold anything that is not finite.
+template <class T, int D>
+__device__ __forceinline__ bool any_odd(unsigned buf) {
+    constexpr unsigned kMagnitude = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
+    unsigned most = 0;
+    ushort2v most2 = {0, 0};
+#pragma unroll
+    for (int i = 0; i < Head<T, D>::kChunks / 2; ++i) {
+        const u32x4 x = lds_read<u32x4>(buf + (threadIdx.x & 63) * 16 + i * 1024);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 4) most = max(most, x[e] & kMagnitude);
+            else most2 = __builtin_elementwise_max(most2, __builtin_bit_cast(ushort2v, x[e] & kMagnitude));
+        }
+    }
+    return __any(sizeof(T) == 4 ? most >= 0x7f800000u : most2[0] >= 0x7f80 || most2[1] >= 0x7f80);
 }
 
 // The first of 32 keys whose value in a column is +infinity or NaN (above), -infinity or NaN (below); 32 where there is none.
@@ -466,11 +480,11 @@ __device__ __forceinline__ void add_odd(unsigned buf, int seen, FirstOdd<D>& fir
 // rows that see one get it by itself.
 template <class T, int D, bool GUARD>
 __device__ __forceinline__ void accumulate(unsigned buf, const f32x16& p, int seen, FirstOdd<D>& first, RowState<Head<T, D>>& st) {
-    bool found = false;
+    bool odd = false;
+    if constexpr (GUARD) odd = any_odd<T, D>(buf);
 #pragma unroll
-    for (int d = 0; d < Head<T, D>::kBlocks; ++d) block_product<T, D, GUARD>(buf, d, p, st.o[d], found);
-    if constexpr (GUARD)
-        if (__any(found)) add_odd<T, D>(buf, seen, first, st);
+    for (int d = 0; d < Head<T, D>::kBlocks; ++d) block_product<T, D, GUARD>(buf, d, p, odd, st.o[d]);
+    if (odd) add_odd<T, D>(buf, seen, first, st);
 }
 
 // A row of q, as the B operand of the first product; zeros where there is no row.
@@ -599,7 +613,7 @@ struct FewRange {
                         s[0][i] = key < limit && at >= 0 ? s[0][i] : WHT_NEG_INF;
                     }
                 }
-                rebase<H, 1>(s, a.scale, st);
+                rebase<H, 1, 0>(s, a.scale, st);
                 weigh(s[0], a.scale, st);
                 if (more) wait_loads<kLoads>();
                 else wait_loads<0>();
@@ -728,24 +742,15 @@ struct ManyRange {
     static constexpr int kLoads = H::kChunks / 4;                   // of one wave for a quarter of 64 rows
     static constexpr int kTileBytes = kStepKeys * H::kRowBytes;
 
-    static __device__ __forceinline__ void issue(const AttentionArgs& a, const PageList& list, int first, int key0, int keys, const unsigned char* kbase,
-                                                 const unsigned char* vbase, unsigned kto, unsigned vto) {
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int n = (wave * kLoads + i) * 64 + lane, r = n / H::kChunks, p = n % H::kChunks;
-            const int64_t off = key_offset(a, list, first, key0 + r, keys);
-            load_to_lds(off >= 0 ? kbase + off + H::k_chunk(r, p) * 16 : zero_chunk, kto + (wave * kLoads + i) * 1024);
-            load_to_lds(off >= 0 ? vbase + off + H::v_chunk(r, p) * 16 : zero_chunk, vto + (wave * kLoads + i) * 1024);
-        }
-    }
-
-    // The pipeline, over steps [lo, hi) of pages that are all there, of 16 tokens at least: a wave's 16 of the 64 keys are in one page, and a lane's
-    // place in it is the same every step.  LDS: keys of even, of odd steps, values of even, of odd steps.
-    static __device__ __forceinline__ void stream(const AttentionArgs& a, const PageList& list, int first, int lo, int hi, const unsigned char* kbase,
-                                                  const unsigned char* vbase, unsigned buf, const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd, RowState<H>& st) {
+    // steps [lo, hi) of listed pages, `end` keys; limit: how many this lane's row sees, any_sees: any row of the wave; up to step `full` every row of the
+    // workgroup sees all.  LDS: keys of even, of odd steps, values of even, of odd steps.
+    static __device__ __forceinline__ void stream(const AttentionArgs& a, const PageList& list, int first, int lo, int hi, int end, int full, bool bad, int limit, int any_sees,
+                                                  const unsigned char* kbase, const unsigned char* vbase, unsigned buf, const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd,
+                                                  RowState<H>& st) {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const unsigned to = buf + wave * kLoads * 1024;
+        // Pages of 16 tokens at least, all there: a wave's 16 of the 64 keys are in one page, and a lane's place in it is the same every step.
+        const int simple = a.page_shift >= 4 && !bad ? end / kStepKeys : lo;               // steps before it are so, and have all their keys
         unsigned koff[kLoads], voff[kLoads];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -757,53 +762,84 @@ struct ManyRange {
             const int key = t * kStepKeys + wave * 16, page = __builtin_amdgcn_readfirstlane(list.page[(key >> a.page_shift) - first]);
             return (uint64_t)(unsigned)page * a.page_stride + (unsigned)(key & ((1 << a.page_shift) - 1)) * a.token_stride;
         };
-        auto load_k = [&](int t, uint64_t from) {
+        auto load_k = [&](int t) {
+            const unsigned char* from = kbase + place(t);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) load_to_lds(kbase + from, koff[i], to + (t & 1) * kTileBytes + i * 1024);
+            for (int i = 0; i < kLoads; ++i) load_to_lds(from, koff[i], to + (t & 1) * kTileBytes + i * 1024);
         };
-        auto load_v = [&](int t, uint64_t from) {
+        auto load_v = [&](int t) {
+            const unsigned char* from = vbase + place(t);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) load_to_lds(vbase + from, voff[i], to + (2 + (t & 1)) * kTileBytes + i * 1024);
+            for (int i = 0; i < kLoads; ++i) load_to_lds(from, voff[i], to + (2 + (t & 1)) * kTileBytes + i * 1024);
         };
-        uint64_t now = place(lo), next = place(min(lo + 1, hi - 1));
-        load_k(lo, now);
-        load_v(lo, now);
-        if (lo + 1 < hi) { load_k(lo + 1, next); wait_loads<2 * kLoads>(); }
-        else wait_loads<kLoads>();
-        workgroup_barrier();
+        // the same of any step
+        auto load_any = [&](int t, bool values) {
+            const unsigned at = to + ((values ? 2 : 0) + (t & 1)) * kTileBytes;
+            const unsigned char* base = values ? vbase : kbase;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int r = ((wave * kLoads + i) * 64 + lane) / H::kChunks;
+                const int64_t off = key_offset(a, list, first, t * kStepKeys + r, end);
+                const unsigned in_row = (values ? voff[i] : koff[i]) - (unsigned)(r - wave * 16) * a.token_stride;
+                load_to_lds(off >= 0 ? base + off + in_row : zero_chunk, at + i * 1024);
+            }
+        };
         auto score = [&](int t, f32x16 (&s)[2]) {
             const unsigned keys = fresh(buf + (t & 1) * kTileBytes);
             s[0] = scores<T, D>(keys, q);
             s[1] = scores<T, D>(keys + 32 * H::kRowBytes, q);
         };
-        auto use = [&](int t, f32x16 (&s)[2]) {
-            const unsigned values = fresh(buf + (2 + (t & 1)) * kTileBytes);
+        auto step = [&](int t, f32x16 (&s)[2], f32x16 (&ahead)[2]) {
+            wait_loads<0>();
+            workgroup_barrier();                                    // V of this step and K of the next have landed; what they replace next has been read
+            load_v(t + 1);
+            load_k(t + 2);
+            rebase<H, 2, 8>(s, a.scale, st);
+            score(t + 1, ahead);
             weigh(s[0], a.scale, st);
             weigh(s[1], a.scale, st);
+            const unsigned values = fresh(buf + (2 + (t & 1)) * kTileBytes);
             accumulate<T, D, false>(values, s[0], 0, odd, st);
             accumulate<T, D, false>(values + 32 * H::kRowBytes, s[1], 0, odd, st);
         };
-        auto step = [&](int t, f32x16 (&s)[2], f32x16 (&ahead)[2]) {        // t + 1 < hi
-            wait_loads<0>();
-            workgroup_barrier();                                    // V of this step and K of the next have landed; what they replace next has been read
-            load_v(t + 1, next);
-            if (t + 2 < hi) { next = place(t + 2); load_k(t + 2, next); }
-            rebase<H, 2>(s, a.scale, st);
-            score(t + 1, ahead);
-            use(t, s);
-        };
-        f32x16 s[2], other[2];
-        score(lo, s);
+
         int t = lo;
-        while (t + 1 < hi) {
-            step(t++, s, other);
-            if (t + 1 < hi) step(t++, other, s);
-            else { s[0] = other[0]; s[1] = other[1]; }
-        }
+        load_any(lo, false);
+        load_any(lo, true);
+        if (lo + 1 < hi) load_any(lo + 1, false);
         wait_loads<0>();
         workgroup_barrier();
-        rebase<H, 2>(s, a.scale, st);
-        use(t, s);
+        f32x16 s[2], other[2];
+        score(lo, s);
+        const int last = min(full, simple - 2);
+        while (t < last) {
+            step(t++, s, other);
+            if (t < last) step(t++, other, s);
+            else { s[0] = other[0]; s[1] = other[1]; }
+        }
+        for (; t < hi; ++t) {
+            const int key0 = t * kStepKeys;
+            wait_loads<0>();
+            workgroup_barrier();
+            if (t + 1 < hi) load_any(t + 1, true);
+            if (t + 2 < hi) load_any(t + 2, false);
+            if (t + 1 < hi) score(t + 1, other);
+            if (key0 < any_sees) {
+                if (t >= full) {
+                    hide(s[0], key0, limit, a, list, first);
+                    hide(s[1], key0 + 32, limit, a, list, first);
+                }
+                rebase<H, 2, 8>(s, a.scale, st);
+                const unsigned values = fresh(buf + (2 + (t & 1)) * kTileBytes);
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    weigh(s[n], a.scale, st);
+                    accumulate<T, D, true>(values + n * 32 * H::kRowBytes, s[n], limit - key0 - n * 32, odd, st);
+                }
+            }
+            s[0] = other[0];
+            s[1] = other[1];
+        }
     }
 
     // steps [t0, t1) of `table`'s `keys` tokens; limit: how many this lane's row sees; all_see: every row of the workgroup, any_sees: any row of the wave
@@ -815,35 +851,7 @@ struct ManyRange {
             const int hi = min(t1, lo + per_list), end = min(hi * kStepKeys, keys), first = (lo * kStepKeys) >> a.page_shift;
             list_pages(list, table + first, 0, ((end - 1) >> a.page_shift) - first + 1, a.pages);
             const bool bad = __builtin_amdgcn_readfirstlane(list.bad) != 0;
-            int from = lo;
-            if (!bad && a.page_shift >= 4 && min(hi, all_see / kStepKeys) > lo) {
-                from = min(hi, all_see / kStepKeys);
-                stream(a, list, first, lo, from, kbase, vbase, buf, q, odd, st);
-                if (from == hi) continue;
-                workgroup_barrier();                                // the pipeline's last reads are done
-            }
-            issue(a, list, first, from * kStepKeys, keys, kbase, vbase, buf, buf + kTileBytes);
-            for (int t = from; t < hi; ++t) {
-                const int key0 = t * kStepKeys, side = (t - from) & 1;
-                wait_loads<0>();
-                workgroup_barrier();                                // everyone's loads of this step have landed, everyone's reads of the last are done
-                const unsigned other = buf + (side ^ 1) * 2 * kTileBytes;
-                if (t + 1 < hi) issue(a, list, first, key0 + kStepKeys, keys, kbase, vbase, other, other + kTileBytes);
-                if (key0 < any_sees) {
-                    const unsigned here = fresh(buf + side * 2 * kTileBytes);
-                    f32x16 s[2] = {scores<T, D>(here, q), scores<T, D>(here + 32 * H::kRowBytes, q)};
-                    if (bad || key0 + kStepKeys > all_see) {
-                        hide(s[0], key0, limit, a, list, first);
-                        hide(s[1], key0 + 32, limit, a, list, first);
-                    }
-                    rebase<H, 2>(s, a.scale, st);
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        weigh(s[n], a.scale, st);
-                        accumulate<T, D, true>(here + kTileBytes + n * 32 * H::kRowBytes, s[n], limit - key0 - n * 32, odd, st);
-                    }
-                }
-            }
+            stream(a, list, first, lo, hi, end, bad ? lo : all_see / kStepKeys, bad, limit, any_sees, kbase, vbase, buf, q, odd, st);
         }
     }
 };
