@@ -310,26 +310,22 @@ struct KeyReads {                                                   // a lane re
     }
 };
 
+template <class T>
+__device__ __forceinline__ f32x16 score_step(u32x4 k, u32x4 q, f32x16 s) {
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q), s, 0, 0, 0);
+    const f32x4 kf = __builtin_bit_cast(f32x4, k), qf = __builtin_bit_cast(f32x4, q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[i], qf[i], s, 0, 0, 0);
+    return s;
+}
+
 // S^T of 32 keys in LDS at `buf` (16-byte aligned rows) and the wave's rows.
 template <class T, int D>
 __device__ __forceinline__ f32x16 scores(unsigned buf, const u32x4 (&q)[Head<T, D>::kSteps]) {
-    using H = Head<T, D>;
-    using R = KeyReads<T, D>;
-    const unsigned first = R::first(buf);
-    f32x16 s;
+    const unsigned first = KeyReads<T, D>::first(buf);
+    f32x16 s{};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < H::kSteps; ++c) {
-        const u32x4 k = lds_read<u32x4>(R::chunk(first, c));
-        if constexpr (!H::kF32) {
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[c]), s, 0, 0, 0);
-        } else {
-            const f32x4 kf = __builtin_bit_cast(f32x4, k), qf = __builtin_bit_cast(f32x4, q[c]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[i], qf[i], s, 0, 0, 0);
-        }
-    }
+    for (int c = 0; c < Head<T, D>::kSteps; ++c) s = score_step<T>(lds_read<u32x4>(KeyReads<T, D>::chunk(first, c)), q[c], s);
     return s;
 }
 
@@ -341,13 +337,8 @@ __device__ __forceinline__ int key_of(int i) { return (i >> 2) * 8 + ((threadIdx
 // one multiplies all the sums over.  Weights are up to 256 then, which float32 sums hold as exactly; but the largest of a row is no longer
 // 1, which bfloat16 holds exactly: the error of the outputs, with that of their own rounding, goes from 1.9e-3 to 2.3e-3 of their norm.
 // With few rows, bound by memory, it is 0.
-template <class H, int NS, int SLACK>
-__device__ __forceinline__ void rebase(const f32x16 (&s)[NS], float scale, RowState<H>& st) {
-    float mx = s[0][0];
-#pragma unroll
-    for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
+template <class H, int SLACK>
+__device__ __forceinline__ void rebase(float mx, float scale, RowState<H>& st) {
     mx = fmaxf(mx, other_half(mx)) * scale;
     if (__any(mx > st.m + (float)SLACK || (st.m == WHT_NEG_INF && mx > WHT_NEG_INF))) {
         const float now = fmaxf(st.m, mx);
@@ -359,6 +350,12 @@ __device__ __forceinline__ void rebase(const f32x16 (&s)[NS], float scale, RowSt
             for (int i = 0; i < 16; ++i) st.o[d][i] *= f;
         st.m = now;
     }
+}
+__device__ __forceinline__ float largest(const f32x16& s) {
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    return mx;
 }
 
 // Scores become weights, and their sum.
@@ -382,29 +379,35 @@ __device__ __forceinline__ bf16x8 finite(bf16x8 v) {
     return __builtin_bit_cast(bf16x8, x);
 }
 
+// The A operand of the second product in bfloat16: 16 of 32 values in LDS at `buf` (ks: which), 32 columns from 32 d on.  A transposing read gives
+// lane i of 16 the i-th of 16 columns, four rows of it, that the 16 lanes address as 4 x 4 pieces of 8 bytes.
+template <int D>
+__device__ __forceinline__ bf16x8 values(unsigned buf, int ks, int d) {
+    using H = Head<bf16, D>;
+    const int lane = threadIdx.x & 63, g = lane >> 4, in = lane & 15, row = (g >> 1) * 4 + (in >> 2), c = (g & 1) * 2 + ((in & 3) >> 1);
+    const unsigned at = (H::kChunks & (H::kChunks - 1)) == 0 ? (buf + row * H::kRowBytes + H::v_place(row, c) * 16 + (in & 1) * 8) ^ (d * 64)
+                                                             : buf + row * H::kRowBytes + H::v_place(row, d * 4 + c) * 16 + (in & 1) * 8;
+    bf16x8 v;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)(at + (ks * 16 + e * 8) * H::kRowBytes));
+        const bf16x4 y = __builtin_bit_cast(bf16x4, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[e * 4 + i] = y[i];
+    }
+    return v;
+}
+
 // o += (V^T P^T) over 32 keys in LDS at `buf`, for the 32 columns of V from 32 d on.  GUARD: where `odd`, values that are not finite stay out.
 template <class T, int D, bool GUARD>
 __device__ __forceinline__ void block_product(unsigned buf, int d, const f32x16& p, bool odd, f32x16& o) {
     using H = Head<T, D>;
-    const int lane = threadIdx.x & 63;
-    constexpr bool kFlip = (H::kChunks & (H::kChunks - 1)) == 0;
     if constexpr (!H::kF32) {
-        // a transposing read gives lane i of 16 the i-th of 16 columns, four rows of it, that the 16 lanes address as 4 x 4 pieces of 8 bytes
-        const int g = lane >> 4, in = lane & 15, row = (g >> 1) * 4 + (in >> 2), c = (g & 1) * 2 + ((in & 3) >> 1);
-        const unsigned at = kFlip ? (buf + row * H::kRowBytes + H::v_place(row, c) * 16 + (in & 1) * 8) ^ (d * 64)
-                                  : buf + row * H::kRowBytes + H::v_place(row, d * 4 + c) * 16 + (in & 1) * 8;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 v, w;
+            bf16x8 v = values<D>(buf, ks, d), w;
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = (bf16)p[ks * 8 + i];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)(at + (ks * 16 + e * 8) * H::kRowBytes));
-                const bf16x4 y = __builtin_bit_cast(bf16x4, x);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[e * 4 + i] = y[i];
-            }
             if constexpr (GUARD)
                 if (odd) {
                     asm volatile("");                               // a branch: not computed where it is not needed
@@ -413,7 +416,8 @@ __device__ __forceinline__ void block_product(unsigned buf, int d, const f32x16&
             o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, o, 0, 0, 0);
         }
     } else {
-        const int col = lane & 31, h4 = (lane >> 5) * 4;
+        constexpr bool kFlip = (H::kChunks & (H::kChunks - 1)) == 0;
+        const int lane = threadIdx.x & 63, col = lane & 31, h4 = (lane >> 5) * 4;
         const unsigned at = kFlip ? (buf + h4 * H::kRowBytes + H::v_place(h4, col >> 2) * 16 + (col & 3) * 4) ^ (d * 128)
                                   : buf + h4 * H::kRowBytes + H::v_place(h4, d * 8 + (col >> 2)) * 16 + (col & 3) * 4;
 #pragma unroll
@@ -613,7 +617,7 @@ struct FewRange {
                         s[0][i] = key < limit && at >= 0 ? s[0][i] : WHT_NEG_INF;
                     }
                 }
-                rebase<H, 1, 0>(s, a.scale, st);
+                rebase<H, 0>(largest(s[0]), a.scale, st);
                 weigh(s[0], a.scale, st);
                 if (more) wait_loads<kLoads>();
                 else wait_loads<0>();
@@ -733,8 +737,9 @@ __device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shar
 
 // ------------------------------------------------------------------------------------------------
 // Many rows: a workgroup takes 128 rows, 32 per wave, and all its waves the same 64 keys a step; keys and values lie in LDS twice over, the
-// next steps' in flight.  Steps that every row sees all of run as a pipeline: the products with the next step's keys stand
-// beside this step's exponentials, so that the matrix units have work while the vector units do.
+// next steps' in flight.  A wave takes 32 keys at a time, as a pipeline: the products with the next 32 keys stand beside the exponentials of
+// these, those with their values beside the next ones' maximum, and every fragment is read from LDS as many products ahead as there are in one of the two,
+// into the registers of the one just used.  Per 32 keys 128 wide: 16 matrix instructions of 32 cycles, 60 vector instructions of 4 and 16 exponentials of 16.
 
 template <class T, int D>
 struct ManyRange {
@@ -784,23 +789,57 @@ struct ManyRange {
                 load_to_lds(off >= 0 ? base + off + in_row : zero_chunk, at + i * 1024);
             }
         };
-        auto score = [&](int t, f32x16 (&s)[2]) {
-            const unsigned keys = fresh(buf + (t & 1) * kTileBytes);
-            s[0] = scores<T, D>(keys, q);
-            s[1] = scores<T, D>(keys + 32 * H::kRowBytes, q);
+        // a fragment of keys or values of the first or second 32 of step t
+        auto keys_at = [&](int t, int half) { return fresh(buf + (t & 1) * kTileBytes + half * 32 * H::kRowBytes); };
+        auto values_at = [&](int t, int half) { return fresh(buf + (2 + (t & 1)) * kTileBytes + half * 32 * H::kRowBytes); };
+        u32x4 frag[H::kSteps];                                      // keys of the 32 after those whose scores are at hand
+        auto read_keys = [&](unsigned at) {
+            const unsigned first_chunk = KeyReads<T, D>::first(at);
+#pragma unroll
+            for (int i = 0; i < H::kSteps; ++i) frag[i] = lds_read<u32x4>(KeyReads<T, D>::chunk(first_chunk, i));
         };
-        auto step = [&](int t, f32x16 (&s)[2], f32x16 (&ahead)[2]) {
-            wait_loads<0>();
-            workgroup_barrier();                                    // V of this step and K of the next have landed; what they replace next has been read
-            load_v(t + 1);
-            load_k(t + 2);
-            rebase<H, 2, 8>(s, a.scale, st);
-            score(t + 1, ahead);
-            weigh(s[0], a.scale, st);
-            weigh(s[1], a.scale, st);
-            const unsigned values = fresh(buf + (2 + (t & 1)) * kTileBytes);
-            accumulate<T, D, false>(values, s[0], 0, odd, st);
-            accumulate<T, D, false>(values + 32 * H::kRowBytes, s[1], 0, odd, st);
+        // The weights of `s` and their products with the values at `vat`; the scores `ahead` of the keys in `frag`, which becomes those at `kat`.
+        auto half_step = [&](f32x16& s, f32x16& ahead, unsigned vat, unsigned kat) {
+            if constexpr (!H::kF32) {
+                const float base = st.m == WHT_NEG_INF ? 0.0f : st.m;
+                const unsigned first_chunk = KeyReads<T, D>::first(kat);
+                bf16x8 w[2];
+                float sum[2] = {0.0f, 0.0f};
+                ahead = f32x16{};
+#pragma unroll
+                for (int i = 0; i < H::kSteps; ++i) {
+                    ahead = score_step<T>(frag[i], q[i], ahead);
+                    frag[i] = __builtin_bit_cast(u32x4, values<D>(vat, i / H::kBlocks, i % H::kBlocks));
+#pragma unroll
+                    for (int e = 16 * i / H::kSteps; e < 16 * (i + 1) / H::kSteps; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale, -base));
+                        sum[e & 1] += p;
+                        w[e >> 3][e & 7] = (bf16)p;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                float mx = WHT_NEG_INF;
+#pragma unroll
+                for (int i = 0; i < H::kSteps; ++i) {
+                    st.o[i % H::kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, frag[i]), w[i / H::kBlocks], st.o[i % H::kBlocks], 0, 0, 0);
+                    frag[i] = lds_read<u32x4>(KeyReads<T, D>::chunk(first_chunk, i));
+                    // the last of `ahead` is a few instructions old
+                    if (i >= H::kSteps / 2)
+#pragma unroll
+                        for (int e = 16 * (2 * i - H::kSteps) / H::kSteps; e < 16 * (2 * i - H::kSteps + 2) / H::kSteps; ++e) mx = fmaxf(mx, ahead[e]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                st.l += sum[0] + sum[1];
+                rebase<H, 8>(mx, a.scale, st);
+            } else {
+                ahead = f32x16{};
+#pragma unroll
+                for (int i = 0; i < H::kSteps; ++i) ahead = score_step<T>(frag[i], q[i], ahead);
+                weigh(s, a.scale, st);
+                accumulate<T, D, false>(vat, s, 0, odd, st);
+                read_keys(kat);
+                rebase<H, 8>(largest(ahead), a.scale, st);
+            }
         };
 
         int t = lo;
@@ -809,36 +848,43 @@ struct ManyRange {
         if (lo + 1 < hi) load_any(lo + 1, false);
         wait_loads<0>();
         workgroup_barrier();
-        f32x16 s[2], other[2];
-        score(lo, s);
-        const int last = min(full, simple - 2);
-        while (t < last) {
-            step(t++, s, other);
-            if (t < last) step(t++, other, s);
-            else { s[0] = other[0]; s[1] = other[1]; }
+        f32x16 s = scores<T, D>(keys_at(lo, 0), q), other;
+        if (lo >= full) hide(s, lo * kStepKeys, limit, a, list, first);
+        rebase<H, 8>(largest(s), a.scale, st);
+        read_keys(keys_at(lo, 1));
+        for (const int last = min(full, simple - 1) - 1; t < last; ++t) {       // this step and the next are seen by all, the one after is simple
+            wait_loads<0>();
+            workgroup_barrier();                                    // V of this step and K of the next have landed; what they replace next has been read
+            load_v(t + 1);
+            load_k(t + 2);
+            half_step(s, other, values_at(t, 0), keys_at(t + 1, 0));
+            half_step(other, s, values_at(t, 1), keys_at(t + 1, 1));
         }
         for (; t < hi; ++t) {
-            const int key0 = t * kStepKeys;
             wait_loads<0>();
             workgroup_barrier();
             if (t + 1 < hi) load_any(t + 1, true);
             if (t + 2 < hi) load_any(t + 2, false);
-            if (t + 1 < hi) score(t + 1, other);
-            if (key0 < any_sees) {
-                if (t >= full) {
-                    hide(s[0], key0, limit, a, list, first);
-                    hide(s[1], key0 + 32, limit, a, list, first);
-                }
-                rebase<H, 2, 8>(s, a.scale, st);
-                const unsigned values = fresh(buf + (2 + (t & 1)) * kTileBytes);
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                const int key0 = t * kStepKeys + half * 32, next = key0 + 32;
+                const bool more = half == 0 || t + 1 < hi;
+                if (more) {
+                    other = f32x16{};
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    weigh(s[n], a.scale, st);
-                    accumulate<T, D, true>(values + n * 32 * H::kRowBytes, s[n], limit - key0 - n * 32, odd, st);
+                    for (int i = 0; i < H::kSteps; ++i) other = score_step<T>(frag[i], q[i], other);
+                }
+                if (key0 < any_sees) {
+                    weigh(s, a.scale, st);
+                    accumulate<T, D, true>(values_at(t, half), s, limit - key0, odd, st);
+                }
+                if (more) {
+                    if (t + 1 < hi) read_keys(keys_at(t + 1, half));
+                    if (next >= full * kStepKeys) hide(other, next, limit, a, list, first);
+                    rebase<H, 8>(largest(other), a.scale, st);
+                    s = other;
                 }
             }
-            s[0] = other[0];
-            s[1] = other[1];
         }
     }
 
