@@ -502,42 +502,6 @@ __device__ __forceinline__ void load_row(const unsigned char* p, bool there, u32
     }
 }
 
-// The pages of up to kListed * page_size keys at a time, in LDS; -1 where a number names no page.
-constexpr int kListed = 512;
-struct PageList { int page[kListed + 4]; int bad; };
-
-__device__ __forceinline__ void list_pages(PageList& list, const int* table, int first, int count, int pages) {
-    __syncthreads();                                                // the last use of the list is over
-    if (threadIdx.x == 0) list.bad = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < count; i += 256) {
-        const int page = table[first + i];
-        const bool good = page >= 0 && page < pages;
-        list.page[i] = good ? page : -1;
-        if (!good) list.bad = 1;
-    }
-    __syncthreads();
-}
-
-// Where key `key` of a table's tokens stands relative to the cache's start; -1 where it is not there.
-__device__ __forceinline__ int64_t key_offset(const AttentionArgs& a, const PageList& list, int first, int key, int keys) {
-    if (key >= keys) return -1;
-    const int page = list.page[(key >> a.page_shift) - first];
-    if (page < 0) return -1;
-    return (int64_t)((uint64_t)(unsigned)page * a.page_stride + (unsigned)(key & ((1 << a.page_shift) - 1)) * a.token_stride);
-}
-
-__device__ __forceinline__ void hide(f32x16& s, int key0, int limit, const AttentionArgs& a, const PageList& list, int first) {
-    const bool bad = list.bad != 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int key = key0 + key_of(i);
-        bool seen = key < limit;
-        if (bad && seen) seen = list.page[(key >> a.page_shift) - first] >= 0;
-        s[i] = seen ? s[i] : WHT_NEG_INF;
-    }
-}
-
 // ------------------------------------------------------------------------------------------------
 // Few rows (decoding): memory-bound.  Every wave works by itself, through LDS slots of its own, without a barrier: V of a block of 32 keys is in flight
 // while its scores are formed, K of the next one while V is used.  All (sequence, head) items' blocks form one line that the grid's
@@ -637,6 +601,9 @@ __device__ __forceinline__ int item_blocks(const AttentionArgs& a, int b) {
     const Sequence s = sequence(a.batch, b);
     return s.queries > 0 ? front + ceil_div(s.length, kBlockKeys) : 0;
 }
+
+constexpr int kListed = 512;        // pages that a workgroup of the many-rows kernel has in LDS at a time; -1 where a number names none
+struct PageList { int page[kListed]; int bad[4]; };
 
 // What a workgroup of either kernel has in LDS.
 template <class T, int D>
@@ -741,21 +708,40 @@ __device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shar
 // these, those with their values beside the next ones' maximum, and every fragment is read from LDS as many products ahead as there are in one of the two,
 // into the registers of the one just used.  Per 32 keys 128 wide: 16 matrix instructions of 32 cycles, 60 vector instructions of 4 and 16 exponentials of 16.
 
+// The keys of one item: the prefix's first, then the sequence's.  Steps of 64 keys count through both (front: the first of the sequence's), so that a step's
+// keys are of one of them.
+struct Keys {
+    const int *prefix_table, *own_table;
+    int front, prefix, own;             // own: of the sequence, those that any row of the workgroup sees
+};
+
 template <class T, int D>
 struct ManyRange {
     using H = Head<T, D>;
     static constexpr int kLoads = H::kChunks / 4;                   // of one wave for a quarter of 64 rows
     static constexpr int kTileBytes = kStepKeys * H::kRowBytes;
 
-    // steps [lo, hi) of listed pages, `end` keys; limit: how many this lane's row sees, any_sees: any row of the wave; up to step `full` every row of the
-    // workgroup sees all.  LDS: keys of even, of odd steps, values of even, of odd steps.
-    static __device__ __forceinline__ void stream(const AttentionArgs& a, const PageList& list, int first, int lo, int hi, int end, int full, bool bad, int limit, int any_sees,
+    // steps [lo, hi), whose pages fit the list; limit: how many of the sequence's keys this lane's row sees, all_see, any_sees: every, any row of the wave
+    // (-1: it has none).  LDS: keys of even, of odd steps, values of even, of odd steps.
+    static __device__ __forceinline__ void stream(const AttentionArgs& a, const Keys& k, PageList& list, int lo, int hi, int limit, int all_see, int any_sees,
                                                   const unsigned char* kbase, const unsigned char* vbase, unsigned buf, const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd,
                                                   RowState<H>& st) {
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), shift = a.page_shift;
+        // the list: pages of the prefix's keys in these steps, then of the sequence's; a key's page is at (key >> shift) + the part's offset
+        const int pre0 = min(lo, k.front) * kStepKeys, pre1 = min(min(hi, k.front) * kStepKeys, k.prefix);
+        const int own0 = max(lo - k.front, 0) * kStepKeys, own1 = min(max(hi - k.front, 0) * kStepKeys, k.own);
+        const int pre_pages = pre1 > pre0 ? ((pre1 - 1) >> shift) - (pre0 >> shift) + 1 : 0, own_pages = own1 > own0 ? ((own1 - 1) >> shift) - (own0 >> shift) + 1 : 0;
+        const int pre_at = -(pre0 >> shift), own_at = pre_pages - (own0 >> shift);
+        bool wrong = false;
+        for (int i = threadIdx.x; i < pre_pages + own_pages; i += 256) {
+            const int page = i < pre_pages ? k.prefix_table[i - pre_at] : k.own_table[i - own_at];
+            const bool good = page >= 0 && page < a.pages;
+            list.page[i] = good ? page : -1;
+            wrong |= !good;
+        }
+        wrong = __any(wrong);
+        if (lane == 0) list.bad[wave] = wrong;
         const unsigned to = buf + wave * kLoads * 1024;
-        // Pages of 16 tokens at least, all there: a wave's 16 of the 64 keys are in one page, and a lane's place in it is the same every step.
-        const int simple = a.page_shift >= 4 && !bad ? end / kStepKeys : lo;               // steps before it are so, and have all their keys
         unsigned koff[kLoads], voff[kLoads];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -763,43 +749,60 @@ struct ManyRange {
             koff[i] = (unsigned)(r - wave * 16) * a.token_stride + H::k_chunk(r, p) * 16;
             voff[i] = (unsigned)(r - wave * 16) * a.token_stride + H::v_chunk(r, p) * 16;
         }
-        auto place = [&](int t) {
-            const int key = t * kStepKeys + wave * 16, page = __builtin_amdgcn_readfirstlane(list.page[(key >> a.page_shift) - first]);
-            return (uint64_t)(unsigned)page * a.page_stride + (unsigned)(key & ((1 << a.page_shift) - 1)) * a.token_stride;
-        };
-        auto load_k = [&](int t) {
-            const unsigned char* from = kbase + place(t);
+        __syncthreads();
+        const bool bad = __builtin_amdgcn_readfirstlane(list.bad[0] | list.bad[1] | list.bad[2] | list.bad[3]) != 0;
+
+        // Loads of a step.  Where its keys are all there, in pages of 16 tokens at least, a wave's 16 of the 64 are in one page, and a lane's place in
+        // it is the same every step.
+        auto load = [&](int t, const unsigned char* base, const unsigned (&off)[kLoads], unsigned at) {
+            const bool own = t >= k.front;
+            const int key0 = (own ? t - k.front : t) * kStepKeys, keys = own ? k.own : k.prefix, list_at = own ? own_at : pre_at;
+            if (!bad && shift >= 4 && key0 + kStepKeys <= keys) {
+                const int key = key0 + wave * 16, page = __builtin_amdgcn_readfirstlane(list.page[(key >> shift) + list_at]);
+                const unsigned char* from = base + ((uint64_t)(unsigned)page * a.page_stride + (unsigned)(key & ((1 << shift) - 1)) * a.token_stride);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) load_to_lds(from, koff[i], to + (t & 1) * kTileBytes + i * 1024);
-        };
-        auto load_v = [&](int t) {
-            const unsigned char* from = vbase + place(t);
+                for (int i = 0; i < kLoads; ++i) load_to_lds(from, off[i], at + i * 1024);
+            } else {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) load_to_lds(from, voff[i], to + (2 + (t & 1)) * kTileBytes + i * 1024);
-        };
-        // the same of any step
-        auto load_any = [&](int t, bool values) {
-            const unsigned at = to + ((values ? 2 : 0) + (t & 1)) * kTileBytes;
-            const unsigned char* base = values ? vbase : kbase;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int r = ((wave * kLoads + i) * 64 + lane) / H::kChunks;
-                const int64_t off = key_offset(a, list, first, t * kStepKeys + r, end);
-                const unsigned in_row = (values ? voff[i] : koff[i]) - (unsigned)(r - wave * 16) * a.token_stride;
-                load_to_lds(off >= 0 ? base + off + in_row : zero_chunk, at + i * 1024);
+                for (int i = 0; i < kLoads; ++i) {
+                    const int r = ((wave * kLoads + i) * 64 + lane) / H::kChunks, key = key0 + r;
+                    const int page = key < keys ? list.page[(key >> shift) + list_at] : -1;
+                    const uint64_t from = (uint64_t)(unsigned)page * a.page_stride + (unsigned)(key & ((1 << shift) - 1)) * a.token_stride;
+                    load_to_lds(page >= 0 ? base + from + (off[i] - (unsigned)(r - wave * 16) * a.token_stride) : zero_chunk, at + i * 1024);
+                }
             }
         };
-        // a fragment of keys or values of the first or second 32 of step t
+        auto load_k = [&](int t) { load(t, kbase, koff, to + (t & 1) * kTileBytes); };
+        auto load_v = [&](int t) { load(t, vbase, voff, to + (2 + (t & 1)) * kTileBytes); };
+        // the first or second 32 keys or values of step t
         auto keys_at = [&](int t, int half) { return fresh(buf + (t & 1) * kTileBytes + half * 32 * H::kRowBytes); };
         auto values_at = [&](int t, int half) { return fresh(buf + (2 + (t & 1)) * kTileBytes + half * 32 * H::kRowBytes); };
-        u32x4 frag[H::kSteps];                                      // keys of the 32 after those whose scores are at hand
+
+        // Blocks of 32 keys count as steps do.  What all rows of the wave see all of; the scores of what they do not, hidden.
+        const int front = 2 * k.front, pre_full = any_sees < 0 ? 0 : k.prefix / 32, own_full = any_sees < 0 ? 0 : all_see / 32;
+        auto full = [&](int j) { return j < front ? j < pre_full : j - front < own_full; };
+        auto hide = [&](f32x16& s, int j) {
+            const bool own = j >= front;
+            const int key0 = (own ? j - front : j) * 32, sees = own ? limit : k.prefix, list_at = own ? own_at : pre_at;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int key = key0 + key_of(i);
+                bool seen = key < sees;
+                if (bad && seen) seen = list.page[(key >> shift) + list_at] >= 0;
+                s[i] = seen ? s[i] : WHT_NEG_INF;
+            }
+        };
+        auto seen_in = [&](int j) { return j < front ? k.prefix - j * 32 : limit - (j - front) * 32; };          // of block j, by this lane's row
+        auto in_sight = [&](int j) { return j < front ? any_sees >= 0 : (j - front) * 32 < any_sees; };
+
+        u32x4 frag[H::kSteps];                                      // keys of the block after the one whose scores are at hand
         auto read_keys = [&](unsigned at) {
             const unsigned first_chunk = KeyReads<T, D>::first(at);
 #pragma unroll
             for (int i = 0; i < H::kSteps; ++i) frag[i] = lds_read<u32x4>(KeyReads<T, D>::chunk(first_chunk, i));
         };
         // The weights of `s` and their products with the values at `vat`; the scores `ahead` of the keys in `frag`, which becomes those at `kat`.
-        auto half_step = [&](f32x16& s, f32x16& ahead, unsigned vat, unsigned kat) {
+        auto full_block = [&](f32x16& s, f32x16& ahead, unsigned vat, unsigned kat) {
             if constexpr (!H::kF32) {
                 const float base = st.m == WHT_NEG_INF ? 0.0f : st.m;
                 const unsigned first_chunk = KeyReads<T, D>::first(kat);
@@ -841,46 +844,46 @@ struct ManyRange {
                 rebase<H, 8>(largest(ahead), a.scale, st);
             }
         };
-
-        int t = lo;
-        load_any(lo, false);
-        load_any(lo, true);
-        if (lo + 1 < hi) load_any(lo + 1, false);
+        load_k(lo);
+        load_v(lo);
+        if (lo + 1 < hi) load_k(lo + 1);
         wait_loads<0>();
         workgroup_barrier();
         f32x16 s = scores<T, D>(keys_at(lo, 0), q), other;
-        if (lo >= full) hide(s, lo * kStepKeys, limit, a, list, first);
+        if (bad || !full(2 * lo)) hide(s, 2 * lo);
         rebase<H, 8>(largest(s), a.scale, st);
         read_keys(keys_at(lo, 1));
-        for (const int last = min(full, simple - 1) - 1; t < last; ++t) {       // this step and the next are seen by all, the one after is simple
-            wait_loads<0>();
-            workgroup_barrier();                                    // V of this step and K of the next have landed; what they replace next has been read
-            load_v(t + 1);
-            load_k(t + 2);
-            half_step(s, other, values_at(t, 0), keys_at(t + 1, 0));
-            half_step(other, s, values_at(t, 1), keys_at(t + 1, 1));
-        }
-        for (; t < hi; ++t) {
+        // A step's barrier stands in both loops below: a wave takes a step in either, whatever the others do.
+        for (int t = lo; t < hi; ++t) {
+            // steps whose blocks, and the first of the next one, are seen by all rows of the wave
+            const int blocks = 2 * t >= front || pre_full == front ? front + own_full : pre_full;
+            for (const int end = bad ? t : min(hi - 1, (blocks - 1) / 2); t < end; ++t) {
+                wait_loads<0>();
+                workgroup_barrier();                                // V of this step and K of the next have landed; what they replace next has been read
+                load_v(t + 1);
+                if (t + 2 < hi) load_k(t + 2);
+                full_block(s, other, values_at(t, 0), keys_at(t + 1, 0));
+                full_block(other, s, values_at(t, 1), keys_at(t + 1, 1));
+            }
             wait_loads<0>();
             workgroup_barrier();
-            if (t + 1 < hi) load_any(t + 1, true);
-            if (t + 2 < hi) load_any(t + 2, false);
+            if (t + 1 < hi) load_v(t + 1);
+            if (t + 2 < hi) load_k(t + 2);
 #pragma unroll 1
             for (int half = 0; half < 2; ++half) {
-                const int key0 = t * kStepKeys + half * 32, next = key0 + 32;
-                const bool more = half == 0 || t + 1 < hi;
+                const int j = 2 * t + half;
+                if (!in_sight(j)) break;                            // nor is any that follows
+                const bool more = j + 1 < 2 * hi && in_sight(j + 1);
                 if (more) {
                     other = f32x16{};
 #pragma unroll
                     for (int i = 0; i < H::kSteps; ++i) other = score_step<T>(frag[i], q[i], other);
                 }
-                if (key0 < any_sees) {
-                    weigh(s, a.scale, st);
-                    accumulate<T, D, true>(values_at(t, half), s, limit - key0, odd, st);
-                }
+                weigh(s, a.scale, st);
+                accumulate<T, D, true>(values_at(t, half), s, seen_in(j), odd, st);
                 if (more) {
                     if (t + 1 < hi) read_keys(keys_at(t + 1, half));
-                    if (next >= full * kStepKeys) hide(other, next, limit, a, list, first);
+                    if (bad || !full(j + 1)) hide(other, j + 1);
                     rebase<H, 8>(largest(other), a.scale, st);
                     s = other;
                 }
@@ -888,16 +891,13 @@ struct ManyRange {
         }
     }
 
-    // steps [t0, t1) of `table`'s `keys` tokens; limit: how many this lane's row sees; all_see: every row of the workgroup, any_sees: any row of the wave
-    static __device__ __forceinline__ void run(const AttentionArgs& a, PageList& list, const int* table, int t0, int t1, int keys, int limit, int all_see, int any_sees,
-                                               const unsigned char* kbase, const unsigned char* vbase, unsigned buf,
-                                               const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd, RowState<H>& st) {
-        const int per_list = (kListed << a.page_shift) / kStepKeys;
+    static __device__ __forceinline__ void run(const AttentionArgs& a, const Keys& k, PageList& list, int t0, int t1, int limit, int all_see, int any_sees,
+                                               const unsigned char* kbase, const unsigned char* vbase, unsigned buf, const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd,
+                                               RowState<H>& st) {
+        const int per_list = max(((kListed - 4) << a.page_shift) / kStepKeys, 1);           // each part may begin and end within a page
         for (int lo = t0; lo < t1; lo += per_list) {
-            const int hi = min(t1, lo + per_list), end = min(hi * kStepKeys, keys), first = (lo * kStepKeys) >> a.page_shift;
-            list_pages(list, table + first, 0, ((end - 1) >> a.page_shift) - first + 1, a.pages);
-            const bool bad = __builtin_amdgcn_readfirstlane(list.bad) != 0;
-            stream(a, list, first, lo, hi, end, bad ? lo : all_see / kStepKeys, bad, limit, any_sees, kbase, vbase, buf, q, odd, st);
+            if (lo > t0) workgroup_barrier();                       // the last steps' reads are done
+            stream(a, k, list, lo, min(t1, lo + per_list), limit, all_see, any_sees, kbase, vbase, buf, q, odd, st);
         }
     }
 };
@@ -942,7 +942,7 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
     auto& buf = shared.buf;
     auto& list = shared.list;
     auto& odd = shared.odd;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int B = a.stacked ? 1 : a.batch.B;
     // Workgroups go to the 8 dies in turn: a die takes whole groups (a sequence's head and share of its keys), so that their keys are in its L2
     // once, tile after tile, the tiles that see most first.
@@ -966,21 +966,15 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
     // own tokens that row r of the tile sees: length - queries + its token + 1
     auto sees = [&](int64_t r) { return a.stacked ? 0 : min(max(s.length - s.queries + (int)(min(r, rows - 1) / a.G) + 1, 0), s.length); };
     const int keys = sees(tile * kTileRows + kTileRows - 1);
-    const int limit = sees(row), all_see = sees((int64_t)tile * kTileRows), any_sees = row0 < rows ? sees(row0 + 31) : 0;
+    const int limit = sees(row), all_see = sees(row0), any_sees = row0 < rows ? sees(row0 + 31) : -1;
     const int front = a.use_prefix ? ceil_div(a.prefix, kStepKeys) : 0;
     const int total = front + ceil_div(keys, kStepKeys), per = ceil_div(total, a.splits);
     const int t0 = min(total, split * per), t1 = min(total, t0 + per);
     RowState<H> st;
     st.clear();
     const unsigned char *kbase = a.k + head * a.head_stride, *vbase = a.v + head * a.head_stride;
-    const unsigned at = __builtin_amdgcn_readfirstlane(lds_address(buf));
-#pragma unroll 1
-    for (int own = 0; own < 2; ++own) {                             // the prefix, the sequence
-        const int lo = own ? max(t0 - front, 0) : t0, hi = own ? t1 - front : min(t1, front);
-        if (lo >= hi) continue;
-        R::run(a, list, own ? a.batch.table + b * a.batch.table_stride : a.prefix_table, lo, hi, own ? keys : a.prefix, own ? limit : a.prefix,
-               own ? all_see : a.prefix, own ? any_sees : row0 < rows ? a.prefix : 0, kbase, vbase, at, q, odd[wave], st);
-    }
+    const Keys k{a.prefix_table, a.batch.table + b * a.batch.table_stride, front, a.use_prefix ? a.prefix : 0, keys};
+    R::run(a, k, list, t0, t1, limit, all_see, any_sees, kbase, vbase, __builtin_amdgcn_readfirstlane(lds_address(buf)), q, odd[wave], st);
     if (!there) return;
     st.l += other_half(st.l);
     const int64_t t = s.first + token;
