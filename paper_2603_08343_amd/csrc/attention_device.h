@@ -595,12 +595,12 @@ struct FewRange {
     }
 };
 
-__device__ __forceinline__ int item_blocks(const AttentionArgs& a, int b) {
-    if (b >= a.batch.B) return ceil_div(a.prefix, kBlockKeys);      // the front
-    const int front = a.use_prefix ? ceil_div(a.prefix, kBlockKeys) : 0;
-    const Sequence s = sequence(a.batch, b);
-    return s.queries > 0 ? front + ceil_div(s.length, kBlockKeys) : 0;
+__device__ __forceinline__ int blocks_of(const AttentionArgs& a, const Sequence& s) {
+    return s.queries > 0 ? (a.use_prefix ? ceil_div(a.prefix, kBlockKeys) : 0) + ceil_div(s.length, kBlockKeys) : 0;
 }
+// The line's b-th sequence; the one past the last stands for the front, the rows of all of them.
+__device__ __forceinline__ Sequence line_sequence(const AttentionArgs& a, int b) { return b < a.batch.B ? sequence(a.batch, b) : Sequence{0, a.batch.T, 0}; }
+__device__ __forceinline__ int line_blocks(const AttentionArgs& a, int b, const Sequence& s) { return b < a.batch.B ? blocks_of(a, s) : ceil_div(a.prefix, kBlockKeys); }
 
 constexpr int kListed = 512;        // pages that a workgroup of the many-rows kernel has in LDS at a time; -1 where a number names none
 struct PageList { int page[kListed]; int bad[4]; };
@@ -610,10 +610,7 @@ template <class T, int D>
 struct Shared {
     __align__(16) unsigned char buf[256 * Head<T, D>::kRowBytes];   // few rows: 32 keys and values of each wave; many: two steps' 64
     FirstOdd<D> odd[4];
-    union {
-        PageList list;
-        struct { int scan[4], found[4][2]; };
-    };
+    PageList list;
 };
 
 template <class T, int D, bool MULTI>
@@ -621,54 +618,45 @@ __device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shar
     using H = Head<T, D>;
     constexpr int kWaveBytes = 2 * 32 * H::kRowBytes;
     auto& buf = shared.buf;
-    auto& scan = shared.scan;
-    auto& found = shared.found;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int B = a.batch.B + a.front_item;
 
-    // each thread's run of sequences, the runs' prefix sums, and the sequences in which the waves' shares begin
-    const int run = ceil_div(B, 256), b0 = min(B, tid * run), b1 = min(B, b0 + run);
+    // Each lane's run of sequences and the runs' prefix sums; every wave does this by itself, so that the chain of loads before the first keys is the
+    // shortest there is.  Up to 64 sequences a lane holds one, and they are not looked up again.
+    const int run = max(ceil_div(B, 64), 1), b0 = min(B, lane * run), b1 = min(B, b0 + run);
+    Sequence held{0, 0, 0};
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += item_blocks(a, b);
+    for (int b = b0; b < b1; ++b) {
+        held = line_sequence(a, b);
+        mine += line_blocks(a, b, held);
+    }
     int upto = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const int x = __shfl_up(upto, o);
         if (lane >= o) upto += x;
     }
-    if (lane == 63) scan[wave] = upto;
-    __syncthreads();
-    int before = upto - mine, all = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) { if (w < wave) before += scan[w]; all += scan[w]; }
-    if (block == 0) {
-        int c = before;
-        for (int b = b0; b < b1; ++b) { a.cum[b] = c; c += item_blocks(a, b); }
-        if (tid == 255) a.cum[B] = all;
+    const int all = __builtin_amdgcn_readlane(upto, 63), worker = block * 4 + wave;
+    if (worker == 0) {
+        int c = upto - mine;
+        for (int b = b0; b < b1; ++b) { a.cum[b] = c; c += line_blocks(a, b, line_sequence(a, b)); }
+        if (lane == 0) a.cum[B] = all;
     }
     const int total = all * a.heads, per = line_share(total, a.rows_cap);
-    for (int w = 0; w < 4; ++w) {
-        const int u = min(total, (block * 4 + w) * per);
-        if (mine > 0 && u >= before * a.heads && u < (before + mine) * a.heads) {
-            int b = b0, c = before;
-            for (int n; u >= (c + (n = item_blocks(a, b))) * a.heads; ++b) c += n;
-            found[w][0] = b;
-            found[w][1] = c;
-        }
-    }
-    __syncthreads();
-    const int worker = block * 4 + wave;
-    int u = min(total, worker * per);
+    int u = min((int64_t)total, (int64_t)worker * per);
     const int end = min(total, u + per);
     if (u >= end) return;
-    int b = __builtin_amdgcn_readfirstlane(found[wave][0]), cum = __builtin_amdgcn_readfirstlane(found[wave][1]);
+    const int from = __popcll(__ballot(upto * a.heads <= u));       // the lane whose run has block u
+    int b = from * run, cum = __builtin_amdgcn_readlane(upto - mine, from);
 
     while (u < end) {
-        const int n = item_blocks(a, b);
+        Sequence s;
+        if (run == 1) s = {__builtin_amdgcn_readlane(held.first, b), __builtin_amdgcn_readlane(held.queries, b), __builtin_amdgcn_readlane(held.length, b)};
+        else s = line_sequence(a, b);
+        const int n = line_blocks(a, b, s);
         if (u >= (cum + n) * a.heads) { cum += n; ++b; continue; }
         const int within = u - cum * a.heads, head = within / n, n0 = within - head * n, n1 = min(n, n0 + (end - u));
         const bool stacked = b >= a.batch.B;
-        const Sequence s = stacked ? Sequence{0, a.batch.T, 0} : sequence(a.batch, b);
         const int rows = min(s.queries * a.G, a.rows_cap), row = lane & 31;
         const int token = row / a.G, qh = head * a.G + row % a.G;
         u32x4 q[H::kSteps];
@@ -801,8 +789,9 @@ struct ManyRange {
 #pragma unroll
             for (int i = 0; i < H::kSteps; ++i) frag[i] = lds_read<u32x4>(KeyReads<T, D>::chunk(first_chunk, i));
         };
-        // The weights of `s` and their products with the values at `vat`; the scores `ahead` of the keys in `frag`, which becomes those at `kat`.
-        auto full_block = [&](f32x16& s, f32x16& ahead, unsigned vat, unsigned kat) {
+        // The weights of `s` and their products with the values at `vat`; the scores `ahead` of the keys in `frag`, which becomes those at `kat`.  Where there are no
+        // more keys, these are what lies there, and not used.
+        auto full_block = [&](f32x16& s, f32x16& ahead, unsigned vat, unsigned kat, bool more) {
             if constexpr (!H::kF32) {
                 const float base = st.m == WHT_NEG_INF ? 0.0f : st.m;
                 const unsigned first_chunk = KeyReads<T, D>::first(kat);
@@ -833,7 +822,7 @@ struct ManyRange {
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 st.l += sum[0] + sum[1];
-                rebase<H, 8>(mx, a.scale, st);
+                if (more) rebase<H, 8>(mx, a.scale, st);
             } else {
                 ahead = f32x16{};
 #pragma unroll
@@ -841,7 +830,7 @@ struct ManyRange {
                 weigh(s, a.scale, st);
                 accumulate<T, D, false>(vat, s, 0, odd, st);
                 read_keys(kat);
-                rebase<H, 8>(largest(ahead), a.scale, st);
+                if (more) rebase<H, 8>(largest(ahead), a.scale, st);
             }
         };
         load_k(lo);
@@ -857,14 +846,15 @@ struct ManyRange {
         for (int t = lo; t < hi; ++t) {
             // steps whose blocks, and the first of the next one, are seen by all rows of the wave
             const int blocks = 2 * t >= front || pre_full == front ? front + own_full : pre_full;
-            for (const int end = bad ? t : min(hi - 1, (blocks - 1) / 2); t < end; ++t) {
+            for (const int end = bad ? t : blocks >= 2 * hi ? hi : min(hi - 1, (blocks - 1) / 2); t < end; ++t) {
                 wait_loads<0>();
                 workgroup_barrier();                                // V of this step and K of the next have landed; what they replace next has been read
-                load_v(t + 1);
+                if (t + 1 < hi) load_v(t + 1);
                 if (t + 2 < hi) load_k(t + 2);
-                full_block(s, other, values_at(t, 0), keys_at(t + 1, 0));
-                full_block(other, s, values_at(t, 1), keys_at(t + 1, 1));
+                full_block(s, other, values_at(t, 0), keys_at(t + 1, 0), true);
+                full_block(other, s, values_at(t, 1), keys_at(t + 1, 1), t + 1 < hi);
             }
+            if (t == hi) break;
             wait_loads<0>();
             workgroup_barrier();
             if (t + 1 < hi) load_v(t + 1);
@@ -1078,11 +1068,21 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Joi
                 const int run = min(64, ceil_div(p.n, WAVES));
                 for (int lo = wave * run; lo < p.n; lo += WAVES * run) {
                     const int n = min(run, p.n - lo);
+                    f32x4 x[kUnroll];
+                    auto fetch = [&](int i) {
+#pragma unroll
+                        for (int e = 0; e < kUnroll; ++e) {
+                            const int at = i + e * kAtOnce + group;
+                            const bool there = group < kAtOnce && at < n;
+                            x[e] = there ? *reinterpret_cast<const f32x4*>(p.part + (p.at + (lo + at) * p.step) * D + col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                        }
+                    };
+                    fetch(0);                                       // with the sums: what they weigh is known when both are there
                     float pm = WHT_NEG_INF, pl = 0.0f;
                     if (lane < n) {
-                        const f32x2 x = *reinterpret_cast<const f32x2*>(p.sums + (p.at + (lo + lane) * p.step) * 2);
-                        pm = x[0];
-                        pl = x[1];
+                        const f32x2 y = *reinterpret_cast<const f32x2*>(p.sums + (p.at + (lo + lane) * p.step) * 2);
+                        pm = y[0];
+                        pl = y[1];
                     }
                     float most = pm;
 #pragma unroll
@@ -1096,17 +1096,12 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Joi
                     o *= f;
                     m = now;
                     for (int i = 0; i < n; i += kAtOnce * kUnroll) {
-                        f32x4 x[kUnroll];
-                        float wi[kUnroll];
+                        if (i > 0) fetch(i);
 #pragma unroll
                         for (int e = 0; e < kUnroll; ++e) {
                             const int at = i + e * kAtOnce + group;
-                            const bool there = group < kAtOnce && at < n;
-                            wi[e] = __shfl(w, there ? at : 0);
-                            x[e] = there ? *reinterpret_cast<const f32x4*>(p.part + (p.at + (lo + at) * p.step) * D + col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                            o += __shfl(w, min(at, n - 1)) * x[e];
                         }
-#pragma unroll
-                        for (int e = 0; e < kUnroll; ++e) o += wi[e] * x[e];
                     }
                 }
             }

@@ -151,6 +151,9 @@ inline int check_paged(const wht_attention_rows_t* q, const wht_attention_rows_t
     if (int rc = check_cache(c, b, dtype)) return rc;
     if (int rc = check_sizes(T, b->B, q_heads, c->heads, c->head_dim, max_q, max_length, prefix, dtype)) return rc;
     if (!(scale > 0.0f) || !(scale <= 3.0e38f)) return WHT_ERR_BAD_DIM;
+    // the few-rows kernel counts the blocks of its line in 31 bits
+    const int64_t own = (int64_t)b->width * c->page_size < max_length ? (int64_t)b->width * c->page_size : max_length;
+    if (((int64_t)b->B + 1) * (own / kBlockKeys + prefix / kBlockKeys + 2) > INT32_MAX / c->heads) return WHT_ERR_BAD_DIM;
     const int size = dtype == WHT_DTYPE_F32 ? 4 : 2;
     if (!good_rows(q, q_heads, c->head_dim, size) || !good_rows(out, q_heads, c->head_dim, size)) return WHT_ERR_MISALIGNED;
     if (((uintptr_t)lse & 3u) != 0 || ((uintptr_t)prefix_table & 3u) != 0) return WHT_ERR_MISALIGNED;

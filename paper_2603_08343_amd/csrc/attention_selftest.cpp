@@ -131,6 +131,13 @@ static void statuses() {
     CHECK(paged(r0, 32, I, -1, 1, 256, 1.0f, 1) == WHT_ERR_BAD_DIM);
     CHECK(paged(r0, 32, I, 100, 0, 256, 1.0f, 1) == WHT_ERR_BAD_DIM);
     CHECK(paged(r0, 32, I, 100, 1, -1, 1.0f, 1) == WHT_ERR_BAD_DIM);
+    {
+        wht_attention_cache_t c = c0;
+        wht_attention_batch_t b = b0;
+        b.B = 1 << 16; b.width = 1 << 14;                                        // 64 Ki sequences of 1 Mi tokens: more blocks than the line counts
+        CHECK(check_paged(&r0, &r0, nullptr, 3, 32, &c, &b, nullptr, 0, 1, (int64_t)1 << 20, 1.0f, 1) == WHT_ERR_BAD_DIM);
+        CHECK(check_paged(&r0, &r0, nullptr, 3, 32, &c, &b, nullptr, 0, 1, 1 << 12, 1.0f, 1) == WHT_OK);
+    }
     for (float s : {0.0f, -1.0f, __builtin_nanf(""), __builtin_inff()}) CHECK(paged(r0, 32, I, 100, 1, 256, s, 1) == WHT_ERR_BAD_DIM);
 }
 
