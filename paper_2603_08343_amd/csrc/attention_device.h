@@ -1,6 +1,7 @@
 // Kernels of the paged cache and its attention (include/wht_attention.h) for gfx950.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <limits.h>
 
 #include "attention_plan.h"
 
@@ -429,14 +430,14 @@ __device__ __forceinline__ void block_product(unsigned buf, int d, const f32x16&
     }
 }
 
-// Whether 32 rows in LDS hold anything that is not finite.
-template <class T, int D>
+// Whether LOADS KiB in LDS hold anything that is not finite.
+template <class T, int LOADS>
 __device__ __forceinline__ bool any_odd(unsigned buf) {
     constexpr unsigned kMagnitude = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
     unsigned most = 0;
     ushort2v most2 = {0, 0};
 #pragma unroll
-    for (int i = 0; i < Head<T, D>::kChunks / 2; ++i) {
+    for (int i = 0; i < LOADS; ++i) {
         const u32x4 x = lds_read<u32x4>(buf + (threadIdx.x & 63) * 16 + i * 1024);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -447,14 +448,27 @@ __device__ __forceinline__ bool any_odd(unsigned buf) {
     return __any(sizeof(T) == 4 ? most >= 0x7f800000u : most2[0] >= 0x7f80 || most2[1] >= 0x7f80);
 }
 
-// The first of 32 keys whose value in a column is +infinity or NaN (above), -infinity or NaN (below); 32 where there is none.
+// The first of a block's keys whose value in a column is +infinity or NaN (above), -infinity or NaN (below); their number where there is none.
 template <int D> struct FirstOdd { int above[D], below[D]; };
 
+// To the outputs of a row that sees `seen` keys of them.
 template <class T, int D>
-__device__ __forceinline__ void add_odd(unsigned buf, int seen, FirstOdd<D>& first, RowState<Head<T, D>>& st) {
+__device__ __forceinline__ void add_odd(int seen, const FirstOdd<D>& first, RowState<Head<T, D>>& st) {
+#pragma unroll
+    for (int d = 0; d < Head<T, D>::kBlocks; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int c = d * 32 + key_of(i);
+            st.o[d][i] += (first.above[c] < seen ? -WHT_NEG_INF : 0.0f) + (first.below[c] < seen ? WHT_NEG_INF : 0.0f);
+            if ((i & 3) == 3) asm volatile("" ::: "memory");        // rare: its registers count, its time does not
+        }
+}
+
+// Of 32 rows in LDS, by one wave.
+template <class T, int D>
+__device__ __forceinline__ void find_odd(unsigned buf, FirstOdd<D>& first) {
     using H = Head<T, D>;
-    const int lane = threadIdx.x & 63;
-    for (int c = lane; c < D; c += 64) {
+    for (int c = threadIdx.x & 63; c < D; c += 64) {
         int above = 32, below = 32;
 #pragma unroll 1
         for (int k = 31; k >= 0; --k) {
@@ -468,15 +482,6 @@ __device__ __forceinline__ void add_odd(unsigned buf, int seen, FirstOdd<D>& fir
         first.below[c] = below;
     }
     reads_done();                                                   // the wave's own writes: no other wave looks at `first`
-#pragma unroll
-    for (int d = 0; d < H::kBlocks; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int c = d * 32 + key_of(i);
-            st.o[d][i] += (first.above[c] < seen ? -WHT_NEG_INF : 0.0f) + (first.below[c] < seen ? WHT_NEG_INF : 0.0f);
-            if ((i & 3) == 3) asm volatile("" ::: "memory");        // rare: its registers count, its time does not
-        }
-    reads_done();
 }
 
 // O^T += V^T P^T over 32 keys.  A key that a row does not see has a weight of zero, and zero times infinity would still be NaN: where rows of
@@ -485,10 +490,14 @@ __device__ __forceinline__ void add_odd(unsigned buf, int seen, FirstOdd<D>& fir
 template <class T, int D, bool GUARD>
 __device__ __forceinline__ void accumulate(unsigned buf, const f32x16& p, int seen, FirstOdd<D>& first, RowState<Head<T, D>>& st) {
     bool odd = false;
-    if constexpr (GUARD) odd = any_odd<T, D>(buf);
+    if constexpr (GUARD) odd = any_odd<T, Head<T, D>::kChunks / 2>(buf);
 #pragma unroll
     for (int d = 0; d < Head<T, D>::kBlocks; ++d) block_product<T, D, GUARD>(buf, d, p, odd, st.o[d]);
-    if (odd) add_odd<T, D>(buf, seen, first, st);
+    if (odd) {
+        find_odd<T, D>(buf, first);
+        add_odd<T, D>(seen, first, st);
+        reads_done();
+    }
 }
 
 // A row of q, as the B operand of the first product; zeros where there is no row.
@@ -603,13 +612,13 @@ __device__ __forceinline__ Sequence line_sequence(const AttentionArgs& a, int b)
 __device__ __forceinline__ int line_blocks(const AttentionArgs& a, int b, const Sequence& s) { return b < a.batch.B ? blocks_of(a, s) : ceil_div(a.prefix, kBlockKeys); }
 
 constexpr int kListed = 512;        // pages that a workgroup of the many-rows kernel has in LDS at a time; -1 where a number names none
-struct PageList { int page[kListed]; int bad[4]; };
+struct PageList { int page[kListed]; int bad[4], odd[4]; };         // by wave: whether a page was bad, a value not finite
 
 // What a workgroup of either kernel has in LDS.
 template <class T, int D>
 struct Shared {
     __align__(16) unsigned char buf[256 * Head<T, D>::kRowBytes];   // few rows: 32 keys and values of each wave; many: two steps' 64
-    FirstOdd<D> odd[4];
+    FirstOdd<D> odd[4];             // few rows: of each wave's block; many: of all keys (the first of the four)
     PageList list;
 };
 
@@ -710,8 +719,8 @@ struct ManyRange {
     static constexpr int kTileBytes = kStepKeys * H::kRowBytes;
 
     // steps [lo, hi), whose pages fit the list; limit: how many of the sequence's keys this lane's row sees, all_see, any_sees: every, any row of the wave
-    // (-1: it has none).  LDS: keys of even, of odd steps, values of even, of odd steps.
-    static __device__ __forceinline__ void stream(const AttentionArgs& a, const Keys& k, PageList& list, int lo, int hi, int limit, int all_see, int any_sees,
+    // (-1: it has none), level: how many every row of the workgroup sees.  LDS: keys of even, of odd steps, values of even, of odd steps.
+    static __device__ __forceinline__ void stream(const AttentionArgs& a, const Keys& k, PageList& list, int lo, int hi, int limit, int all_see, int any_sees, int level,
                                                   const unsigned char* kbase, const unsigned char* vbase, unsigned buf, const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd,
                                                   RowState<H>& st) {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), shift = a.page_shift;
@@ -780,8 +789,30 @@ struct ManyRange {
                 s[i] = seen ? s[i] : WHT_NEG_INF;
             }
         };
-        auto seen_in = [&](int j) { return j < front ? k.prefix - j * 32 : limit - (j - front) * 32; };          // of block j, by this lane's row
         auto in_sight = [&](int j) { return j < front ? any_sees >= 0 : (j - front) * 32 < any_sees; };
+
+        // From this step on rows of the workgroup see different keys, and a key that a row does not see has a weight of zero, but zero times infinity is NaN: values
+        // that are not finite are taken out of LDS by the wave that loaded them, and given to the rows that see them at the end.
+        const int uneven = k.front + level / kStepKeys;
+        auto clean_values = [&](int t) {
+            const unsigned at = to + (2 + (t & 1)) * kTileBytes;
+            if (!any_odd<T, kLoads>(at)) return;
+            list.odd[wave] = 1;
+#pragma unroll 1
+            for (int n = lane; n < kLoads * 64; n += 64) {
+                const int r = (wave * kLoads * 64 + n) / H::kChunks, c = H::v_chunk(r, (wave * kLoads * 64 + n) % H::kChunks);
+#pragma unroll 1
+                for (int e = 0; e < 16 / (int)sizeof(T); ++e) {
+                    auto* p = (__attribute__((address_space(3))) T*)(uintptr_t)(at + n * 16 + e * sizeof(T));
+                    const float v = (float)*p;
+                    if (fabsf(v) < __builtin_inff()) continue;
+                    const int col = c * (16 / (int)sizeof(T)) + e, key = (t - k.front) * kStepKeys + r;
+                    if (v != WHT_NEG_INF) atomicMin(&odd.above[col], key);
+                    if (v != -WHT_NEG_INF) atomicMin(&odd.below[col], key);
+                    *p = (T)0.0f;
+                }
+            }
+        };
 
         u32x4 frag[H::kSteps];                                      // keys of the block after the one whose scores are at hand
         auto read_keys = [&](unsigned at) {
@@ -846,7 +877,7 @@ struct ManyRange {
         for (int t = lo; t < hi; ++t) {
             // steps whose blocks, and the first of the next one, are seen by all rows of the wave
             const int blocks = 2 * t >= front || pre_full == front ? front + own_full : pre_full;
-            for (const int end = bad ? t : blocks >= 2 * hi ? hi : min(hi - 1, (blocks - 1) / 2); t < end; ++t) {
+            for (const int end = bad ? t : min(uneven, blocks >= 2 * hi ? hi : min(hi - 1, (blocks - 1) / 2)); t < end; ++t) {
                 wait_loads<0>();
                 workgroup_barrier();                                // V of this step and K of the next have landed; what they replace next has been read
                 if (t + 1 < hi) load_v(t + 1);
@@ -856,6 +887,7 @@ struct ManyRange {
             }
             if (t == hi) break;
             wait_loads<0>();
+            if (t >= uneven) clean_values(t);
             workgroup_barrier();
             if (t + 1 < hi) load_v(t + 1);
             if (t + 2 < hi) load_k(t + 2);
@@ -870,7 +902,12 @@ struct ManyRange {
                     for (int i = 0; i < H::kSteps; ++i) other = score_step<T>(frag[i], q[i], other);
                 }
                 weigh(s, a.scale, st);
-                accumulate<T, D, true>(values_at(t, half), s, seen_in(j), odd, st);
+                const unsigned values = values_at(t, half);
+#pragma unroll
+                for (int d = 0; d < H::kBlocks; ++d) {
+                    block_product<T, D, false>(values, d, s, false, st.o[d]);
+                    asm volatile("" ::: "memory");                  // one block's values in registers at a time
+                }
                 if (more) {
                     if (t + 1 < hi) read_keys(keys_at(t + 1, half));
                     if (bad || !full(j + 1)) hide(other, j + 1);
@@ -881,14 +918,18 @@ struct ManyRange {
         }
     }
 
-    static __device__ __forceinline__ void run(const AttentionArgs& a, const Keys& k, PageList& list, int t0, int t1, int limit, int all_see, int any_sees,
+    static __device__ __forceinline__ void run(const AttentionArgs& a, const Keys& k, PageList& list, int t0, int t1, int limit, int all_see, int any_sees, int level,
                                                const unsigned char* kbase, const unsigned char* vbase, unsigned buf, const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd,
                                                RowState<H>& st) {
+        for (int c = threadIdx.x; c < D; c += 256) odd.above[c] = odd.below[c] = INT_MAX;
+        if (threadIdx.x < 4) list.odd[threadIdx.x] = 0;
         const int per_list = max(((kListed - 4) << a.page_shift) / kStepKeys, 1);           // each part may begin and end within a page
         for (int lo = t0; lo < t1; lo += per_list) {
             if (lo > t0) workgroup_barrier();                       // the last steps' reads are done
-            stream(a, k, list, lo, min(t1, lo + per_list), limit, all_see, any_sees, kbase, vbase, buf, q, odd, st);
+            stream(a, k, list, lo, min(t1, lo + per_list), limit, all_see, any_sees, level, kbase, vbase, buf, q, odd, st);
         }
+        workgroup_barrier();
+        if ((list.odd[0] | list.odd[1] | list.odd[2] | list.odd[3]) != 0) add_odd<T, D>(limit, odd, st);
     }
 };
 
@@ -964,7 +1005,7 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
     st.clear();
     const unsigned char *kbase = a.k + head * a.head_stride, *vbase = a.v + head * a.head_stride;
     const Keys k{a.prefix_table, a.batch.table + b * a.batch.table_stride, front, a.use_prefix ? a.prefix : 0, keys};
-    R::run(a, k, list, t0, t1, limit, all_see, any_sees, kbase, vbase, __builtin_amdgcn_readfirstlane(lds_address(buf)), q, odd[wave], st);
+    R::run(a, k, list, t0, t1, limit, all_see, any_sees, sees((int64_t)tile * kTileRows), kbase, vbase, __builtin_amdgcn_readfirstlane(lds_address(buf)), q, odd[0], st);
     if (!there) return;
     st.l += other_half(st.l);
     const int64_t t = s.first + token;
