@@ -1100,7 +1100,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Joi
             if (a.own_few) {
                 const int units = (a.own_prefix ? ceil_div(a.prefix, kBlockKeys) : 0) + ceil_div(s.length, kBlockKeys);
                 parts[1] = slots(a.own_part, a.own_sums, b * a.heads + head, a.cum[b] * a.heads + head * units, units, total, a.own_cap, j * a.G + g);
-            } else parts[1] = {a.own_part, a.own_sums, r, (int64_t)a.batch.T * a.q_heads, a.own_splits};
+            }
             const int group = lane / kLanes, col = (lane % kLanes) * 4;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -1172,6 +1172,59 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Joi
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     if (lane < kLanes) store4<T>(a.out + t * a.out_ts + qh * a.out_hs + lane * 4 * sizeof(T), o * inv + value);
     if (a.lse && lane == 0) a.lse[r] = l == 0.0f ? WHT_NEG_INF : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// The same where every row has its pieces at the same places: the shares that a tile's keys were split into.  D / 4 lanes take a row, so that a wave has two
+// or more; which row it is matters only for what is written, and is looked up beside the loads.
+template <class T, int D>
+__global__ __launch_bounds__(256) void join_splits_kernel(JoinArgs a) {
+    constexpr int kLanes = D / 4, kRows = 256 / kLanes, kUnroll = 4;
+    const int64_t rows = (int64_t)a.batch.T * a.q_heads, r = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
+    const int t0 = (int)min((int64_t)blockIdx.x * kRows / a.q_heads, (int64_t)a.batch.T - 1);       // sequence_of takes a whole wave
+    const bool there = threadIdx.x < kRows * kLanes && r < rows;
+    const int64_t at = there ? r : 0;
+    const int col = threadIdx.x % kLanes * 4, t = (int)(at / a.q_heads);
+    float m = WHT_NEG_INF, l = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int lo = 0; lo < a.own_splits; lo += kUnroll) {
+        f32x2 ml[kUnroll];
+        f32x4 x[kUnroll];
+#pragma unroll
+        for (int e = 0; e < kUnroll; ++e) {
+            const int64_t p = at + min(lo + e, a.own_splits - 1) * rows;
+            ml[e] = *reinterpret_cast<const f32x2*>(a.own_sums + p * 2);
+            x[e] = *reinterpret_cast<const f32x4*>(a.own_part + p * D + col);
+            if (lo + e >= a.own_splits) ml[e] = f32x2{WHT_NEG_INF, 0.0f};
+        }
+        float now = m;
+#pragma unroll
+        for (int e = 0; e < kUnroll; ++e) now = fmaxf(now, ml[e][0]);
+        const float base = now == WHT_NEG_INF ? 0.0f : now, f = __builtin_amdgcn_exp2f(m - base);
+        l *= f;
+        o *= f;
+        m = now;
+#pragma unroll
+        for (int e = 0; e < kUnroll; ++e) {
+            const float w = __builtin_amdgcn_exp2f(ml[e][0] - base);
+            l += ml[e][1] * w;
+            if (lo + e < a.own_splits) o += w * x[e];
+        }
+    }
+    int b = sequence_of(a.batch, t0);                               // of the block's first row; the others' is that or one soon after
+    if (!there) return;
+    float value = 0.0f;
+    while (b >= 0 && b < a.batch.B) {
+        const Sequence s = sequence(a.batch, b);
+        if (t < s.first + s.queries) {
+            if (t < s.first || t - s.first >= a.max_q) value = l = __builtin_nanf("");
+            break;
+        }
+        ++b;
+    }
+    if (b < 0 || b >= a.batch.B) { l = 0.0f; o = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; m = WHT_NEG_INF; }      // padding: no workgroup wrote its pieces
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    store4<T>(a.out + t * a.out_ts + (r % a.q_heads) * a.out_hs + col * sizeof(T), value == 0.0f ? o * inv : f32x4{value, value, value, value});
+    if (a.lse && col == 0) a.lse[r] = l == 0.0f ? WHT_NEG_INF : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 }  // namespace wht

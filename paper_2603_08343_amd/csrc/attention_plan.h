@@ -40,9 +40,13 @@ struct AttentionPlan {
     size_t front_at, own_at, front_sums_at, own_sums_at, cum_at, bytes;     // byte offsets in the workspace
 };
 
-inline int splits_for(int64_t tiles, int64_t keys, int workgroups) {
-    // at least 256 keys each
-    int64_t s = tiles > 0 ? workgroups / tiles : 1;
+// Workgroups that share a tile's keys, 256 keys each at least: so that every compute unit has one.  A second one there is worth 8 % (8 sequences of 128 new
+// tokens behind 16256, 32 heads of 128: 351 us with one, 325 with two), less than partial results of short ranges cost (1000 new tokens at
+// 32 x 128: 29 and 45 us), so that tiles are split for it where the shares are long.
+inline int splits_for(int64_t tiles, int64_t keys) {
+    if (tiles <= 0) return 1;
+    int64_t s = kWorkgroups / tiles;
+    if (s > 1 && keys / s < 4096) s = kWorkgroups / 2 / tiles;
     const int64_t most = ceil_div64(keys, 256);
     if (s > most) s = most;
     return s < 1 ? 1 : (int)s;
@@ -60,14 +64,14 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
     p.front_splits = p.own_splits = 1;
     if (p.front) {
         if (!p.front_few) {
-            p.front_splits = splits_for(ceil_div64(T * G, kTileRows) * heads, prefix, kWorkgroups / 2);
+            p.front_splits = splits_for(ceil_div64(T * G, kTileRows) * heads, prefix);
             p.front_rows = (size_t)p.front_splits * (size_t)(T * q_heads);
         }
     }
     p.own_cap = p.front && p.front_few ? (int32_t)(T * G) : max_q * (int32_t)G;
     if (p.own_few) p.own_rows = (((size_t)B + 1) * heads + kWorkers) * (size_t)p.own_cap;
     else {
-        p.own_splits = splits_for(ceil_div64((int64_t)max_q * G, kTileRows) * heads * B, max_length + prefix, kWorkgroups);
+        p.own_splits = splits_for(ceil_div64((int64_t)max_q * G, kTileRows) * heads * B, max_length + prefix);
         if (p.own_splits > 1) p.own_rows = (size_t)p.own_splits * (size_t)(T * q_heads);
     }
     p.combine = p.front || p.own_few || p.own_splits > 1;

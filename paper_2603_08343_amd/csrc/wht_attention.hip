@@ -114,7 +114,8 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     j.own_few = p.own_few; j.own_splits = p.own_splits; j.own_cap = a.rows_cap; j.own_prefix = a.use_prefix;
     return with_type(dtype, c->head_dim, [&](auto t, auto d) {
         const int64_t rows = T * q_heads;
-        if (rows <= kJoinRowsWide) hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 16>), dim3((unsigned)rows), dim3(1024), 0, stream, j);
+        if (!p.own_few) hipLaunchKernelGGL((join_splits_kernel<decltype(t), decltype(d)::value>), dim3((unsigned)ceil_div64(rows, 256 / (decltype(d)::value / 4))), dim3(256), 0, stream, j);
+        else if (rows <= kJoinRowsWide) hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 16>), dim3((unsigned)rows), dim3(1024), 0, stream, j);
         else if (rows <= kJoinRows) hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 4>), dim3((unsigned)rows), dim3(256), 0, stream, j);
         else hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 1>), dim3((unsigned)ceil_div64(rows, 4)), dim3(256), 0, stream, j);
         return launched();
