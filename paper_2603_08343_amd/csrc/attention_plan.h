@@ -89,15 +89,23 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
 // The few-rows kernel's line: the blocks of all items one after the other, an equal share of them to a worker (a wave).  The pieces of an item
 // of n blocks from u0 on lie in the slots item + w of the workers w that it meets: first .. first + count - 1.  A piece writes `rows`
 // rows of results, 4 bytes an element, for the keys and values it reads: a share is a block for every eight rows at least.
+// With a gang of heads a worker is a workgroup, an item a group of heads, and every slot holds one piece for each of them.
 struct Slots { int64_t first; int count; };
-WHT_HD int line_share(int total, int rows) {
-    const int even = ceil_div(total, kWorkers), least = ceil_div(rows, 8);
+constexpr int kWorkersLog2 = 11;
+static_assert(kWorkers == 1 << kWorkersLog2, "shares are counted by shifting");
+WHT_HD int line_share(int total, int rows, int gang_log2) {
+    const int workers_log2 = kWorkersLog2 - gang_log2, even = (total + (1 << workers_log2) - 1) >> workers_log2, least = (rows + 7) >> 3;
     return even > least ? even : least;
 }
-WHT_HD Slots item_slots(int item, int u0, int n, int total, int rows) {
+WHT_HD Slots item_slots(int item, int u0, int n, int total, int rows, int gang_log2) {
     if (n == 0) return {0, 0};
-    const int per = line_share(total, rows), w0 = u0 / per, w1 = (u0 + n - 1) / per;
+    const int per = line_share(total, rows, gang_log2), w0 = u0 / per, w1 = (u0 + n - 1) / per;
     return {(int64_t)item + w0, w1 - w0 + 1};
+}
+// Four heads side by side: where a row is no whole number of 128-byte lines, and the next head's row follows it in memory.
+constexpr int kGangLog2 = 2;
+inline int gang_log2_of(int32_t heads, int64_t row_bytes, int64_t head_stride_bytes) {
+    return row_bytes % 128 != 0 && head_stride_bytes == row_bytes && heads % (1 << kGangLog2) == 0 ? kGangLog2 : 0;
 }
 
 // Argument checks, in the order of the status codes.

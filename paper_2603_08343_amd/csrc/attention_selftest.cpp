@@ -16,36 +16,38 @@ using namespace wht;
 #define CHECK(c) do { if (!(c)) { printf("FAILED %s:%d: %s\n", __FILE__, __LINE__, #c); exit(1); } } while (0)
 
 // Walks the line as the workers do, and compares what each item leaves with what item_slots says.
-static void walk(const std::vector<int>& lengths, int heads, int front, int rows) {
-    const int B = (int)lengths.size(), W = kWorkers;
+static void walk(const std::vector<int>& lengths, int heads, int front, int rows, int gang_log2) {
+    const int gang = 1 << gang_log2;
+    heads = (heads + gang - 1) / gang * gang;
+    const int B = (int)lengths.size(), W = kWorkers / gang, groups = heads / gang;
     std::vector<int> units(B), cum(B + 1, 0);
     for (int b = 0; b < B; ++b) {
         units[b] = ceil_div(front, kBlockKeys) + ceil_div(lengths[b], kBlockKeys);
         cum[b + 1] = cum[b] + units[b];
     }
-    const int total = cum[B] * heads, per = line_share(total, rows);
+    const int total = cum[B] * groups, per = line_share(total, rows, gang_log2);
     std::map<int, std::vector<int64_t>> of;             // item -> slots, in order
     std::set<int64_t> used;
     int covered = 0;
     for (int w = 0; w < W; ++w) {
         int u = w * per, end = total < u + per ? total : u + per, b = 0;
         while (u < end) {
-            if (u >= cum[b + 1] * heads) { ++b; continue; }
-            const int n = units[b], within = u - cum[b] * heads, head = within / n, u0 = within - head * n;
+            if (u >= cum[b + 1] * groups) { ++b; continue; }
+            const int n = units[b], within = u - cum[b] * groups, group = within / n, u0 = within - group * n;
             const int u1 = n < u0 + (end - u) ? n : u0 + (end - u);
-            const int64_t slot = (int64_t)b * heads + head + w;
+            const int64_t slot = (int64_t)b * groups + group + w;
             CHECK(used.insert(slot).second);
-            CHECK(slot >= 0 && slot < (int64_t)B * heads + W);
-            of[b * heads + head].push_back(slot);
+            CHECK(slot >= 0 && (slot + 1) * gang <= (int64_t)B * heads + kWorkers);
+            of[b * groups + group].push_back(slot);
             covered += u1 - u0;
             u += u1 - u0;
         }
     }
     CHECK(covered == total);
     for (int b = 0; b < B; ++b)
-        for (int h = 0; h < heads; ++h) {
-            const Slots s = item_slots(b * heads + h, cum[b] * heads + h * units[b], units[b], total, rows);
-            const auto& got = of[b * heads + h];
+        for (int h = 0; h < groups; ++h) {
+            const Slots s = item_slots(b * groups + h, cum[b] * groups + h * units[b], units[b], total, rows, gang_log2);
+            const auto& got = of[b * groups + h];
             CHECK(s.count == (int)got.size());
             for (int i = 0; i < s.count; ++i) CHECK(got[i] == s.first + i);
         }
@@ -147,11 +149,12 @@ int main() {
         std::vector<int> lengths(rng() % 200);
         const int most = 1 << (rng() % 16);
         for (int& n : lengths) n = (int)(rng() % (unsigned)most) * (rng() % 5 != 0);
-        walk(lengths, 1 + (int)(rng() % 40), i % 3 ? 0 : (int)(rng() % 5000), 1 + (int)(rng() % 32));
+        walk(lengths, 1 + (int)(rng() % 40), i % 3 ? 0 : (int)(rng() % 5000), 1 + (int)(rng() % 32), i % 2 ? 0 : kGangLog2);
     }
-    walk({}, 8, 0, 4);
-    walk({0, 0}, 8, 0, 4);
-    walk({1}, 1, 0, 1);
+    walk({}, 8, 0, 4, 0);
+    walk({0, 0}, 8, 0, 4, kGangLog2);
+    walk({1}, 1, 0, 1, 0);
+    CHECK(gang_log2_of(16, 192, 192) == kGangLog2 && gang_log2_of(16, 192, 64 * 192) == 0 && gang_log2_of(6, 192, 192) == 0 && gang_log2_of(16, 256, 256) == 0);
     plans();
     statuses();
     printf("attention_selftest: ok\n");

@@ -83,6 +83,7 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     }
     a.use_prefix = !p.front && prefix > 0;
     a.front_item = p.front && p.front_few;
+    a.gang_log2 = gang_log2_of(c->heads, c->head_dim * size, a.head_stride);
     a.splits = p.own_splits; a.tiles = (int)tiles_one; a.rows_cap = p.own_cap;
     a.part = reinterpret_cast<float*>(ws + p.own_at); a.sums = reinterpret_cast<float*>(ws + p.own_sums_at);
     a.cum = reinterpret_cast<int*>(ws + p.cum_at);
@@ -109,7 +110,7 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     j.batch = a.batch; j.out = a.out; j.lse = lse; j.out_ts = a.out_ts; j.out_hs = a.out_hs;
     j.front_part = reinterpret_cast<float*>(ws + p.front_at); j.front_sums = reinterpret_cast<float*>(ws + p.front_sums_at);
     j.own_part = a.part; j.own_sums = a.sums; j.cum = a.cum;
-    j.q_heads = q_heads; j.heads = a.heads; j.G = a.G; j.max_q = max_q; j.prefix = a.prefix;
+    j.q_heads = q_heads; j.heads = a.heads; j.G = a.G; j.max_q = max_q; j.prefix = a.prefix; j.gang_log2 = a.gang_log2;
     j.front = p.front; j.front_few = p.front_few; j.front_splits = p.front_splits;
     j.own_few = p.own_few; j.own_splits = p.own_splits; j.own_cap = a.rows_cap; j.own_prefix = a.use_prefix;
     return with_type(dtype, c->head_dim, [&](auto t, auto d) {

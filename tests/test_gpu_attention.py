@@ -47,6 +47,15 @@ def test_decode(dtype, heads, prefix, page, order):
     assert torch.equal(out, _paged(c, lse=False)), "without the statistic, with q_starts"
 
 
+@pytest.mark.parametrize("heads", [(12, 4, 96), (8, 8, 96), (16, 16, 96)])
+@pytest.mark.parametrize("queries,prefix", [([1] * 9, 0), ([1] * 9, 200), ([1, 1, 2, 1, 1, 1, 1, 1, 1], 200)])
+def test_heads_whose_rows_share_lines(heads, queries, prefix):
+    """Rows of 192 bytes one after the other: four heads side by side; the rows of all sequences few, and many, against the prefix."""
+    lengths = [0, 1, 2, 33, 64, 300, 31, 1000, 128]
+    c = check.make(9, queries, [max(n, q) for n, q in zip(lengths, queries)], heads, 16, prefix, BF16, "token", seed=30)
+    _compare(c)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("heads", [(4, 4, 64), (3, 3, 96), (8, 2, 128), (64, 1, 64), (12, 1, 128)])
 @pytest.mark.parametrize("length,prefix,page", [(1, 0, 8), (1, 1, 16), (0, 5, 16), (5000, 0, 16), (700, 4000, 64), (130, 0, 1024)])
