@@ -1091,70 +1091,67 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Joi
     const int b = __builtin_amdgcn_readfirstlane(sequence_of(a.batch, t));
     float value = 0.0f, m = WHT_NEG_INF, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int group = lane / kLanes, col = (lane % kLanes) * 4;
+    auto add = [&](const Parts& p) {
+        // the wave takes every WAVES-th run of 64 pieces, or an even share where there are fewer
+        const int run = min(64, ceil_div(p.n, WAVES));
+        for (int lo = wave * run; lo < p.n; lo += WAVES * run) {
+            const int n = min(run, p.n - lo);
+            f32x4 x[kUnroll];
+            auto fetch = [&](int i) {
+#pragma unroll
+                for (int e = 0; e < kUnroll; ++e) {
+                    const int at = i + e * kAtOnce + group;
+                    const bool there = group < kAtOnce && at < n;
+                    x[e] = there ? *reinterpret_cast<const f32x4*>(p.part + (p.at + (lo + at) * p.step) * D + col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                }
+            };
+            fetch(0);                                               // with the sums: what they weigh is known when both are there
+            float pm = WHT_NEG_INF, pl = 0.0f;
+            if (lane < n) {
+                const f32x2 y = *reinterpret_cast<const f32x2*>(p.sums + (p.at + (lo + lane) * p.step) * 2);
+                pm = y[0];
+                pl = y[1];
+            }
+            float most = pm;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+            const float now = fmaxf(m, most), base = now == WHT_NEG_INF ? 0.0f : now;
+            const float f = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(pm - base);
+            float sum = pl * w;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+            l = l * f + sum;
+            o *= f;
+            m = now;
+            for (int i = 0; i < n; i += kAtOnce * kUnroll) {
+                if (i > 0) fetch(i);
+#pragma unroll
+                for (int e = 0; e < kUnroll; ++e) {
+                    const int at = i + e * kAtOnce + group;
+                    o += __shfl(w, min(at, n - 1)) * x[e];
+                }
+            }
+        }
+    };
+    // shares of the prefix stand in the same places for every row: they are on their way while the row's sequence is looked up
+    if (a.front && !a.front_few) add({a.front_part, a.front_sums, r, (int64_t)a.batch.T * a.q_heads, a.front_splits});
+    const bool empty = b < 0;
     if (b >= 0) {
         const Sequence s = sequence(a.batch, b);
         const int j = t - s.first;
-        if (j < 0 || j >= s.queries || j >= a.max_q) value = l = __builtin_nanf("");
+        if (j < 0 || j >= s.queries || j >= a.max_q) value = __builtin_nanf("");
         else {
-            Parts parts[2] = {{nullptr, nullptr, 0, 0, 0}, {nullptr, nullptr, 0, 0, 0}};
-            const int total = a.own_few ? a.cum[a.batch.B + (a.front && a.front_few)] : 0;
-            if (a.front) {
-                if (a.front_few) parts[0] = slots(a, a.batch.B, head, ceil_div(a.prefix, kBlockKeys), total, t * a.G + g);
-                else parts[0] = {a.front_part, a.front_sums, r, (int64_t)a.batch.T * a.q_heads, a.front_splits};
-            }
-            if (a.own_few) parts[1] = slots(a, b, head, (a.own_prefix ? ceil_div(a.prefix, kBlockKeys) : 0) + ceil_div(s.length, kBlockKeys), total, j * a.G + g);
-            const int group = lane / kLanes, col = (lane % kLanes) * 4;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const Parts& p = parts[k];
-                // the wave takes every WAVES-th run of 64 pieces, or an even share where there are fewer
-                const int run = min(64, ceil_div(p.n, WAVES));
-                for (int lo = wave * run; lo < p.n; lo += WAVES * run) {
-                    const int n = min(run, p.n - lo);
-                    f32x4 x[kUnroll];
-                    auto fetch = [&](int i) {
-#pragma unroll
-                        for (int e = 0; e < kUnroll; ++e) {
-                            const int at = i + e * kAtOnce + group;
-                            const bool there = group < kAtOnce && at < n;
-                            x[e] = there ? *reinterpret_cast<const f32x4*>(p.part + (p.at + (lo + at) * p.step) * D + col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                        }
-                    };
-                    fetch(0);                                       // with the sums: what they weigh is known when both are there
-                    float pm = WHT_NEG_INF, pl = 0.0f;
-                    if (lane < n) {
-                        const f32x2 y = *reinterpret_cast<const f32x2*>(p.sums + (p.at + (lo + lane) * p.step) * 2);
-                        pm = y[0];
-                        pl = y[1];
-                    }
-                    float most = pm;
-#pragma unroll
-                    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
-                    const float now = fmaxf(m, most), base = now == WHT_NEG_INF ? 0.0f : now;
-                    const float f = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(pm - base);
-                    float sum = pl * w;
-#pragma unroll
-                    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-                    l = l * f + sum;
-                    o *= f;
-                    m = now;
-                    for (int i = 0; i < n; i += kAtOnce * kUnroll) {
-                        if (i > 0) fetch(i);
-#pragma unroll
-                        for (int e = 0; e < kUnroll; ++e) {
-                            const int at = i + e * kAtOnce + group;
-                            o += __shfl(w, min(at, n - 1)) * x[e];
-                        }
-                    }
-                }
-            }
-            const f32x4 mine = o;
-#pragma unroll
-            for (int e = 1; e < kAtOnce; ++e)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] += __shfl(mine[i], lane + e * kLanes);      // the first group's lanes hold the sum
+            const int total = a.cum[a.batch.B + (a.front && a.front_few)];
+            if (a.front && a.front_few) add(slots(a, a.batch.B, head, ceil_div(a.prefix, kBlockKeys), total, t * a.G + g));
+            add(slots(a, b, head, (a.own_prefix ? ceil_div(a.prefix, kBlockKeys) : 0) + ceil_div(s.length, kBlockKeys), total, j * a.G + g));
         }
     }
+    const f32x4 mine = o;
+#pragma unroll
+    for (int e = 1; e < kAtOnce; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] += __shfl(mine[i], lane + e * kLanes);              // the first group's lanes hold the sum
     if constexpr (WAVES > 1) {
         if (lane < kLanes) shares[wave].o[lane] = o;
         if (lane == 0) { shares[wave].m = m; shares[wave].l = l; }
@@ -1171,8 +1168,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Joi
             o += f * shares[w].o[lane % kLanes];
         }
     }
+    if (empty) { l = 0.0f; m = WHT_NEG_INF; o = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }              // padding
+    if (value != 0.0f) l = value;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    if (lane < kLanes) store4<T>(a.out + t * a.out_ts + qh * a.out_hs + lane * 4 * sizeof(T), o * inv + value);
+    if (lane < kLanes) store4<T>(a.out + t * a.out_ts + qh * a.out_hs + lane * 4 * sizeof(T), value != 0.0f ? f32x4{value, value, value, value} : o * inv);
     if (a.lse && lane == 0) a.lse[r] = l == 0.0f ? WHT_NEG_INF : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
