@@ -34,7 +34,7 @@
  * What lies in a place that no token sees has no influence, whatever it holds (infinities and NaN as well).  The kernels
  * look at the device arrays' values before they use them:
  *   - a page number outside [0, pages) names no memory: nothing is stored there, and its tokens count as not there;
- *   - lengths are taken within [0, width * page_size] (attention: and up to max_length);
+ *   - attention takes lengths within [0, width * page_size] and up to max_length;
  *   - a token without a place in the cache (no sequence, p < 0, p past the table) is not stored;
  *   - a position outside the rows of `rope` is not stored either, and its row of q_out is NaN;
  *   - a row of q that belongs to no sequence gives a row of zeros (append and attention; lse = -inf);

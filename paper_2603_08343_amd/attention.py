@@ -195,6 +195,7 @@ def wht_attention_append(q, k, v, k_pages, v_pages, table, lengths, rope, q_star
       k_pages, v_pages [pages, heads, page_size, head_dim]: any order in memory (equal strides)
       table int32 [B, width], lengths int32 [B] (the new tokens included), q_starts int32 [B + 1] (None: a token each)
       rope [positions, rotary / 2, 2] float32 (wht_attention_rope_table) or None; position: of a sequence's first own token
+    For serving: nothing here is recorded for a backward pass.
     """
     if stream is None:
         done = _native().append(q, k, v, k_pages, v_pages, table, lengths, rope, q_starts, position, interleaved, q_out)
@@ -246,6 +247,7 @@ def wht_attention_paged(q, k_pages, v_pages, table, lengths, q_starts=None, pref
       max_q: at least the largest number of new tokens of a sequence (None: 1 without q_starts, T with them)
       max_length: at least the largest of lengths (None: what the table can hold); goes into how the work is split
       scale: None for 1 / sqrt(head_dim)
+    For serving: nothing here is recorded for a backward pass.
     """
     if stream is None:
         done = _native().paged(q, k_pages, v_pages, table, lengths, q_starts, prefix_table, prefix_length, max_q, max_length, scale, out, lse,

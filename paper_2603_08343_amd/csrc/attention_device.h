@@ -28,7 +28,7 @@ constexpr float kLn2 = 0.693147180559945309f;
 struct Batch {
     const int *table, *lengths, *q_starts;
     int64_t table_stride;
-    int B, T, most;                     // most: tokens a sequence has at most
+    int B, T, most;                     // most: lengths are cut to it
 };
 
 struct Sequence { int first, queries, length; };     // first row, new tokens, own tokens
@@ -69,7 +69,7 @@ struct AppendArgs {
     int64_t page_stride, head_stride, token_stride;                 // bytes
     const float* rope;
     int64_t rope_rows;
-    int q_heads, heads, pages, page_shift, rotary, interleaved, position;
+    int q_heads, heads, pages, page_shift, rotary, interleaved, position, places;         // places: that a row of the table has
 };
 
 template <class T> struct Vec16 { static constexpr int n = 16 / sizeof(T); T e[n]; };
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
         const int p = s.length - s.queries + (t - s.first);
         if (t >= s.first && t < s.first + s.queries) {
             position = (int64_t)a.position + p;
-            if (p >= 0) {
+            if (p >= 0 && p < a.places) {
                 const int page = a.batch.table[b * a.batch.table_stride + (p >> a.page_shift)];
                 if (page >= 0 && page < a.pages) place = page * a.page_stride + (p & ((1 << a.page_shift) - 1)) * a.token_stride;
             }

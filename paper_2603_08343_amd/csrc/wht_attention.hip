@@ -31,7 +31,8 @@ static int append(const wht_attention_rows_t* q, const wht_attention_rows_t* k, 
                   int64_t rope_rows, int32_t rotary, int32_t interleaved, int64_t position, int32_t dtype, hipStream_t stream) {
     const int64_t size = dtype == WHT_DTYPE_F32 ? 4 : 2;
     AppendArgs a{};
-    a.batch = batch_of(b, T, (int64_t)b->width * c->page_size);
+    a.batch = batch_of(b, T, INT32_MAX);
+    a.places = b->width * c->page_size;
     a.q = static_cast<const unsigned char*>(q->data);
     a.kn = static_cast<const unsigned char*>(k->data);
     a.vn = static_cast<const unsigned char*>(v->data);

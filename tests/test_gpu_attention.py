@@ -303,6 +303,18 @@ def test_append_where_there_is_no_place():
     assert torch.equal(c["v_pages"].cpu().double(), want[2])
 
 
+def test_append_past_the_table():
+    """A sequence that has outgrown its row of the table: its tokens are not stored, and nothing else is written over."""
+    wht = _wht()
+    for lengths in ([48, 49, 60, 1 << 30], [47, 50, -3, (1 << 31) - 1]):
+        c = check.make(4, [1, 3, 2, 1], [48, 48, 48, 48], (4, 2, 64), 16, 0, seed=29)
+        c["lengths"] = torch.tensor(lengths, dtype=torch.int32, device="cuda:0")
+        want = check.append(c, None, False, 0)
+        out = wht.wht_attention_append(c["q"], c["k"], c["v"], c["k_pages"], c["v_pages"], c["table"], c["lengths"], None, c["starts"])
+        assert torch.equal(out, c["q"])
+        assert torch.equal(c["k_pages"].cpu().double(), want[1]) and torch.equal(c["v_pages"].cpu().double(), want[2])
+
+
 def test_offsets_past_32_bits():
     """A cache of more than 4 GiB: its last pages."""
     wht = _wht()
