@@ -271,8 +271,11 @@ __device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigne
 // 16 bytes per lane from memory to LDS at base + 16 * lane, past the registers.  Assembly, because the compiler would otherwise wait for
 // every such load in flight before any read of LDS; which have landed is known where wait_loads stands.  Reads of what is overwritten
 // have returned (lgkmcnt).
+// STREAM: read once, not kept in the caches.
+template <bool STREAM>
 __device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(to) : "memory");
+    if constexpr (STREAM) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" : : "v"(from), "s"(to) : "memory");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(to) : "memory");
 }
 // The same from a place that all lanes share, `off` bytes on.
 __device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned off, unsigned to) {
@@ -520,7 +523,7 @@ __device__ __forceinline__ void load_row(const unsigned char* p, bool there, u32
 // Gang: where a token's rows of neighbouring heads share 128-byte lines, the four waves of a workgroup are one worker that takes four heads' rows, whole lines
 // together, at the same time (200 sequences at 16 x 96, rows of 192 bytes one after the other: 525 MB fetched without it, of 406 MB that there are).
 
-template <class T, int D, bool MULTI>
+template <class T, int D, bool MULTI, bool STREAM>
 struct FewRange {
     using H = Head<T, D>;
     static constexpr int kLoads = H::kChunks / 2;                   // of one wave for 32 rows
@@ -553,7 +556,8 @@ struct FewRange {
         for (int i = 0; i < kLoads; ++i) {
             const int r = (i * 64 + lane) / H::kChunks, p = (i * 64 + lane) % H::kChunks;
             const int c = V ? H::v_chunk(r, p) : H::k_chunk(r, p);
-            load_to_lds(off[i] >= 0 ? base + off[i] + c * 16 : zero_chunk, to + i * 1024);
+            const unsigned char* from = off[i] >= 0 ? base + off[i] + c * 16 : zero_chunk;
+            load_to_lds<STREAM>(from, to + i * 1024);
         }
     }
 
@@ -625,7 +629,7 @@ struct Shared {
     PageList list;
 };
 
-template <class T, int D, bool MULTI>
+template <class T, int D, bool MULTI, bool STREAM>
 __device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shared<T, D>& shared) {
     using H = Head<T, D>;
     constexpr int kWaveBytes = 2 * 32 * H::kRowBytes;
@@ -687,7 +691,7 @@ __device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shar
         for (int part = 0; part < 2; ++part) {                      // the prefix, the sequence
             const int lo = part ? max(n0 - front, 0) : n0, hi = part ? n1 - front : min(n1, front);
             if (lo >= hi) continue;
-            FewRange<T, D, MULTI>::run(a, part ? a.batch.table + b * a.batch.table_stride : a.prefix_table, lo, hi, part ? keys : a.prefix, part ? limit : a.prefix,
+            FewRange<T, D, MULTI, STREAM>::run(a, part ? a.batch.table + b * a.batch.table_stride : a.prefix_table, lo, hi, part ? keys : a.prefix, part ? limit : a.prefix,
                                        part ? all_see : a.prefix, kbase, vbase, own, q, first, st);
         }
         st.l += other_half(st.l);
@@ -770,7 +774,7 @@ struct ManyRange {
                     const int r = ((wave * kLoads + i) * 64 + lane) / H::kChunks, key = key0 + r;
                     const int page = key < keys ? list.page[(key >> shift) + list_at] : -1;
                     const uint64_t from = (uint64_t)(unsigned)page * a.page_stride + (unsigned)(key & ((1 << shift) - 1)) * a.token_stride;
-                    load_to_lds(page >= 0 ? base + from + (off[i] - (unsigned)(r - wave * 16) * a.token_stride) : zero_chunk, at + i * 1024);
+                    load_to_lds<false>(page >= 0 ? base + from + (off[i] - (unsigned)(r - wave * 16) * a.token_stride) : zero_chunk, at + i * 1024);
                 }
             }
         };
@@ -1044,14 +1048,14 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void many_rows_kerne
     many_rows<T, D>(a, blockIdx.x, shared);
 }
 
-template <class T, int D, bool MULTI, bool FRONT>
+template <class T, int D, bool MULTI, bool FRONT, bool STREAM>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel(AttentionArgs a, AttentionArgs front, int front_blocks) {
     __shared__ Shared<T, D> shared;
     if constexpr (FRONT) {
         const int block = blockIdx.x;
         if (block < front_blocks) many_rows<T, D>(front, block, shared);
-        else few_rows<T, D, MULTI>(a, block - front_blocks, shared);
-    } else few_rows<T, D, MULTI>(a, blockIdx.x, shared);
+        else few_rows<T, D, MULTI, STREAM>(a, block - front_blocks, shared);
+    } else few_rows<T, D, MULTI, STREAM>(a, blockIdx.x, shared);
 }
 
 // ------------------------------------------------------------------------------------------------

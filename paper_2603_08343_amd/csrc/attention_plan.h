@@ -108,6 +108,14 @@ inline int gang_log2_of(int32_t heads, int64_t row_bytes, int64_t head_stride_by
     return row_bytes % 128 != 0 && head_stride_bytes == row_bytes && heads % (1 << kGangLog2) == 0 ? kGangLog2 : 0;
 }
 
+// Whether the few-rows kernel reads keys and values past the caches: where a call's own ones are more than half of the 256 MB Infinity Cache, so that
+// little of them would be left there for the next step.  Lengths are on the GPU: it goes by what they can be.  32 x 128 heads, 8 key heads, kept / past, the
+// same cache read again every third call: 65 MB 20.9 / 21.5 us, 98 MB 25.8 / 25.3, 130 MB 33.9 / 30.8, 1 GB 191 / 169; with four heads side by side
+// (lines shared by two loads) 96.8 / 100.3.
+inline bool streams(int32_t B, int32_t heads, int32_t head_dim, int64_t size, int64_t max_length, int32_t gang_log2) {
+    return gang_log2 == 0 && (double)B * max_length * heads * head_dim * 2 * size >= 130e6;
+}
+
 // Argument checks, in the order of the status codes.
 inline bool good_rows(const wht_attention_rows_t* r, int heads, int head_dim, int size) {
     return ((uintptr_t)r->data & 15u) == 0 && r->token_stride * size % 16 == 0 && r->head_stride * size % 16 == 0 && r->token_stride >= 0 &&

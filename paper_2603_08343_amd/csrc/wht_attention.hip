@@ -15,6 +15,14 @@ static int with_type(int dtype, int head_dim, F&& f) {
     return dtype == WHT_DTYPE_F32 ? width(float{}) : width(bf16{});
 }
 
+// f with a std::bool_constant for each of three flags.
+template <class F>
+static void with_flags(F&& f, bool a, bool b, bool c) {
+    auto third = [&](auto x, auto y) { if (c) f(x, y, std::true_type{}); else f(x, y, std::false_type{}); };
+    auto second = [&](auto x) { if (b) third(x, std::true_type{}); else third(x, std::false_type{}); };
+    if (a) second(std::true_type{}); else second(std::false_type{});
+}
+
 static int launched() { return hipGetLastError() == hipSuccess ? WHT_OK : WHT_ERR_LAUNCH; }
 
 // Rows up to which 16, or 4, waves share a row's pieces: where few rows have to fill the chip.
@@ -85,6 +93,7 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     a.use_prefix = !p.front && prefix > 0;
     a.front_item = p.front && p.front_few;
     a.gang_log2 = gang_log2_of(c->heads, c->head_dim * size, a.head_stride);
+    const bool stream_keys = streams(b->B, c->heads, c->head_dim, size, a.batch.most + (a.use_prefix ? prefix : 0), a.gang_log2);
     a.splits = p.own_splits; a.tiles = (int)tiles_one; a.rows_cap = p.own_cap;
     a.part = reinterpret_cast<float*>(ws + p.own_at); a.sums = reinterpret_cast<float*>(ws + p.own_sums_at);
     a.cum = reinterpret_cast<int*>(ws + p.cum_at);
@@ -95,13 +104,10 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
         constexpr int D = decltype(d)::value;
         const dim3 grid((unsigned)(front_blocks + own_blocks)), block(256);
         if (!p.own_few) hipLaunchKernelGGL((many_rows_kernel<E, D>), grid, block, 0, stream, a);
-        else if (max_q == 1) {                                      // a sequence's rows all see the same keys
-            if (front_blocks) hipLaunchKernelGGL((few_rows_kernel<E, D, false, true>), grid, block, 0, stream, a, f, (int)front_blocks);
-            else hipLaunchKernelGGL((few_rows_kernel<E, D, false, false>), grid, block, 0, stream, a, f, 0);
-        } else {
-            if (front_blocks) hipLaunchKernelGGL((few_rows_kernel<E, D, true, true>), grid, block, 0, stream, a, f, (int)front_blocks);
-            else hipLaunchKernelGGL((few_rows_kernel<E, D, true, false>), grid, block, 0, stream, a, f, 0);
-        }
+        else
+            with_flags([&](auto multi, auto front, auto past) {
+                hipLaunchKernelGGL((few_rows_kernel<E, D, decltype(multi)::value, decltype(front)::value, decltype(past)::value>), grid, block, 0, stream, a, f, (int)front_blocks);
+            }, max_q > 1, front_blocks > 0, stream_keys);           // max_q = 1: a sequence's rows all see the same keys
         return launched();
     });
     if (rc) return rc;
