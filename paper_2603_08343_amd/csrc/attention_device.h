@@ -57,9 +57,9 @@ __device__ __forceinline__ int sequence_of(const Batch& bt, int t) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// Append: bound by memory, and one token by the latency of its chain (length -> table entry -> store).  A workgroup takes one token, so that what is
-// looked up for it -- sequence, page, angles -- is looked up once; a thread takes the same 16-byte vector pair of every
-// (256 / vectors)-th head, with that pair's cosines and sines in registers over the heads.
+// Append: bound by memory, and one token by the latency of its chain (length -> table entry -> store).  A workgroup, or a wave of it (THREADS), takes one
+// token, so that what is looked up for it -- sequence, page, angles -- is looked up once; a thread takes the same 16-byte vector pair
+// of every (THREADS / pairs)-th head, with that pair's cosines and sines in registers over the heads.
 
 struct AppendArgs {
     Batch batch;
@@ -89,10 +89,12 @@ __device__ __forceinline__ void store16(unsigned char* p, const float (&f)[16 / 
     *reinterpret_cast<u32x4*>(p) = __builtin_bit_cast(u32x4, v);
 }
 
-template <class T, int D>
+template <class T, int D, int THREADS>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
-    constexpr int N = 16 / sizeof(T), kPairs = D / (2 * N), kHeads = 256 / kPairs;
-    const int t = blockIdx.x, pair = threadIdx.x % kPairs, first = threadIdx.x / kPairs;
+    constexpr int N = 16 / sizeof(T), kPairs = D / (2 * N), kHeads = THREADS / kPairs;
+    const int thread = threadIdx.x % THREADS, pair = thread % kPairs, first = thread / kPairs;
+    const int t = THREADS == 256 ? blockIdx.x : __builtin_amdgcn_readfirstlane(blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS);
+    if (t >= a.batch.T) return;
     const int b = sequence_of(a.batch, t);
     int64_t place = -1, position = -1;
     if (b >= 0) {
@@ -144,7 +146,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
             }
         }
     };
-    if (first >= kHeads) return;                                    // 96 wide: 256 is no multiple of the pairs
+    if (first >= kHeads) return;                                    // 96 wide: the threads are no multiple of the pairs
     constexpr int kSize = sizeof(T);
     if (a.q) {
         for (int h = first; h < a.q_heads; h += kHeads) {

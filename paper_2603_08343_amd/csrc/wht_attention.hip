@@ -28,6 +28,11 @@ static int launched() { return hipGetLastError() == hipSuccess ? WHT_OK : WHT_ER
 // Rows up to which 16, or 4, waves share a row's pieces: where few rows have to fill the chip.
 constexpr int64_t kJoinRowsWide = 256, kJoinRows = 2048;
 
+// Vector pairs of a token's queries and keys from which on a workgroup takes it, not a wave.  Workgroup / wave, in us: 4 x 64 (32 pairs), 64000 tokens
+// 104 / 50; 16 and 1 x 128 (136), 32000 tokens 66 / 50; 16 and 4 x 64 float32 (160), 67966 tokens 163 / 158; 16 x 128 (256), 8326 tokens 36.5 / 39.6;
+// 32 and 8 x 128 (320), 16000 tokens 73 / 78.
+constexpr int kWideToken = 256;
+
 static int page_shift(const wht_attention_cache_t* c) { return __builtin_ctz((unsigned)c->page_size); }
 
 static Batch batch_of(const wht_attention_batch_t* b, int64_t T, int64_t most) {
@@ -55,7 +60,11 @@ static int append(const wht_attention_rows_t* q, const wht_attention_rows_t* k, 
     a.rope = rope; a.rope_rows = rope_rows; a.rotary = rotary; a.interleaved = interleaved != 0; a.position = (int)position;
     a.q_heads = q_heads; a.heads = c->heads; a.pages = c->pages; a.page_shift = page_shift(c);
     return with_type(dtype, c->head_dim, [&](auto t, auto d) {
-        hipLaunchKernelGGL((append_kernel<decltype(t), decltype(d)::value>), dim3((unsigned)T), dim3(256), 0, stream, a);
+        using E = decltype(t);
+        constexpr int D = decltype(d)::value;
+        const int pairs = (int)((a.q ? q_heads : 0) + c->heads) * (int)(D * sizeof(E) / 32);
+        if (pairs < kWideToken) hipLaunchKernelGGL((append_kernel<E, D, 64>), dim3((unsigned)ceil_div64(T, 4)), dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((append_kernel<E, D, 256>), dim3((unsigned)T), dim3(256), 0, stream, a);
         return launched();
     });
 }
