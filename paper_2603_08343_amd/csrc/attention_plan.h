@@ -57,9 +57,11 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
     AttentionPlan p{};
     const int64_t G = q_heads / heads;
     p.own_few = max_q * G <= kFewRows;
-    // Several sequences of few rows each: their rows together read the prefix once.  Where a sequence's own rows fill
-    // tiles by themselves nothing is saved by that, and prefix and own keys are one range.
-    p.front = prefix > 0 && B > 1 && p.own_few;
+    // Several sequences of few rows each: their rows together read the prefix once.  Where a sequence's own rows fill tiles by themselves nothing is saved
+    // by that, and prefix and own keys are one range; as where the prefix, read by every sequence, is two blocks for each worker or fewer:
+    // apart / as one range, in us: 15 sequences behind 1 token, 16 heads of 128, 28.4 / 11.9; 8 behind 2048, 8 key heads, 22.1 / 20.1;
+    // 32 behind 1024 (four blocks) 18.2 / 29.2; 200 behind 64, 16 of 64 (three) 60.5 / 50.8.
+    p.front = prefix > 0 && B > 1 && p.own_few && (int64_t)B * heads * ceil_div64(prefix, kBlockKeys) > 2 * kWorkers;
     p.front_few = T * G <= kFewRows;
     p.front_splits = p.own_splits = 1;
     if (p.front) {
