@@ -378,14 +378,6 @@ __device__ __forceinline__ void weigh(f32x16& s, float scale, RowState<H>& st) {
     st.l += sum[0] + sum[1];
 }
 
-// Values that are not finite, as zeros.
-__device__ __forceinline__ bf16x8 finite(bf16x8 v) {
-    u32x4 x = __builtin_bit_cast(u32x4, v);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] &= ((x[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((x[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
-    return __builtin_bit_cast(bf16x8, x);
-}
-
 // The A operand of the second product in bfloat16: 16 of 32 values in LDS at `buf` (ks: which), 32 columns from 32 d on.  A transposing read gives
 // lane i of 16 the i-th of 16 columns, four rows of it, that the 16 lanes address as 4 x 4 pieces of 8 bytes.
 template <int D>
@@ -405,22 +397,17 @@ __device__ __forceinline__ bf16x8 values(unsigned buf, int ks, int d) {
     return v;
 }
 
-// o += (V^T P^T) over 32 keys in LDS at `buf`, for the 32 columns of V from 32 d on.  GUARD: where `odd`, values that are not finite stay out.
-template <class T, int D, bool GUARD>
-__device__ __forceinline__ void block_product(unsigned buf, int d, const f32x16& p, bool odd, f32x16& o) {
+// o += (V^T P^T) over 32 keys in LDS at `buf`, for the 32 columns of V from 32 d on.
+template <class T, int D>
+__device__ __forceinline__ void block_product(unsigned buf, int d, const f32x16& p, f32x16& o) {
     using H = Head<T, D>;
     if constexpr (!H::kF32) {
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 v = values<D>(buf, ks, d), w;
+            bf16x8 w;
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = (bf16)p[ks * 8 + i];
-            if constexpr (GUARD)
-                if (odd) {
-                    asm volatile("");                               // a branch: not computed where it is not needed
-                    v = finite(v);
-                }
-            o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, o, 0, 0, 0);
+            o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values<D>(buf, ks, d), w, o, 0, 0, 0);
         }
     } else {
         constexpr bool kFlip = (H::kChunks & (H::kChunks - 1)) == 0;
@@ -429,8 +416,7 @@ __device__ __forceinline__ void block_product(unsigned buf, int d, const f32x16&
                                   : buf + h4 * H::kRowBytes + H::v_place(h4, d * 8 + (col >> 2)) * 16 + (col & 3) * 4;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            float v = lds_read<float>(at + ((i >> 2) * 8 + (i & 3)) * H::kRowBytes);
-            if constexpr (GUARD) v = fabsf(v) < __builtin_inff() ? v : 0.0f;
+            const float v = lds_read<float>(at + ((i >> 2) * 8 + (i & 3)) * H::kRowBytes);
             o = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], o, 0, 0, 0);
         }
     }
@@ -470,37 +456,41 @@ __device__ __forceinline__ void add_odd(int seen, const FirstOdd<D>& first, RowS
         }
 }
 
-// Of 32 rows in LDS, by one wave.
+// Of 32 rows in LDS, by one wave, which makes zeros of them.
 template <class T, int D>
-__device__ __forceinline__ void find_odd(unsigned buf, FirstOdd<D>& first) {
+__device__ __forceinline__ void take_odd(unsigned buf, FirstOdd<D>& first) {
     using H = Head<T, D>;
     for (int c = threadIdx.x & 63; c < D; c += 64) {
         int above = 32, below = 32;
 #pragma unroll 1
         for (int k = 31; k >= 0; --k) {
-            const float v = (float)lds_read<T>(buf + k * H::kRowBytes + H::v_place(k, c * (int)sizeof(T) / 16) * 16 + c * (int)sizeof(T) % 16);
+            auto* p = (__attribute__((address_space(3))) T*)(uintptr_t)(buf + k * H::kRowBytes + H::v_place(k, c * (int)sizeof(T) / 16) * 16 + c * (int)sizeof(T) % 16);
+            const float v = (float)*p;
             if (!(fabsf(v) < __builtin_inff())) {
                 if (v != WHT_NEG_INF) above = k;
                 if (v != -WHT_NEG_INF) below = k;
+                *p = (T)0.0f;
             }
         }
         first.above[c] = above;
         first.below[c] = below;
     }
-    reads_done();                                                   // the wave's own writes: no other wave looks at `first`
+    reads_done();                                                   // the wave's own writes: no other wave looks at `first` or the rows
 }
 
-// O^T += V^T P^T over 32 keys.  A key that a row does not see has a weight of zero, and zero times infinity would still be NaN: where rows of
-// the tile see different keys (GUARD; a row sees the first `seen` of the 32), values that are not finite stay out of the product, and the
-// rows that see one get it by itself.
+// O^T += V^T P^T over 32 keys in LDS at `buf`, which are this wave's.  A key that a row does not see has a weight of zero, and zero times infinity would still
+// be NaN: where rows see different ones of the keys (GUARD, `uneven`; a row sees the first `seen` of the 32), values that are not finite
+// stay out of the product, and the rows that see one get it by itself.
 template <class T, int D, bool GUARD>
-__device__ __forceinline__ void accumulate(unsigned buf, const f32x16& p, int seen, FirstOdd<D>& first, RowState<Head<T, D>>& st) {
+__device__ __forceinline__ void accumulate(unsigned buf, const f32x16& p, int seen, bool uneven, FirstOdd<D>& first, RowState<Head<T, D>>& st) {
     bool odd = false;
-    if constexpr (GUARD) odd = any_odd<T, Head<T, D>::kChunks / 2>(buf);
+    if constexpr (GUARD) {
+        odd = uneven && any_odd<T, Head<T, D>::kChunks / 2>(buf);
+        if (odd) take_odd<T, D>(buf, first);
+    }
 #pragma unroll
-    for (int d = 0; d < Head<T, D>::kBlocks; ++d) block_product<T, D, GUARD>(buf, d, p, odd, st.o[d]);
+    for (int d = 0; d < Head<T, D>::kBlocks; ++d) block_product<T, D>(buf, d, p, st.o[d]);
     if (odd) {
-        find_odd<T, D>(buf, first);
         add_odd<T, D>(seen, first, st);
         reads_done();
     }
@@ -603,7 +593,7 @@ struct FewRange {
                 weigh(s[0], a.scale, st);
                 if (more) wait_loads<kLoads>();
                 else wait_loads<0>();
-                accumulate<T, D, MULTI>(vbuf, s[0], limit - key0, odd, st);
+                accumulate<T, D, MULTI>(vbuf, s[0], limit - key0, all_see < min(key0 + kBlockKeys, keys), odd, st);
                 key0 = next;
                 if (!more) break;
                 issue<true>(off, vbase, vbuf);
@@ -870,7 +860,7 @@ struct ManyRange {
 #pragma unroll
                 for (int i = 0; i < H::kSteps; ++i) ahead = score_step<T>(frag[i], q[i], ahead);
                 weigh(s, a.scale, st);
-                accumulate<T, D, false>(vat, s, 0, odd, st);
+                accumulate<T, D, false>(vat, s, 0, false, odd, st);
                 read_keys(kat);
                 if (more) rebase<H, 8>(largest(ahead), a.scale, st);
             }
@@ -916,7 +906,7 @@ struct ManyRange {
                 const unsigned values = values_at(t, half);
 #pragma unroll
                 for (int d = 0; d < H::kBlocks; ++d) {
-                    block_product<T, D, false>(values, d, s, false, st.o[d]);
+                    block_product<T, D>(values, d, s, st.o[d]);
                     asm volatile("" ::: "memory");                  // one block's values in registers at a time
                 }
                 if (more) {
