@@ -203,8 +203,7 @@ struct AttentionArgs {
     int64_t head_stride;                            // bytes
     unsigned page_stride, token_stride;             // bytes
     int q_heads, heads, G, pages, page_shift, prefix, max_q;
-    int splits, tiles, rows_cap;                    // rows_cap: rows of one slot of partial results
-    int stacked;                                    // many rows: those of all sequences, against the prefix alone
+    int splits, fill, rows_cap;                     // fill: the workgroups (of each die) that take the rows no tile covers; rows_cap: rows of one slot of partial results
     int use_prefix;                                 // the range begins with the prefix
     int gang_log2;                                  // few rows: heads that a worker takes side by side
     int front_item;                                 // few rows: the rows of all sequences against the prefix are one more sequence on the line
@@ -972,7 +971,8 @@ __device__ __forceinline__ void fill_rows(const AttentionArgs& a, int group) {
     fill(last + (int)((int64_t)left * group / kFillGroups), last + (int)((int64_t)left * (group + 1) / kFillGroups), 0.0f, WHT_NEG_INF);
 }
 
-template <class T, int D>
+// STACKED: the rows of all sequences, against the prefix alone.
+template <class T, int D, bool STACKED>
 __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Shared<T, D>& shared) {
     using H = Head<T, D>;
     using R = ManyRange<T, D>;
@@ -980,28 +980,51 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
     auto& list = shared.list;
     auto& odd = shared.odd;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int B = a.stacked ? 1 : a.batch.B;
-    // Workgroups go to the 8 dies in turn: a die takes whole groups (a sequence's head and share of its keys), so that their keys are in its L2
-    // once, tile after tile, the tiles that see most first.
-    const int groups = B * a.heads * a.splits, x = block & 7, y = block >> 3;
-    const int group = x + 8 * (y / a.tiles), tile = a.tiles - 1 - y % a.tiles;
-    if (group >= groups) {
-        // the grid's last workgroups, one per die
-        if (!a.stacked && a.splits == 1 && y / a.tiles == ceil_div(groups, 8)) fill_rows<T, D>(a, x);
-        return;
+    const int x = block & 7, y = block >> 3, groups = a.heads * a.splits;
+    auto tiles_of = [&](int queries) { return (int)(((int64_t)queries * a.G + kTileRows - 1) / kTileRows); };
+    int b = 0, cum = 0;
+    Sequence s{0, a.batch.T, 0};
+    if constexpr (STACKED) {
+        if (y >= die_groups(0, groups, x) * tiles_of(s.queries)) return;
+    } else {
+        if (y == a.fill) {                                          // the grid's last workgroups, one per die
+            if (a.splits == 1) fill_rows<T, D>(a, x);
+            return;
+        }
+        // Which tile: the line of the die's groups' tiles, looked up as the few-rows kernel looks up its own line.
+        const int B = a.batch.B, run = max(ceil_div(B, 64), 1), b0 = min(B, lane * run), b1 = min(B, b0 + run);
+        auto tiles_at = [&](int i) { return die_groups(i, groups, x) * tiles_of(min(s.queries, a.max_q)); };
+        int mine = 0;
+        for (int i = b0; i < b1; ++i) {
+            s = sequence(a.batch, i);
+            mine += tiles_at(i);
+        }
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (y >= __builtin_amdgcn_readlane(upto, 63)) return;
+        const int from = __popcll(__ballot(upto <= y));             // the lane whose run has it
+        b = from * run;
+        cum = __builtin_amdgcn_readlane(upto - mine, from);
+        if (run == 1) s = {__builtin_amdgcn_readlane(s.first, b), __builtin_amdgcn_readlane(s.queries, b), __builtin_amdgcn_readlane(s.length, b)};
+        else
+            for (s = sequence(a.batch, b); y >= cum + tiles_at(b); s = sequence(a.batch, ++b)) cum += tiles_at(b);
     }
-    const int split = group % a.splits, head = group / a.splits % a.heads, b = group / a.splits / a.heads;
-    const Sequence s = a.stacked ? Sequence{0, a.batch.T, 0} : sequence(a.batch, b);
-    const int queries = a.stacked ? s.queries : min(s.queries, a.max_q);
+    const int queries = STACKED ? s.queries : min(s.queries, a.max_q);
+    // of a group the tiles that see most come first
+    const int tiles = tiles_of(queries), k = (y - cum) / tiles, tile = tiles - 1 - (y - cum - k * tiles);
+    const int group = die_group(b, groups, x, k), split = group % a.splits, head = group / a.splits;
     const int64_t rows = (int64_t)queries * a.G;
-    if ((int64_t)tile * kTileRows >= rows) return;
     const int row0 = tile * kTileRows + wave * 32, row = row0 + (lane & 31);
     const int token = row / a.G, qh = head * a.G + row % a.G;
     const bool there = row < rows;
     u32x4 q[H::kSteps];
     load_row<T, D>(a.q + (s.first + (there ? token : 0)) * a.q_ts + qh * a.q_hs, there, q);
     // own tokens that row r of the tile sees: length - queries + its token + 1
-    auto sees = [&](int64_t r) { return a.stacked ? 0 : min(max(s.length - s.queries + (int)(min(r, rows - 1) / a.G) + 1, 0), s.length); };
+    auto sees = [&](int64_t r) { return STACKED ? 0 : min(max(s.length - s.queries + (int)(min(r, rows - 1) / a.G) + 1, 0), s.length); };
     const int keys = sees(tile * kTileRows + kTileRows - 1);
     const int limit = sees(row), all_see = sees(row0), any_sees = row0 < rows ? sees(row0 + 31) : -1;
     const int front = a.use_prefix ? ceil_div(a.prefix, kStepKeys) : 0;
@@ -1010,12 +1033,12 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
     RowState<H> st;
     st.clear();
     const unsigned char *kbase = a.k + head * a.head_stride, *vbase = a.v + head * a.head_stride;
-    const Keys k{a.prefix_table, a.batch.table + b * a.batch.table_stride, front, a.use_prefix ? a.prefix : 0, keys};
-    R::run(a, k, list, t0, t1, limit, all_see, any_sees, sees((int64_t)tile * kTileRows), kbase, vbase, __builtin_amdgcn_readfirstlane(lds_address(buf)), q, odd[0], st);
+    const Keys keys_of{a.prefix_table, a.batch.table + b * a.batch.table_stride, front, a.use_prefix ? a.prefix : 0, keys};
+    R::run(a, keys_of, list, t0, t1, limit, all_see, any_sees, sees((int64_t)tile * kTileRows), kbase, vbase, __builtin_amdgcn_readfirstlane(lds_address(buf)), q, odd[0], st);
     if (!there) return;
     st.l += other_half(st.l);
     const int64_t t = s.first + token;
-    if (a.splits > 1 || a.stacked) {
+    if (a.splits > 1 || STACKED) {
         const int64_t at = ((int64_t)split * a.batch.T + t) * a.q_heads + qh;
         if (lane < 32) { a.sums[at * 2] = st.m; a.sums[at * 2 + 1] = st.l; }
 #pragma unroll
@@ -1042,7 +1065,7 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
 template <class T, int D>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void many_rows_kernel(AttentionArgs a) {
     __shared__ Shared<T, D> shared;
-    many_rows<T, D>(a, blockIdx.x, shared);
+    many_rows<T, D, false>(a, blockIdx.x, shared);
 }
 
 template <class T, int D, bool MULTI, bool FRONT, bool STREAM>
@@ -1050,7 +1073,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel
     __shared__ Shared<T, D> shared;
     if constexpr (FRONT) {
         const int block = blockIdx.x;
-        if (block < front_blocks) many_rows<T, D>(front, block, shared);
+        if (block < front_blocks) many_rows<T, D, true>(front, block, shared);
         else few_rows<T, D, MULTI, STREAM>(a, block - front_blocks, shared);
     } else few_rows<T, D, MULTI, STREAM>(a, blockIdx.x, shared);
 }

@@ -53,6 +53,32 @@ static void walk(const std::vector<int>& lengths, int heads, int front, int rows
         }
 }
 
+// Every tile of every group is some die's, once, and within the workgroups that a die has.
+static void deal(const std::vector<int>& queries, int heads, int splits, int G) {
+    const int B = (int)queries.size(), per = heads * splits;
+    int64_t T = 0, max_q = 1;
+    for (int q : queries) { T += q; max_q = q > max_q ? q : max_q; }
+    const int64_t most = die_blocks(T, B, G, max_q, per);
+    std::set<std::pair<int, int>> seen;
+    for (int x = 0; x < 8; ++x) {
+        int64_t blocks = 0;
+        for (int b = 0; b < B; ++b) {
+            const int n = die_groups(b, per, x);
+            CHECK(n >= 0);
+            for (int k = 0; k < n; ++k) {
+                const int g = die_group(b, per, x, k);
+                CHECK(g >= 0 && g < per && (b * per + g) % 8 == x && seen.insert({b, g}).second);
+                blocks += ceil_div64((int64_t)queries[b] * G, kTileRows);
+            }
+        }
+        CHECK(blocks <= most);
+    }
+    CHECK((int64_t)seen.size() == (int64_t)B * per);
+    int64_t tiles = 0;
+    for (int q : queries) tiles += ceil_div64((int64_t)q * G, kTileRows);
+    CHECK(tiles <= most_tiles(T, B, G, max_q));
+}
+
 static void plans() {
     std::mt19937 rng(7);
     auto upto = [&](int n) { return (int)(rng() % (unsigned)n); };
@@ -150,6 +176,12 @@ int main() {
         const int most = 1 << (rng() % 16);
         for (int& n : lengths) n = (int)(rng() % (unsigned)most) * (rng() % 5 != 0);
         walk(lengths, 1 + (int)(rng() % 40), i % 3 ? 0 : (int)(rng() % 5000), 1 + (int)(rng() % 32), i % 2 ? 0 : kGangLog2);
+    }
+    for (int i = 0; i < 300; ++i) {
+        std::vector<int> queries(rng() % 60);
+        const int most = 1 + (1 << (rng() % 12));
+        for (int& n : queries) n = (int)(rng() % (unsigned)most) * (rng() % 5 != 0);
+        deal(queries, 1 + (int)(rng() % 40), 1 + (int)(rng() % 9), 1 + (int)(rng() % 17));
     }
     walk({}, 8, 0, 4, 0);
     walk({0, 0}, 8, 0, 4, kGangLog2);

@@ -89,25 +89,23 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     a.q_heads = q_heads; a.heads = c->heads; a.G = q_heads / c->heads; a.pages = c->pages; a.page_shift = page_shift(c);
     a.prefix = (int)prefix; a.max_q = max_q;
     a.scale = (float)((double)scale * 1.4426950408889634074);
-    const int64_t tiles_all = ceil_div64(T * a.G, kTileRows), tiles_one = ceil_div64((max_q < T ? max_q : T) * a.G, kTileRows);
-
-    const auto many_blocks = [](const AttentionArgs& m, int64_t groups) { return (ceil_div64(groups, 8) * m.tiles + 1) * 8; };   // the last 8: rows that no tile covers
     AttentionArgs f = a;
     int64_t front_blocks = 0;
     if (p.front && !p.front_few) {
-        f.stacked = 1; f.use_prefix = 1; f.splits = p.front_splits; f.tiles = (int)tiles_all;
+        f.use_prefix = 1; f.splits = p.front_splits;
         f.part = reinterpret_cast<float*>(ws + p.front_at); f.sums = reinterpret_cast<float*>(ws + p.front_sums_at);
-        front_blocks = many_blocks(f, (int64_t)c->heads * f.splits);
+        front_blocks = 8 * die_blocks(T, 1, a.G, T, (int64_t)c->heads * f.splits);
     }
     a.use_prefix = !p.front && prefix > 0;
     a.front_item = p.front && p.front_few;
     a.gang_log2 = gang_log2_of(c->heads, c->head_dim * size, a.head_stride);
     const bool stream_keys = streams(b->B, c->heads, c->head_dim, size, a.batch.most + (a.use_prefix ? prefix : 0), a.gang_log2);
-    a.splits = p.own_splits; a.tiles = (int)tiles_one; a.rows_cap = p.own_cap;
+    a.splits = p.own_splits; a.rows_cap = p.own_cap;
     a.part = reinterpret_cast<float*>(ws + p.own_at); a.sums = reinterpret_cast<float*>(ws + p.own_sums_at);
     a.cum = reinterpret_cast<int*>(ws + p.cum_at);
-    const int64_t own_blocks = p.own_few ? kWorkgroups : many_blocks(a, (int64_t)b->B * c->heads * a.splits);
+    const int64_t each = die_blocks(T, b->B, a.G, max_q, (int64_t)c->heads * a.splits), own_blocks = p.own_few ? kWorkgroups : (each + 1) * 8;
     if (front_blocks + own_blocks > INT32_MAX) return WHT_ERR_BAD_DIM;
+    a.fill = (int)each;
     const int rc = with_type(dtype, c->head_dim, [&](auto t, auto d) {
         using E = decltype(t);
         constexpr int D = decltype(d)::value;

@@ -79,6 +79,15 @@ def test_prompts(dtype, heads, queries, lengths, prefix, page):
     _compare(check.make(len(queries), queries, lengths, heads, page, prefix, dtype, seed=4))
 
 
+@pytest.mark.parametrize("B,heads", [(70, (2, 1, 64)), (200, (4, 4, 64)), (130, (6, 2, 128))])
+def test_a_prompt_among_many_short_ones(B, heads):
+    """More sequences than a wave has lanes, one of them long, some without a token."""
+    queries = [(i * 7) % 4 for i in range(B)]
+    queries[B // 2] = 300
+    c = check.make(B, queries, [n + (i * 5) % 40 for i, n in enumerate(queries)], heads, 16, 20, seed=31)
+    _compare(c)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_prompts_in_more_tiles_than_workgroups(dtype):
     """No partial results: the kernel writes the outputs itself, and the rows that no tile covers."""
