@@ -189,6 +189,8 @@ PyObject* paged(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!c.ok) return none();
     const int64_t T = qt->size(0), q_heads = qt->size(1);
     c.take_batch(args[3], args[4], args[5], T);
+    const int want_lse = PyObject_IsTrue(args[13]);
+    if (want_lse < 0) return nullptr;
     const int64_t prefix = whole(args[7], 0, (int64_t)1 << 30, c.ok);
     const int32_t* prefix_table = nullptr;
     if (c.ok && prefix > 0) {
@@ -231,7 +233,7 @@ PyObject* paged(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         made_out = c.empty(qt->sizes(), c.type);
         o = {made_out.data_ptr(), made_out.stride(0), made_out.stride(1)};
     }
-    if (!lse && args[13] == Py_True) {
+    if (!lse && want_lse) {
         made_lse = c.empty({T, q_heads}, at::kFloat);
         lse = static_cast<float*>(made_lse.data_ptr());
     }

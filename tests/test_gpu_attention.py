@@ -1,6 +1,7 @@
 """The paged cache's append and its attention on the GPU, against the definition in 64 bits (attention_check)."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -480,3 +481,17 @@ def test_native_marshalling_and_python_give_the_same(monkeypatch, interleaved):
     monkeypatch.setattr(attention, "_native_module", native)
     with pytest.raises(wht.WhtAttentionError, match="status 2"):
         _paged(c, scale=-1.0)
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("want_lse", [True, 1, np.True_, False, 0, None])
+def test_want_lse_is_a_truth_value(monkeypatch, native, want_lse):
+    from paper_2603_08343_amd import attention
+    if not native:
+        monkeypatch.setattr(attention, "_native_module", attention._NoNative)
+    c = check.make(2, [1, 1], [20, 30], (4, 2, 64), 16, 10, seed=32)
+    got = _paged(c, lse=want_lse)
+    if want_lse:
+        assert type(got) is tuple and got[0].shape == (2, 4, 64) and got[1].shape == (2, 4)
+    else:
+        assert got.shape == (2, 4, 64)
