@@ -110,6 +110,8 @@ def _rows(t, name, like, heads=None):
 def _cache(k_pages, v_pages):
     if k_pages.dim() != 4 or not k_pages.is_cuda or k_pages.stride(3) != 1:
         raise ValueError("k_pages must be a [pages, heads, page_size, head_dim] GPU tensor with a contiguous last dimension")
+    if 0 in k_pages.shape:
+        raise ValueError(f"k_pages must not be empty, got {list(k_pages.shape)}")
     if v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype or v_pages.device != k_pages.device or v_pages.stride() != k_pages.stride():
         raise ValueError("v_pages must match k_pages in shape, strides, dtype and device")
     pages, heads, page_size, head_dim = k_pages.shape

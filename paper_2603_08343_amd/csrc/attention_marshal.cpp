@@ -65,7 +65,7 @@ struct Call {
         const c10::impl::VirtualGuardImpl guard(c10::DeviceType::CUDA);
         if ((type != at::kFloat && type != at::kBFloat16) || guard.getDevice() != device) { ok = false; return; }
         pages = k->size(0); heads = k->size(1); page_size = k->size(2); head_dim = k->size(3);
-        if (pages > INT32_MAX || heads > INT32_MAX || page_size > INT32_MAX) { ok = false; return; }
+        if (k->numel() == 0 || pages > INT32_MAX || heads > INT32_MAX || page_size > INT32_MAX) { ok = false; return; }
         cache = {k->data_ptr(), v->data_ptr(), k->stride(0), k->stride(1), k->stride(2), (int32_t)pages, (int32_t)heads, (int32_t)page_size, (int32_t)head_dim};
     }
     // int32 [n], or [n][width]

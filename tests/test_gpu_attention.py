@@ -495,3 +495,21 @@ def test_want_lse_is_a_truth_value(monkeypatch, native, want_lse):
         assert type(got) is tuple and got[0].shape == (2, 4, 64) and got[1].shape == (2, 4)
     else:
         assert got.shape == (2, 4, 64)
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("shape", [(0, 2, 16, 64), (5, 0, 16, 64), (5, 2, 0, 64), (5, 2, 16, 0)])
+def test_empty_pages_are_refused(monkeypatch, native, shape):
+    """Behind a prefix too, whose pages are counted by the page's size."""
+    wht = _wht()
+    from paper_2603_08343_amd import attention
+    if not native:
+        monkeypatch.setattr(attention, "_native_module", attention._NoNative)
+    c = check.make(2, [1, 1], [20, 30], (4, 2, 64), 16, 10, seed=33)
+    pages = torch.empty(shape, dtype=BF16, device="cuda:0")
+    rows = torch.empty(2, shape[1], shape[3], dtype=BF16, device="cuda:0")
+    for prefix in (0, 10):
+        with pytest.raises(ValueError, match="k_pages must not be empty"):
+            wht.wht_attention_paged(c["q"], pages, pages, c["table"], c["lengths"], None, c["prefix_table"], prefix)
+    with pytest.raises(ValueError, match="k_pages must not be empty"):
+        wht.wht_attention_append(None, rows, rows, pages, pages, c["table"], c["lengths"], None)
