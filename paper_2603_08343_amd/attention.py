@@ -213,7 +213,9 @@ def wht_attention_append(q, k, v, k_pages, v_pages, table, lengths, rope, q_star
     if v.shape[0] != T:
         raise ValueError("k and v must have the same number of rows")
     qr, outr, q_heads = Rows(None, 0, 0), Rows(None, 0, 0), 0
-    if q is not None:
+    if q is None:
+        q_out = None
+    else:
         qr, q_heads = _rows(q, "q", k_pages), q.shape[1]
         if q.shape[0] != T:
             raise ValueError("q and k must have the same number of rows")

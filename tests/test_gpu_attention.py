@@ -513,3 +513,20 @@ def test_empty_pages_are_refused(monkeypatch, native, shape):
             wht.wht_attention_paged(c["q"], pages, pages, c["table"], c["lengths"], None, c["prefix_table"], prefix)
     with pytest.raises(ValueError, match="k_pages must not be empty"):
         wht.wht_attention_append(None, rows, rows, pages, pages, c["table"], c["lengths"], None)
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("T", [0, 2])
+def test_append_without_queries_returns_none(monkeypatch, native, T):
+    """Whether a q_out is given or not, which stays as it was."""
+    wht = _wht()
+    from paper_2603_08343_amd import attention
+    if not native:
+        monkeypatch.setattr(attention, "_native_module", attention._NoNative)
+    c = check.make(2, [1, 1], [20, 30], (4, 2, 64), 16, 0, seed=34)
+    if T == 0:
+        c = {**c, "k": c["k"][:0], "v": c["v"][:0], "table": c["table"][:0], "lengths": c["lengths"][:0]}
+    q_out = torch.full((T, 4, 64), 7.0, dtype=BF16, device="cuda:0")
+    for given in (None, q_out):
+        assert wht.wht_attention_append(None, c["k"], c["v"], c["k_pages"], c["v_pages"], c["table"], c["lengths"], None, q_out=given) is None
+    assert (q_out == 7.0).all()
