@@ -74,8 +74,21 @@ def wht_attention_status_string(status: int) -> str:
     return library().wht_attention_status_string(int(status)).decode()
 
 
+def _whole(x, name, bits=32):
+    """x as an int that the library's argument of so many bits holds; ctypes would cut off what does not fit."""
+    try:
+        n = int(x)
+    except (TypeError, ValueError, OverflowError):
+        raise TypeError(f"{name} must be a whole number, got {x!r}") from None
+    if n != x or not -(1 << (bits - 1)) <= n < 1 << (bits - 1):
+        raise ValueError(f"{name} must be a whole number of {bits} bits, got {x!r}")
+    return n
+
+
 def wht_attention_workspace_bytes(T, B, q_heads, heads, head_dim, max_q, max_length, prefix_length, dtype) -> int:
-    return int(library().wht_attention_workspace_bytes(T, B, q_heads, heads, head_dim, max_q, max_length, prefix_length, dtype))
+    return int(library().wht_attention_workspace_bytes(
+        _whole(T, "T", 64), _whole(B, "B"), _whole(q_heads, "q_heads"), _whole(heads, "heads"), _whole(head_dim, "head_dim"), _whole(max_q, "max_q"),
+        _whole(max_length, "max_length", 64), _whole(prefix_length, "prefix_length", 64), _whole(dtype, "dtype")))
 
 
 def wht_attention_rope_table(positions, rotary, base=10000.0, device="cuda"):
@@ -116,6 +129,8 @@ def _cache(k_pages, v_pages):
         raise ValueError("v_pages must match k_pages in shape, strides, dtype and device")
     pages, heads, page_size, head_dim = k_pages.shape
     ps, hs, ts, _ = k_pages.stride()
+    for n, name in ((pages, "the number of pages"), (heads, "heads"), (page_size, "page_size"), (head_dim, "head_dim")):
+        _whole(n, name)
     return Cache(k_pages.data_ptr(), v_pages.data_ptr(), ps, hs, ts, pages, heads, page_size, head_dim)
 
 
@@ -129,6 +144,8 @@ def _batch(table, lengths, q_starts, T, device, torch):
     if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
         raise ValueError("table must be an int32 [B, width] tensor with contiguous rows")
     B, width = table.shape
+    _whole(B, "the number of sequences")
+    _whole(width, "the table's width")
     _ints(table, "table", (B, width), device, torch)
     _ints(lengths, "lengths", (B,), device, torch)
     if q_starts is not None:
@@ -216,7 +233,7 @@ def wht_attention_append(q, k, v, k_pages, v_pages, table, lengths, rope, q_star
     if q is None:
         q_out = None
     else:
-        qr, q_heads = _rows(q, "q", k_pages), q.shape[1]
+        qr, q_heads = _rows(q, "q", k_pages), _whole(q.shape[1], "q_heads")
         if q.shape[0] != T:
             raise ValueError("q and k must have the same number of rows")
         if q_out is None:
@@ -230,13 +247,14 @@ def wht_attention_append(q, k, v, k_pages, v_pages, table, lengths, rope, q_star
         if not rope.is_cuda or rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous() \
                 or rope.device != k_pages.device:
             raise ValueError("rope must be a contiguous float32 [positions, rotary / 2, 2] tensor on the cache's device")
-        rope_rows, rotary = rope.shape[0], 2 * rope.shape[1]
+        rope_rows, rotary = rope.shape[0], _whole(2 * rope.shape[1], "rotary")
         rope_at = rope.data_ptr() or device_dummy(torch, rope.device)
+    position = _whole(position, "position", 64)
     if T == 0:
         return q_out
     with _DeviceGuard(torch, k_pages.device):
         rc = library().wht_attention_append(qr, kr, vr, outr, T, q_heads, cache, batch, rope_at, rope_rows, rotary, int(bool(interleaved)),
-                                            int(position), code, _stream_handle(stream, torch, k_pages.device))
+                                            position, code, _stream_handle(stream, torch, k_pages.device))
     if rc != 0:
         raise WhtAttentionError(rc, "wht_attention_append")
     return q_out
@@ -265,6 +283,7 @@ def wht_attention_paged(q, k_pages, v_pages, table, lengths, q_starts=None, pref
     code = _code(k_pages, torch)
     qr = _rows(q, "q", k_pages)
     T, q_heads, head_dim = q.shape
+    _whole(q_heads, "q_heads")
     batch = _batch(table, lengths, q_starts, T, k_pages.device, torch)
     if out is None:
         out = _empty((T, q_heads, head_dim), q.dtype, q.device, stream, torch)
@@ -276,16 +295,14 @@ def wht_attention_paged(q, k_pages, v_pages, table, lengths, q_starts=None, pref
             raise ValueError("lse must be a contiguous float32 [T, q_heads] tensor on q's device")
     elif want_lse:
         lse = _empty((T, q_heads), torch.float32, q.device, stream, torch)
-    prefix_length = int(prefix_length)
+    prefix_length = _whole(prefix_length, "prefix_length", 64)
     if prefix_length > 0:
         need = -(-prefix_length // k_pages.shape[2])
         if prefix_table is None or prefix_table.dim() != 1 or prefix_table.numel() < need:
             raise ValueError(f"prefix_table must name the {need} pages of prefix_length = {prefix_length}")
         _ints(prefix_table, "prefix_table", tuple(prefix_table.shape), k_pages.device, torch)
-    if max_q is None:
-        max_q = 1 if q_starts is None else max(T, 1)
-    if max_length is None:
-        max_length = table.shape[1] * k_pages.shape[2]
+    max_q = _whole(max_q, "max_q") if max_q is not None else 1 if q_starts is None else max(T, 1)
+    max_length = _whole(max_length, "max_length", 64) if max_length is not None else table.shape[1] * k_pages.shape[2]
     if scale is None:
         scale = 1.0 / math.sqrt(head_dim)
     if T > 0:
@@ -296,7 +313,7 @@ def wht_attention_paged(q, k_pages, v_pages, table, lengths, q_starts=None, pref
             raise ValueError("workspace must be a contiguous GPU tensor on q's device")
         with _DeviceGuard(torch, q.device):
             rc = library().wht_attention_paged(qr, outr, None if lse is None else lse.data_ptr(), T, q_heads, cache, batch,
-                                               prefix_table.data_ptr() if prefix_length > 0 else None, prefix_length, int(max_q), int(max_length),
+                                               prefix_table.data_ptr() if prefix_length > 0 else None, prefix_length, max_q, max_length,
                                                float(scale), code, None if workspace is None else workspace.data_ptr(),
                                                0 if workspace is None else workspace.numel() * workspace.element_size(),
                                                _stream_handle(stream, torch, q.device))

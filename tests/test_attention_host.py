@@ -6,6 +6,7 @@ import os
 import re
 import subprocess
 
+import numpy as np
 import pytest
 import torch
 
@@ -110,3 +111,22 @@ def test_without_the_extension_module_calls_are_declined_after_one_warning(monke
         native = attention._native()
         assert native.append(*[None] * 12) is None and native.paged(*[None] * 15) is None
     assert [w.category for w in recwarn] == [RuntimeWarning]
+
+
+@pytest.mark.parametrize("x,error", [(1 << 31, ValueError), (-(1 << 31) - 1, ValueError), ((1 << 32) + 1, ValueError), (1 << 64, ValueError), (2.5, ValueError),
+                                     ("7", ValueError), (None, TypeError), ("x", TypeError), (math.nan, TypeError), (math.inf, TypeError)])
+def test_numbers_that_do_not_fit_are_refused(x, error):
+    """ctypes would cut them off: max_q = 2^32 + 1 would be 1."""
+    with pytest.raises(error, match="max_q must be a whole number"):
+        wht.wht_attention_workspace_bytes(3, 3, 4, 4, 128, x, 128, 0, 1)
+    wide = (1 << 64) + 5 if x == 1 << 64 else x
+    if error is TypeError or x == 1 << 64:
+        with pytest.raises(error, match="max_length must be a whole number"):
+            wht.wht_attention_workspace_bytes(3, 3, 4, 4, 128, 1, wide, 0, 1)
+
+
+def test_whole_numbers_of_any_kind():
+    want = wht.wht_attention_workspace_bytes(3, 3, 4, 4, 128, 2, 128, 0, 1)
+    assert want > 0
+    for kind in (np.int64, np.int32, torch.tensor, float):
+        assert wht.wht_attention_workspace_bytes(3, 3, 4, 4, 128, kind(2), kind(128), kind(0), 1) == want

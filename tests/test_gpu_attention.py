@@ -530,3 +530,20 @@ def test_append_without_queries_returns_none(monkeypatch, native, T):
     for given in (None, q_out):
         assert wht.wht_attention_append(None, c["k"], c["v"], c["k_pages"], c["v_pages"], c["table"], c["lengths"], None, q_out=given) is None
     assert (q_out == 7.0).all()
+
+
+def test_numbers_that_do_not_fit_are_refused():
+    wht = _wht()
+    c = check.make(2, [1, 1], [20, 30], (4, 2, 64), 16, 10, seed=35)
+    for name, x in (("max_q", (1 << 32) + 1), ("max_q", 1.5), ("max_length", 1 << 64), ("prefix", 1 << 64), ("prefix", 9.5)):
+        with pytest.raises(ValueError, match="must be a whole number"):
+            _paged({**c, **({"prefix": x} if name == "prefix" else {})}, **({name: x} if name != "prefix" else {}))
+    with pytest.raises(ValueError, match="position must be a whole number"):
+        wht.wht_attention_append(None, c["k"], c["v"], c["k_pages"], c["v_pages"], c["table"], c["lengths"], None, position=1 << 64)
+    # as many pages as 32 bits do not count
+    wide = c["k_pages"][:1].expand(1 << 32, 2, 16, 64)
+    with pytest.raises(ValueError, match="number of pages must be"):
+        wht.wht_attention_paged(c["q"], wide, wide, c["table"], c["lengths"])
+    want = _paged(c)
+    got = _paged(c, max_q=np.int64(c["max_q"]), max_length=np.int32(c["max_length"]))
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
