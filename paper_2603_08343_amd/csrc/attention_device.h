@@ -273,16 +273,21 @@ __device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigne
 // 16 bytes per lane from memory to LDS at base + 16 * lane, past the registers.  Assembly, because the compiler would otherwise wait for
 // every such load in flight before any read of LDS; which have landed is known where wait_loads stands.  Reads of what is overwritten
 // have returned (lgkmcnt).
+// m0 is named as overwritten: the compiler, which never holds a value there for long, puts none across the statement then (that it cannot keep a reserved
+// register's value over it is what the warning says, and what is meant).
 // STREAM: read once, not kept in the caches.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 template <bool STREAM>
 __device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned to) {
-    if constexpr (STREAM) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" : : "v"(from), "s"(to) : "memory");
-    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(to) : "memory");
+    if constexpr (STREAM) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" : : "v"(from), "s"(to) : "memory", "m0");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(to) : "memory", "m0");
 }
 // The same from a place that all lanes share, `off` bytes on.
 __device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned off, unsigned to) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(from), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(from), "s"(to) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 template <int PENDING> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PENDING) : "memory"); }
 __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void workgroup_barrier() {

@@ -130,3 +130,14 @@ def test_whole_numbers_of_any_kind():
     assert want > 0
     for kind in (np.int64, np.int32, torch.tensor, float):
         assert wht.wht_attention_workspace_bytes(3, 3, 4, 4, 128, kind(2), kind(128), kind(0), 1) == want
+
+
+def test_assembly_that_writes_m0_says_so():
+    """A register that an asm statement writes and does not name may hold a value of the compiler's."""
+    statements = []
+    for name in sorted(os.listdir(CSRC)):
+        text = open(os.path.join(CSRC, name)).read()
+        statements += [s for s in re.findall(r"asm volatile\((.*?)\);", text, flags=re.S) if re.search(r"s_mov_b32 m0", s)]
+    assert len(statements) == 3
+    for s in statements:
+        assert '"m0"' in s.rsplit(":", 1)[1], s
