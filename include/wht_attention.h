@@ -110,7 +110,7 @@ size_t wht_attention_workspace_bytes(int64_t T, int32_t B, int32_t q_heads, int3
  *   prefix_table  in    [ceil(prefix_length / page_size)], NULL where prefix_length = 0
  *   max_q               at least the largest number of new tokens of a sequence
  *   max_length          at least the largest of lengths; how the work is split goes by it (width * page_size always does)
- *   scale               finite, > 0
+ *   scale               > 0, at most 2.3e38 (its product with log2(e) is finite)
  *   workspace           device scratch, 16-byte aligned, at least ..._workspace_bytes(...) bytes; contents on entry are ignored
  */
 int wht_attention_paged(const wht_attention_rows_t *q, const wht_attention_rows_t *out, float *lse, int64_t T, int32_t q_heads,

@@ -185,13 +185,19 @@ inline int check_sizes(int64_t T, int32_t B, int32_t q_heads, int32_t heads, int
     return WHT_OK;
 }
 
+// The kernels' exponentials are of base 2.
+inline float base2_scale(float scale) {
+    const double s = (double)scale * 1.4426950408889634074;
+    return s <= 3.4028234663852886e38 ? (float)s : __builtin_inff();        // past the largest float; what rounds to it is taken
+}
+
 inline int check_paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out, const float* lse, int64_t T, int32_t q_heads,
                        const wht_attention_cache_t* c, const wht_attention_batch_t* b, const int32_t* prefix_table, int64_t prefix,
                        int32_t max_q, int64_t max_length, float scale, int32_t dtype) {
     if (!q || !out || !q->data || !out->data || (prefix > 0 && !prefix_table)) return WHT_ERR_NULL_PTR;
     if (int rc = check_cache(c, b, dtype)) return rc;
     if (int rc = check_sizes(T, b->B, q_heads, c->heads, c->head_dim, max_q, max_length, prefix, dtype)) return rc;
-    if (!(scale > 0.0f) || !(scale <= 3.0e38f)) return WHT_ERR_BAD_DIM;
+    if (!(scale > 0.0f) || !(base2_scale(scale) < __builtin_inff())) return WHT_ERR_BAD_DIM;
     // the few-rows kernel counts the blocks of its line in 31 bits
     const int64_t own = (int64_t)b->width * c->page_size < max_length ? (int64_t)b->width * c->page_size : max_length;
     if (((int64_t)b->B + 1) * (own / kBlockKeys + prefix / kBlockKeys + 2) > INT32_MAX / c->heads) return WHT_ERR_BAD_DIM;

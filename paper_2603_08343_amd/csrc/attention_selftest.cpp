@@ -166,6 +166,9 @@ static void statuses() {
         CHECK(check_paged(&r0, &r0, nullptr, 3, 32, &c, &b, nullptr, 0, 1, (int64_t)1 << 20, 1.0f, 1) == WHT_ERR_BAD_DIM);
         CHECK(check_paged(&r0, &r0, nullptr, 3, 32, &c, &b, nullptr, 0, 1, 1 << 12, 1.0f, 1) == WHT_OK);
     }
+    // a scale whose product with log2(e) is infinite would make NaN of every score of zero
+    for (float s : {1e-45f, 1e-38f, 1.0f, 1e38f, 2.3e38f}) CHECK(paged(r0, 32, I, 100, 1, 256, s, 1) == WHT_OK && base2_scale(s) > 0.0f && base2_scale(s) < __builtin_inff());
+    for (float s : {2.4e38f, 3.0e38f, 3.4e38f}) CHECK(paged(r0, 32, I, 100, 1, 256, s, 1) == WHT_ERR_BAD_DIM);
     for (float s : {0.0f, -1.0f, __builtin_nanf(""), __builtin_inff()}) CHECK(paged(r0, 32, I, 100, 1, 256, s, 1) == WHT_ERR_BAD_DIM);
 }
 

@@ -88,7 +88,7 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     a.prefix_table = prefix_table;
     a.q_heads = q_heads; a.heads = c->heads; a.G = q_heads / c->heads; a.pages = c->pages; a.page_shift = page_shift(c);
     a.prefix = (int)prefix; a.max_q = max_q;
-    a.scale = (float)((double)scale * 1.4426950408889634074);
+    a.scale = base2_scale(scale);
     AttentionArgs f = a;
     int64_t front_blocks = 0;
     if (p.front && !p.front_few) {
@@ -176,7 +176,7 @@ const char* wht_attention_status_string(int status) {
     switch (status) {
     case WHT_OK:             return "ok";
     case WHT_ERR_NULL_PTR:   return "a required pointer is NULL";
-    case WHT_ERR_BAD_DIM:    return "a size is not taken: head_dim 64, 96 or 128; page_size a power of two, 8 to 1024; q_heads a multiple of heads, at most 1024; rotary a multiple of 16 up to head_dim; counts not negative and below 2^30; a page below 4 GiB; scale finite and > 0";
+    case WHT_ERR_BAD_DIM:    return "a size is not taken: head_dim 64, 96 or 128; page_size a power of two, 8 to 1024; q_heads a multiple of heads, at most 1024; rotary a multiple of 16 up to head_dim; counts not negative and below 2^30; a page below 4 GiB; scale > 0 and at most 2.3e38";
     case WHT_ERR_BAD_DTYPE:  return "dtype must be WHT_DTYPE_F32 or WHT_DTYPE_BF16";
     case WHT_ERR_MISALIGNED: return "tensors must be 16-byte aligned and their strides 16-byte steps of at least a row (heads: below 2 GiB)";
     case WHT_ERR_WORKSPACE:  return "workspace is NULL or smaller than wht_attention_workspace_bytes";
