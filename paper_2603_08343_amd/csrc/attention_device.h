@@ -56,6 +56,9 @@ __device__ __forceinline__ int sequence_of(const Batch& bt, int t) {
     return lo < bt.B ? lo : -1;
 }
 
+// Which of a grid's workgroups (grid_of) this is.
+__device__ __forceinline__ int block_of() { return (int)((blockIdx.y << kGridLog2) + blockIdx.x); }
+
 // ------------------------------------------------------------------------------------------------
 // Append: bound by memory, and one token by the latency of its chain (length -> table entry -> store).  A workgroup, or a wave of it (THREADS), takes one
 // token, so that what is looked up for it -- sequence, page, angles -- is looked up once; a thread takes the same 16-byte vector pair
@@ -94,7 +97,7 @@ template <class T, int D, int THREADS>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     constexpr int N = 16 / sizeof(T), kPairs = D / (2 * N), kHeads = THREADS / kPairs;
     const int thread = threadIdx.x % THREADS, pair = thread % kPairs, first = thread / kPairs;
-    const int t = THREADS == 256 ? blockIdx.x : __builtin_amdgcn_readfirstlane(blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS);
+    const int t = THREADS == 256 ? block_of() : __builtin_amdgcn_readfirstlane(block_of() * (256 / THREADS) + threadIdx.x / THREADS);
     if (t >= a.batch.T) return;
     const int b = sequence_of(a.batch, t);
     int64_t place = -1, position = -1;
@@ -1115,7 +1118,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Joi
     struct Share { float m, l; f32x4 o[kLanes]; };
     __shared__ Share shares[WAVES];
     const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t r = WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    const int64_t r = WAVES == 1 ? (int64_t)block_of() * 4 + (threadIdx.x >> 6) : blockIdx.x;
     if (r >= (int64_t)a.batch.T * a.q_heads) return;
     const int t = (int)(r / a.q_heads), qh = (int)(r % a.q_heads), head = qh / a.G, g = qh % a.G;
     const int b = __builtin_amdgcn_readfirstlane(sequence_of(a.batch, t));

@@ -26,7 +26,9 @@ constexpr int kStepKeys = 64;       // keys of one step of a workgroup in the ma
 constexpr int kWorkgroups = 512;    // two per compute unit
 constexpr int kWorkers = 4 * kWorkgroups;       // waves of the few-rows kernel's grid
 
-enum class Range { Own, Prefix, Both };
+// A launch has below 2^32 threads along x.  Kernels that take a token or row each have this many workgroups there, and as many rows of them as it takes.
+constexpr int kGridLog2 = 22;
+constexpr int64_t kMostWorkgroups = ((int64_t)1 << 32) / 256 - 1;       // of 256 threads, along x
 
 // What one call launches.  `front`: the rows of all sequences against the prefix; `own`: each sequence's rows against its own
 // keys -- or, where there is no front, against prefix and own keys as one range.  A front of few rows is one more sequence on the

@@ -33,6 +33,11 @@ constexpr int64_t kJoinRowsWide = 256, kJoinRows = 2048;
 // 32 and 8 x 128 (320), 16000 tokens 73 / 78.
 constexpr int kWideToken = 256;
 
+static dim3 grid_of(int64_t blocks) {
+    const int64_t x = (int64_t)1 << kGridLog2;
+    return blocks <= x ? dim3((unsigned)blocks) : dim3((unsigned)x, (unsigned)ceil_div64(blocks, x));
+}
+
 static int page_shift(const wht_attention_cache_t* c) { return __builtin_ctz((unsigned)c->page_size); }
 
 static Batch batch_of(const wht_attention_batch_t* b, int64_t T, int64_t most) {
@@ -63,8 +68,8 @@ static int append(const wht_attention_rows_t* q, const wht_attention_rows_t* k, 
         using E = decltype(t);
         constexpr int D = decltype(d)::value;
         const int pairs = (int)((a.q ? q_heads : 0) + c->heads) * (int)(D * sizeof(E) / 32);
-        if (pairs < kWideToken) hipLaunchKernelGGL((append_kernel<E, D, 64>), dim3((unsigned)ceil_div64(T, 4)), dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((append_kernel<E, D, 256>), dim3((unsigned)T), dim3(256), 0, stream, a);
+        if (pairs < kWideToken) hipLaunchKernelGGL((append_kernel<E, D, 64>), grid_of(ceil_div64(T, 4)), dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((append_kernel<E, D, 256>), grid_of(T), dim3(256), 0, stream, a);
         return launched();
     });
 }
@@ -104,7 +109,7 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     a.part = reinterpret_cast<float*>(ws + p.own_at); a.sums = reinterpret_cast<float*>(ws + p.own_sums_at);
     a.cum = reinterpret_cast<int*>(ws + p.cum_at);
     const int64_t each = die_blocks(T, b->B, a.G, max_q, (int64_t)c->heads * a.splits), own_blocks = p.own_few ? kWorkgroups : (each + 1) * 8;
-    if (front_blocks + own_blocks > INT32_MAX) return WHT_ERR_BAD_DIM;
+    if (front_blocks + own_blocks > kMostWorkgroups) return WHT_ERR_BAD_DIM;
     a.fill = (int)each;
     const int rc = with_type(dtype, c->head_dim, [&](auto t, auto d) {
         using E = decltype(t);
@@ -132,7 +137,7 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
         if (!p.own_few) hipLaunchKernelGGL((join_splits_kernel<decltype(t), decltype(d)::value>), dim3((unsigned)ceil_div64(rows, 256 / (decltype(d)::value / 4))), dim3(256), 0, stream, j);
         else if (rows <= kJoinRowsWide) hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 16>), dim3((unsigned)rows), dim3(1024), 0, stream, j);
         else if (rows <= kJoinRows) hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 4>), dim3((unsigned)rows), dim3(256), 0, stream, j);
-        else hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 1>), dim3((unsigned)ceil_div64(rows, 4)), dim3(256), 0, stream, j);
+        else hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 1>), grid_of(ceil_div64(rows, 4)), dim3(256), 0, stream, j);
         return launched();
     });
 }

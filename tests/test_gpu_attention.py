@@ -547,3 +547,32 @@ def test_numbers_that_do_not_fit_are_refused():
     want = _paged(c)
     got = _paged(c, max_q=np.int64(c["max_q"]), max_length=np.int32(c["max_length"]))
     assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+@pytest.mark.parametrize("dtype,heads,T", [(F32, (16, 128), (1 << 24) + 5), (BF16, (4, 64), (1 << 26) + 5)])
+def test_append_of_more_tokens_than_one_row_of_a_grid_has(dtype, heads, T):
+    """2^32 threads, a workgroup a token and a wave a token; all but the last five tokens are in pages that are none."""
+    wht = _wht()
+    H, D = heads
+    g = torch.Generator(device="cuda:0").manual_seed(36)
+    k, v = (torch.randn(1, H, D, generator=g, device="cuda:0").to(dtype) for _ in range(2))
+    pages = [torch.zeros(1, H, 1024, D, dtype=dtype, device="cuda:0") for _ in range(2)]
+    table = torch.full((1, T // 1024 + 1), -1, dtype=torch.int32, device="cuda:0")
+    table[0, -1] = 0
+    numbers = torch.tensor([T, 0, T], dtype=torch.int32, device="cuda:0")
+    wht.wht_attention_append(None, k.expand(T, H, D), v.expand(T, H, D), *pages, table, numbers[:1], None, numbers[1:])
+    for page, row in zip(pages, (k, v)):
+        assert (page[0, :, :5] == row[0][:, None]).all() and (page[0, :, 5:] == 0).all()
+
+
+def test_attention_of_more_rows_than_one_row_of_a_grid_has():
+    """2^26 rows to join: a wave each, 2^32 threads."""
+    B, H, D = 1 << 20, 64, 64
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("not enough memory")
+    g = torch.Generator(device="cuda:0").manual_seed(37)
+    q = torch.randn(1, H, D, generator=g, device="cuda:0").to(BF16).expand(B, H, D)
+    k_pages, v_pages = (torch.randn(2, H, 8, D, generator=g, device="cuda:0").to(BF16) for _ in range(2))
+    table = (torch.arange(B, dtype=torch.int32, device="cuda:0") & 1)[:, None]
+    out = _wht().wht_attention_paged(q, k_pages, v_pages, table, torch.ones(B, dtype=torch.int32, device="cuda:0"))
+    assert all((out[i::2] == v_pages[i, :, 0]).all() for i in range(2))             # one key each: its value
