@@ -1005,7 +1005,7 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
         int mine = 0;
         for (int i = b0; i < b1; ++i) {
             s = sequence(a.batch, i);
-            mine += tiles_at(i);
+            mine = add_tiles(mine, tiles_at(i));
         }
         int upto = mine;
 #pragma unroll

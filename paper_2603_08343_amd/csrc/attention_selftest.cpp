@@ -79,6 +79,31 @@ static void deal(const std::vector<int>& queries, int heads, int splits, int G) 
     CHECK(tiles <= most_tiles(T, B, G, max_q));
 }
 
+// Starts that do not ascend give many sequences all of T: the many-rows kernel's look-up still ends at one of the batch that has tiles.
+static void deal_to_overlapping(int B, int64_t T, int heads, int G) {
+    const int splits = splits_for(most_tiles(T, B, G, T) * heads, 1 << 20), per = heads * splits, run = ceil_div(B, 64);
+    auto tiles_at = [&](int i, int x) { return die_groups(i, per, x) * (i % 2 ? 0 : (int)ceil_div64(T * G, kTileRows)); };
+    const int64_t most = die_blocks(T, B, G, T, per);
+    CHECK(most <= kMostWorkgroups / 8);
+    for (int x = 0; x < 8; x += 7) {
+        int upto[64], last = 0;
+        for (int lane = 0; lane < 64; ++lane) {
+            int mine = 0;
+            for (int i = lane * run; i < B && i < (lane + 1) * run; ++i) mine = add_tiles(mine, tiles_at(i, x));
+            last = upto[lane] = last + mine;
+        }
+        for (int64_t y = 0; y <= most; y = y * 5 / 4 + 1) {
+            if (y >= upto[63]) continue;
+            int from = 0;
+            while (upto[from] <= y) ++from;
+            int b = from * run;
+            int64_t cum = from ? upto[from - 1] : 0;
+            for (; b < B && y >= cum + tiles_at(b, x); ++b) cum += tiles_at(b, x);
+            CHECK(b < B && tiles_at(b, x) > 0);
+        }
+    }
+}
+
 static void plans() {
     std::mt19937 rng(7);
     auto upto = [&](int n) { return (int)(rng() % (unsigned)n); };
@@ -186,6 +211,9 @@ int main() {
         for (int& n : queries) n = (int)(rng() % (unsigned)most) * (rng() % 5 != 0);
         deal(queries, 1 + (int)(rng() % 40), 1 + (int)(rng() % 9), 1 + (int)(rng() % 17));
     }
+    deal_to_overlapping(1 << 20, 1 << 19, 8, 128);
+    deal_to_overlapping(8192, 1 << 20, 8, 128);
+    deal_to_overlapping(70, 5000, 8, 4);
     walk({}, 8, 0, 4, 0);
     walk({0, 0}, 8, 0, 4, kGangLog2);
     walk({1}, 1, 0, 1, 0);
