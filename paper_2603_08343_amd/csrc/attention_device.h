@@ -248,15 +248,15 @@ struct Head {
     }
 };
 
-// What a lane of a row (column of the products) keeps: the row's maximum so far (scaled, base 2), this lane's share of the sum,
-// and its half of the row's outputs.
+// What a lane of a row (column of the products) keeps: the score that the row's weights are relative to (its maximum, or a little less: rebase), how far scores may
+// pass it, what is taken off a scaled score in front of the exponential, this lane's share of the sum, and its half of the row's outputs.
 template <class H>
 struct RowState {
-    float m, l;
+    float top, most, base, l;
     f32x16 o[H::kBlocks];
     __device__ __forceinline__ void clear() {
-        m = WHT_NEG_INF;
-        l = 0.0f;
+        top = most = WHT_NEG_INF;                                   // nothing seen yet: weights of zero
+        base = l = 0.0f;
 #pragma unroll
         for (int d = 0; d < H::kBlocks; ++d)
 #pragma unroll
@@ -352,18 +352,31 @@ __device__ __forceinline__ int key_of(int i) { return (i >> 2) * 8 + ((threadIdx
 // one multiplies all the sums over.  Weights are up to 256 then, which float32 sums hold as exactly; but the largest of a row is no longer
 // 1, which bfloat16 holds exactly: the error of the outputs, with that of their own rounding, goes from 1.9e-3 to 2.3e-3 of their norm.
 // With few rows, bound by memory, it is 0.
+//
+// A weight is exp2(s scale - base), one rounding, with base = top scale rounded: what that rounding is off by is a factor that all weights share, but for those that bfloat16
+// rounds and their sum, which is not rounded.  Of a maximum of 2^31 it may be 2^128 or 2^-128, and the weights infinite or zero.  From kFar on, where the factor may be 1 + 2e-5,
+// the maximum is taken off the scores themselves (exactly where it matters), in every step, and the base is zero.
+constexpr float kFar = 1024.0f;
+
 template <class H, int SLACK>
-__device__ __forceinline__ void rebase(float mx, float scale, RowState<H>& st) {
-    mx = fmaxf(mx, other_half(mx)) * scale;
-    if (__any(mx > st.m + (float)SLACK || (st.m == WHT_NEG_INF && mx > WHT_NEG_INF))) {
-        const float now = fmaxf(st.m, mx);
-        const float f = __builtin_amdgcn_exp2f(st.m - (now == WHT_NEG_INF ? 0.0f : now));
+__device__ __forceinline__ void rebase(float mx, float scale, f32x16& s, RowState<H>& st) {
+    mx = fmaxf(mx, other_half(mx));
+    if (__any(mx > st.most)) {
+        const float now = fmaxf(st.top, mx), m = now == WHT_NEG_INF ? 0.0f : now * scale;
+        const bool far = fabsf(m) >= kFar;
+        const float f = __builtin_amdgcn_exp2f(far ? (st.top - now) * scale : st.top * scale - m);
         st.l *= f;
 #pragma unroll
         for (int d = 0; d < H::kBlocks; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) st.o[d][i] *= f;
-        st.m = now;
+        st.top = now;
+        st.base = far ? 0.0f : m;
+        st.most = far ? WHT_NEG_INF : SLACK == 0 ? now : now + fminf(SLACK / scale, 3e38f);
+        if (__any(far)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] -= far ? now : 0.0f;
+        }
     }
 }
 __device__ __forceinline__ float largest(const f32x16& s) {
@@ -376,11 +389,10 @@ __device__ __forceinline__ float largest(const f32x16& s) {
 // Scores become weights, and their sum.
 template <class H>
 __device__ __forceinline__ void weigh(f32x16& s, float scale, RowState<H>& st) {
-    const float base = st.m == WHT_NEG_INF ? 0.0f : st.m;           // nothing seen yet: weights of zero
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -base));
+        s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -st.base));
         sum[i & 1] += s[i];
     }
     st.l += sum[0] + sum[1];
@@ -598,7 +610,7 @@ struct FewRange {
                         s[0][i] = key < limit && at >= 0 ? s[0][i] : WHT_NEG_INF;
                     }
                 }
-                rebase<H, 0>(largest(s[0]), a.scale, st);
+                rebase<H, 0>(largest(s[0]), a.scale, s[0], st);
                 weigh(s[0], a.scale, st);
                 if (more) wait_loads<kLoads>();
                 else wait_loads<0>();
@@ -698,7 +710,7 @@ __device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shar
         st.l += other_half(st.l);
         if (row < rows) {
             const int64_t at = (((int64_t)(b * groups + group + worker) << a.gang_log2) + in_gang) * a.rows_cap + row;
-            if (lane < 32) *reinterpret_cast<f32x2*>(a.sums + at * 2) = f32x2{st.m, st.l};
+            if (lane < 32) *reinterpret_cast<f32x2*>(a.sums + at * 2) = f32x2{st.top * a.scale, st.l};
 #pragma unroll
             for (int d = 0; d < H::kBlocks; ++d)
 #pragma unroll
@@ -837,7 +849,6 @@ struct ManyRange {
         // more keys, these are what lies there, and not used.
         auto full_block = [&](f32x16& s, f32x16& ahead, unsigned vat, unsigned kat, bool more) {
             if constexpr (!H::kF32) {
-                const float base = st.m == WHT_NEG_INF ? 0.0f : st.m;
                 const unsigned first_chunk = KeyReads<T, D>::first(kat);
                 bf16x8 w[2];
                 float sum[2] = {0.0f, 0.0f};
@@ -848,7 +859,7 @@ struct ManyRange {
                     frag[i] = __builtin_bit_cast(u32x4, values<D>(vat, i / H::kBlocks, i % H::kBlocks));
 #pragma unroll
                     for (int e = 16 * i / H::kSteps; e < 16 * (i + 1) / H::kSteps; ++e) {
-                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale, -base));
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale, -st.base));
                         sum[e & 1] += p;
                         w[e >> 3][e & 7] = (bf16)p;
                     }
@@ -866,7 +877,7 @@ struct ManyRange {
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 st.l += sum[0] + sum[1];
-                if (more) rebase<H, 8>(mx, a.scale, st);
+                if (more) rebase<H, 8>(mx, a.scale, ahead, st);
             } else {
                 ahead = f32x16{};
 #pragma unroll
@@ -874,7 +885,7 @@ struct ManyRange {
                 weigh(s, a.scale, st);
                 accumulate<T, D, false>(vat, s, 0, false, odd, st);
                 read_keys(kat);
-                if (more) rebase<H, 8>(largest(ahead), a.scale, st);
+                if (more) rebase<H, 8>(largest(ahead), a.scale, ahead, st);
             }
         };
         load_k(lo);
@@ -884,7 +895,7 @@ struct ManyRange {
         workgroup_barrier();
         f32x16 s = scores<T, D>(keys_at(lo, 0), q), other;
         if (bad || !full(2 * lo)) hide(s, 2 * lo);
-        rebase<H, 8>(largest(s), a.scale, st);
+        rebase<H, 8>(largest(s), a.scale, s, st);
         read_keys(keys_at(lo, 1));
         // A step's barrier stands in both loops below: a wave takes a step in either, whatever the others do.
         for (int t = lo; t < hi; ++t) {
@@ -924,7 +935,7 @@ struct ManyRange {
                 if (more) {
                     if (t + 1 < hi) read_keys(keys_at(t + 1, half));
                     if (bad || !full(j + 1)) hide(other, j + 1);
-                    rebase<H, 8>(largest(other), a.scale, st);
+                    rebase<H, 8>(largest(other), a.scale, other, st);
                     s = other;
                 }
             }
@@ -1048,7 +1059,7 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
     const int64_t t = s.first + token;
     if (a.splits > 1 || STACKED) {
         const int64_t at = ((int64_t)split * a.batch.T + t) * a.q_heads + qh;
-        if (lane < 32) { a.sums[at * 2] = st.m; a.sums[at * 2 + 1] = st.l; }
+        if (lane < 32) { a.sums[at * 2] = st.top * a.scale; a.sums[at * 2 + 1] = st.l; }
 #pragma unroll
         for (int d = 0; d < H::kBlocks; ++d)
 #pragma unroll
@@ -1056,7 +1067,7 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
                 *reinterpret_cast<f32x4*>(a.part + at * D + d * 32 + i * 8 + (lane >> 5) * 4) = f32x4{st.o[d][4 * i], st.o[d][4 * i + 1], st.o[d][4 * i + 2], st.o[d][4 * i + 3]};
     } else {
         const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
-        if (a.lse && lane < 32) a.lse[t * a.q_heads + qh] = st.l == 0.0f ? WHT_NEG_INF : (st.m + __builtin_amdgcn_logf(st.l)) * kLn2;
+        if (a.lse && lane < 32) a.lse[t * a.q_heads + qh] = st.l == 0.0f ? WHT_NEG_INF : (st.top * a.scale + __builtin_amdgcn_logf(st.l)) * kLn2;
 #pragma unroll
         for (int d = 0; d < H::kBlocks; ++d)
 #pragma unroll

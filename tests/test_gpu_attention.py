@@ -576,3 +576,40 @@ def test_attention_of_more_rows_than_one_row_of_a_grid_has():
     table = (torch.arange(B, dtype=torch.int32, device="cuda:0") & 1)[:, None]
     out = _wht().wht_attention_paged(q, k_pages, v_pages, table, torch.ones(B, dtype=torch.int32, device="cuda:0"))
     assert all((out[i::2] == v_pages[i, :, 0]).all() for i in range(2))             # one key each: its value
+
+
+def far_scores(c, seed):
+    """Queries and keys whose scores are exact and so far apart that the greatest takes all the weight: q's first element is 181 times a power of two of either sign, the
+    keys' one of five, three of them common; beside them rows of ordinary size.  Returns where the exact rows are."""
+    g = torch.Generator().manual_seed(seed)
+    T, Hq, _ = c["q"].shape
+    sizes = torch.tensor([4.0] + [181 * 2.0 ** e for e in (11, 12, 14, 27, 28, 31, 53, 93)])
+    pick = torch.randint(0, len(sizes), (T, Hq), generator=g)
+    q, sign = torch.zeros(c["q"].shape), torch.randint(0, 2, (T, Hq), generator=g) * 2 - 1
+    q[:, :, 0] = sizes[pick] * sign
+    k = torch.zeros(c["k_pages"].shape)
+    levels = torch.tensor([0.5, 0.25, 0.125])[torch.randint(0, 3, k.shape[:3], generator=g)]
+    rare = torch.rand(k.shape[:3], generator=g)
+    levels[rare < 0.02], levels[rare > 0.98] = 1.0, 0.0625
+    k[..., 0] = levels
+    c["q"].copy_(q)
+    c["k_pages"].copy_(k)
+    return pick > 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads", [(4, 4, 64), (6, 2, 96), (8, 2, 128)])
+@pytest.mark.parametrize("queries,lengths,prefix", [([1] * 6, [0, 1, 33, 300, 64, 700], 0), ([1] * 6, [0, 1, 33, 300, 64, 700], 515), ([3, 1, 2], [40, 1, 700], 77),
+                                                    ([130, 33, 64], [500, 33, 64], 0), ([200], [1300], 70), ([64] * 3, [64, 90, 200], 10)])
+def test_scores_so_large_that_a_rounding_of_them_is_large(dtype, heads, queries, lengths, prefix):
+    """From 2^31 on a rounding of a score may be 128, and exp2 of that infinite or zero."""
+    c = check.make(len(queries), queries, lengths, heads, 16, prefix, dtype, seed=38)
+    exact = far_scores(c, 39)
+    out, lse = _paged(c)
+    want, want_lse, tol, tol_lse = check.attend(c)
+    n = prefix + max(lengths)
+    sums = (2 * n + 64) * check.F                                   # weights are exactly one and zero: additions, and the output's own rounding
+    tol[exact] = (sums * float(c["v_pages"].float().abs().max()) + check.HALF[dtype] * want.abs() * 1.01)[exact]
+    tol_lse[exact] = (sums + 4 * check.F * want_lse.abs())[exact]
+    check.same(lse, want_lse, tol_lse, "lse")
+    check.same(out, want, tol, "out")
