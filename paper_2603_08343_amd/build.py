@@ -36,6 +36,8 @@ ATTENTION_SRC = os.path.join(HERE, "csrc", "wht_attention.hip")
 ATTENTION_LIB = os.path.join(HERE, "libwht_attention.so")
 ATTENTION_MARSHAL_SRC = os.path.join(HERE, "csrc", "attention_marshal.cpp")
 ATTENTION_MARSHAL_LIB = os.path.join(HERE, "_attention_marshal.so")
+ATTENTION_QUERY_SRC = os.path.join(HERE, "csrc", "attention_query.cpp")         # its rules, for the tests
+ATTENTION_QUERY_LIB = os.path.join(HERE, "libwht_attention_query.so")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -58,7 +60,8 @@ def build(verbose: bool = False, extra=()) -> str:
     _compile(SRC, POISON_LIB, verbose, (*extra, "-DWHT_POISON_LDS"))
     _compile_marshal(MARSHAL_SRC, MARSHAL_LIB, verbose)
     _compile_marshal(ATTENTION_MARSHAL_SRC, ATTENTION_MARSHAL_LIB, verbose)
-    _compile_route(verbose)
+    _compile_rules(ROUTE_SRC, ROUTE_LIB, verbose)
+    _compile_rules(ATTENTION_QUERY_SRC, ATTENTION_QUERY_LIB, verbose)
     _compile(ATTENTION_SRC, ATTENTION_LIB, verbose, extra)
     return _compile(SRC, LIB, verbose, extra)
 
@@ -76,8 +79,8 @@ def _compile_marshal(src: str, lib: str, verbose: bool) -> None:
     subprocess.run(cmd, check=True)
 
 
-def _compile_route(verbose: bool) -> None:
-    cmd = [os.environ.get("CXX", "g++"), "-O1", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra", "-o", ROUTE_LIB, ROUTE_SRC]
+def _compile_rules(src: str, lib: str, verbose: bool) -> None:
+    cmd = [os.environ.get("CXX", "g++"), "-O1", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra", "-o", lib, src]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
@@ -101,7 +104,7 @@ def _compile(src: str, lib: str, verbose: bool, extra=()) -> str:
 def ensure_built(verbose: bool = False) -> str:
     """For harnesses (tests, smoke check, benchmark): compile only if nothing has been built yet.
     The binding itself never builds: a missing library is an error there."""
-    if not all(os.path.exists(lib) for lib in (LIB, COPY_LIB, POISON_LIB, MARSHAL_LIB, ROUTE_LIB, ATTENTION_LIB, ATTENTION_MARSHAL_LIB)):
+    if not all(os.path.exists(lib) for lib in (LIB, COPY_LIB, POISON_LIB, MARSHAL_LIB, ROUTE_LIB, ATTENTION_LIB, ATTENTION_MARSHAL_LIB, ATTENTION_QUERY_LIB)):
         build(verbose=verbose)
     elif any(os.path.getmtime(f) > os.path.getmtime(MARSHAL_LIB) for f in (MARSHAL_SRC, HEADER)):
         raise RuntimeError(f"{MARSHAL_LIB} is older than its source: run `python -m paper_2603_08343_amd.build`")
@@ -110,6 +113,9 @@ def ensure_built(verbose: bool = False) -> str:
         raise RuntimeError(f"{ROUTE_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_MARSHAL_LIB) for f in (ATTENTION_MARSHAL_SRC, ATTENTION_HEADER, HEADER)):
         raise RuntimeError(f"{ATTENTION_MARSHAL_LIB} is older than its source: run `python -m paper_2603_08343_amd.build`")
+    elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_QUERY_LIB)
+             for f in (ATTENTION_QUERY_SRC, os.path.join(HERE, "csrc", "attention_plan.h"), ATTENTION_HEADER, HEADER)):
+        raise RuntimeError(f"{ATTENTION_QUERY_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_LIB) for f in ATTENTION_SOURCES):
         raise RuntimeError(f"{ATTENTION_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > min(os.path.getmtime(LIB), os.path.getmtime(POISON_LIB))

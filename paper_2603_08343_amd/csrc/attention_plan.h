@@ -144,6 +144,9 @@ inline bool streams(int32_t B, int32_t heads, int32_t head_dim, int64_t size, in
     return gang_log2 == 0 && (double)B * max_length * heads * head_dim * 2 * size >= 130e6;
 }
 
+// Waves that share a row's pieces where the few-rows kernel left them: more where few rows have to fill the chip.
+inline int join_waves(int64_t rows) { return rows <= 256 ? 16 : rows <= 2048 ? 4 : 1; }
+
 // Argument checks, in the order of the status codes.
 inline bool good_rows(const wht_attention_rows_t* r, int heads, int head_dim, int size) {
     return ((uintptr_t)r->data & 15u) == 0 && r->token_stride * size % 16 == 0 && r->head_stride * size % 16 == 0 && r->token_stride >= 0 &&

@@ -25,9 +25,6 @@ static void with_flags(F&& f, bool a, bool b, bool c) {
 
 static int launched() { return hipGetLastError() == hipSuccess ? WHT_OK : WHT_ERR_LAUNCH; }
 
-// Rows up to which 16, or 4, waves share a row's pieces: where few rows have to fill the chip.
-constexpr int64_t kJoinRowsWide = 256, kJoinRows = 2048;
-
 // Vector pairs of a token's queries and keys from which on a workgroup takes it, not a wave.  Workgroup / wave, in us: 4 x 64 (32 pairs), 64000 tokens
 // 104 / 50; 16 and 1 x 128 (136), 32000 tokens 66 / 50; 16 and 4 x 64 float32 (160), 67966 tokens 163 / 158; 16 x 128 (256), 8326 tokens 36.5 / 39.6;
 // 32 and 8 x 128 (320), 16000 tokens 73 / 78.
@@ -135,8 +132,8 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     return with_type(dtype, c->head_dim, [&](auto t, auto d) {
         const int64_t rows = T * q_heads;
         if (!p.own_few) hipLaunchKernelGGL((join_splits_kernel<decltype(t), decltype(d)::value>), dim3((unsigned)ceil_div64(rows, 256 / (decltype(d)::value / 4))), dim3(256), 0, stream, j);
-        else if (rows <= kJoinRowsWide) hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 16>), dim3((unsigned)rows), dim3(1024), 0, stream, j);
-        else if (rows <= kJoinRows) hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 4>), dim3((unsigned)rows), dim3(256), 0, stream, j);
+        else if (join_waves(rows) == 16) hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 16>), dim3((unsigned)rows), dim3(1024), 0, stream, j);
+        else if (join_waves(rows) == 4) hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 4>), dim3((unsigned)rows), dim3(256), 0, stream, j);
         else hipLaunchKernelGGL((join_kernel<decltype(t), decltype(d)::value, 1>), grid_of(ceil_div64(rows, 4)), dim3(256), 0, stream, j);
         return launched();
     });

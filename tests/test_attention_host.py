@@ -141,3 +141,13 @@ def test_assembly_that_writes_m0_says_so():
     assert len(statements) == 3
     for s in statements:
         assert '"m0"' in s.rsplit(":", 1)[1], s
+
+
+@pytest.mark.parametrize("source", ["attention_query.cpp", "attention_plan.h", build.ATTENTION_HEADER])
+def test_older_rules_are_refused(source, monkeypatch):
+    source = os.path.join(build.HERE, "csrc", source)
+    real = os.path.getmtime
+    build.ensure_built()
+    monkeypatch.setattr(os.path, "getmtime", lambda f: real(source) - 1.0 if f == build.ATTENTION_QUERY_LIB else real(f))
+    with pytest.raises(RuntimeError, match="older than its source"):
+        build.ensure_built()
