@@ -561,21 +561,27 @@ struct FewRange {
             }
         }
     }
-    template <bool V>
+    template <bool V, bool PAST>
     static __device__ __forceinline__ void issue(const int64_t (&off)[kLoads], const unsigned char* base, unsigned to) {
         const int lane = threadIdx.x & 63;
-        reads_done();
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int r = (i * 64 + lane) / H::kChunks, p = (i * 64 + lane) % H::kChunks;
             const int c = V ? H::v_chunk(r, p) : H::k_chunk(r, p);
             const unsigned char* from = off[i] >= 0 ? base + off[i] + c * 16 : zero_chunk;
-            load_to_lds<STREAM>(from, to + i * 1024);
+            load_to_lds<PAST>(from, to + i * 1024);
         }
+    }
+    // past: they are read once
+    template <bool V>
+    static __device__ __forceinline__ void issue(const int64_t (&off)[kLoads], const unsigned char* base, unsigned to, bool past) {
+        reads_done();
+        if (STREAM && past) issue<V, true>(off, base, to);
+        else issue<V, false>(off, base, to);
     }
 
     // blocks [n0, n1) of `table`'s tokens, of which there are `keys`; limit: how many of them this lane's row sees, all_see: how many every row sees
-    static __device__ __forceinline__ void run(const AttentionArgs& a, const int* table, int n0, int n1, int keys, int limit, int all_see,
+    static __device__ __forceinline__ void run(const AttentionArgs& a, const int* table, int n0, int n1, int keys, int limit, int all_see, bool past,
                                                const unsigned char* kbase, const unsigned char* vbase, unsigned kbuf,
                                                const u32x4 (&q)[H::kSteps], FirstOdd<D>& odd, RowState<H>& st) {
         const int lane = threadIdx.x & 63;
@@ -592,8 +598,8 @@ struct FewRange {
             const bool bad = __any(listed && page < 0);
             int64_t off[kLoads];
             addresses(off, a, page, first, key0, end);
-            issue<false>(off, kbase, kbuf);
-            issue<true>(off, vbase, vbuf);
+            issue<false>(off, kbase, kbuf, past);
+            issue<true>(off, vbase, vbuf, past);
             while (true) {
                 const int next = key0 + kBlockKeys;
                 const bool more = next < end;
@@ -601,7 +607,7 @@ struct FewRange {
                 f32x16 s[1] = {scores<T, D>(kbuf, q)};
                 if (more) {
                     addresses(off, a, page, first, next, end);
-                    issue<false>(off, kbase, kbuf);
+                    issue<false>(off, kbase, kbuf, past);
                 }
                 if (bad || key0 + kBlockKeys > all_see) {
 #pragma unroll
@@ -617,7 +623,7 @@ struct FewRange {
                 accumulate<T, D, MULTI>(vbuf, s[0], limit - key0, all_see < min(key0 + kBlockKeys, keys), odd, st);
                 key0 = next;
                 if (!more) break;
-                issue<true>(off, vbase, vbuf);
+                issue<true>(off, vbase, vbuf, past);
             }
             reads_done();
         }
@@ -642,7 +648,8 @@ struct Shared {
     PageList list;
 };
 
-template <class T, int D, bool MULTI, bool STREAM>
+// FRONT: the prefix is the launch's other workgroups' work.
+template <class T, int D, bool MULTI, bool STREAM, bool FRONT>
 __device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shared<T, D>& shared) {
     using H = Head<T, D>;
     constexpr int kWaveBytes = 2 * 32 * H::kRowBytes;
@@ -701,11 +708,11 @@ __device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shar
         const int limit = min(max(s.length - s.queries + token + 1, 0), s.length), all_see = min(max(s.length - s.queries + 1, 0), s.length);
         const int keys = min(max(s.length - s.queries + min(s.queries, a.max_q), 0), s.length);           // what the last of the rows sees
 #pragma unroll 1
-        for (int part = 0; part < 2; ++part) {                      // the prefix, the sequence
+        for (int part = FRONT ? 1 : 0; part < 2; ++part) {          // the prefix, the sequence
             const int lo = part ? max(n0 - front, 0) : n0, hi = part ? n1 - front : min(n1, front);
             if (lo >= hi) continue;
             FewRange<T, D, MULTI, STREAM>::run(a, part ? a.batch.table + b * a.batch.table_stride : a.prefix_table, lo, hi, part ? keys : a.prefix, part ? limit : a.prefix,
-                                       part ? all_see : a.prefix, kbase, vbase, own, q, first, st);
+                                       part ? all_see : a.prefix, FRONT || part || a.batch.B == 1, kbase, vbase, own, q, first, st);
         }
         st.l += other_half(st.l);
         if (row < rows) {
@@ -1093,8 +1100,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows_kernel
     if constexpr (FRONT) {
         const int block = blockIdx.x;
         if (block < front_blocks) many_rows<T, D, true>(front, block, shared);
-        else few_rows<T, D, MULTI, STREAM>(a, block - front_blocks, shared);
-    } else few_rows<T, D, MULTI, STREAM>(a, blockIdx.x, shared);
+        else few_rows<T, D, MULTI, STREAM, true>(a, block - front_blocks, shared);
+    } else few_rows<T, D, MULTI, STREAM, false>(a, blockIdx.x, shared);
 }
 
 // ------------------------------------------------------------------------------------------------

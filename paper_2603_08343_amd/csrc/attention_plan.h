@@ -136,12 +136,13 @@ inline int gang_log2_of(int32_t heads, int64_t row_bytes, int64_t head_stride_by
     return row_bytes % 128 != 0 && head_stride_bytes == row_bytes && heads % (1 << kGangLog2) == 0 ? kGangLog2 : 0;
 }
 
-// Whether the few-rows kernel reads keys and values past the caches: where a call's own ones are more than half of the 256 MB Infinity Cache, so that
-// little of them would be left there for the next step.  Lengths are on the GPU: it goes by what they can be.  32 x 128 heads, 8 key heads, kept / past, the
-// same cache read again every third call: 65 MB 20.9 / 21.5 us, 98 MB 25.8 / 25.3, 130 MB 33.9 / 30.8, 1 GB 191 / 169; with four heads side by side
-// (lines shared by two loads) 96.8 / 100.3.
-inline bool streams(int32_t B, int32_t heads, int32_t head_dim, int64_t size, int64_t max_length, int32_t gang_log2) {
-    return gang_log2 == 0 && (double)B * max_length * heads * head_dim * 2 * size >= 130e6;
+// Whether the few-rows kernel reads a call's own keys and values past the caches (a prefix that several sequences share is not): where they are more than the share
+// of the 256 MB Infinity Cache that a step of a few layers leaves each of them.  Lengths are on the GPU: it goes by what they can be, and counts a prefix once.  Three caches
+// read in turn, kept / past, us: 1 sequence at 32 and 8 x 128, 80 MB 23.4 / 23.8, 96 MB 26.3 / 26.2, 112 MB 31.3 / 28.6, 256 MB 55.4 / 49.0; 16 of them 21.7 / 22.2,
+// 25.6 / 25.3, 31.2 / 28.1, 55.6 / 48.9; 128 at 16 x 64 23.8 / 23.2, 26.5 / 25.6, 30.3 / 27.9, 55.0 / 49.3; 16 float32 ones at 12 x 64 28.0 / 28.5, 29.3 / 29.3,
+// 33.8 / 32.5, 58.3 / 53.6.  Not with four heads side by side, whose lines are shared by two loads: 200 sequences at 16 x 96 96.8 / 100.3.
+inline bool streams(int32_t B, int32_t heads, int32_t head_dim, int64_t size, int64_t max_length, int64_t prefix, int32_t gang_log2) {
+    return gang_log2 == 0 && ((double)B * max_length + prefix) * heads * head_dim * 2 * size >= 96e6;
 }
 
 // Waves that share a row's pieces where the few-rows kernel left them: more where few rows have to fill the chip.

@@ -14,7 +14,7 @@ void wht_query_attention(int64_t T, int32_t B, int32_t q_heads, int32_t heads, i
     const AttentionPlan p = plan_attention(T, B, q_heads, heads, head_dim, max_q, max_length, prefix);
     const int gang = p.own_few ? gang_log2_of(heads, head_dim * size, head_stride * size) : 0;
     const int64_t values[] = {p.front, p.front_few, p.own_few, p.front_splits, p.own_splits, p.own_cap, p.own_few ? join_waves(T * q_heads) : 0, gang,
-                              p.own_few && streams(B, heads, head_dim, size, most + (p.front ? 0 : prefix), gang)};
+                              p.own_few && streams(B, heads, head_dim, size, most, p.front ? 0 : prefix, gang)};
     for (int64_t v : values) *out++ = v;
 }
 int32_t wht_query_line_share(int32_t total, int32_t rows, int32_t gang_log2) { return line_share(total, rows, gang_log2); }

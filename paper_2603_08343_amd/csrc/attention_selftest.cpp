@@ -218,6 +218,9 @@ int main() {
     walk({0, 0}, 8, 0, 4, kGangLog2);
     walk({1}, 1, 0, 1, 0);
     CHECK(gang_log2_of(16, 192, 192) == kGangLog2 && gang_log2_of(16, 192, 64 * 192) == 0 && gang_log2_of(6, 192, 192) == 0 && gang_log2_of(16, 256, 256) == 0);
+    // 400 sequences of 10 tokens behind 100, 8 heads of 128: 16.8 MB, though every sequence reads the prefix's 0.4 MB; of 100 tokens 164 MB
+    CHECK(!streams(400, 8, 128, 2, 10, 100, 0) && streams(400, 8, 128, 2, 100, 100, 0) && !streams(400, 8, 128, 2, 100, 100, kGangLog2));
+    CHECK(streams(1, 8, 128, 2, 0, 1 << 20, 0));
     plans();
     statuses();
     printf("attention_selftest: ok\n");

@@ -101,7 +101,7 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     a.use_prefix = !p.front && prefix > 0;
     a.front_item = p.front && p.front_few;
     a.gang_log2 = gang_log2_of(c->heads, c->head_dim * size, a.head_stride);
-    const bool stream_keys = streams(b->B, c->heads, c->head_dim, size, a.batch.most + (a.use_prefix ? prefix : 0), a.gang_log2);
+    const bool stream_keys = streams(b->B, c->heads, c->head_dim, size, a.batch.most, a.use_prefix ? prefix : 0, a.gang_log2);
     a.splits = p.own_splits; a.rows_cap = p.own_cap;
     a.part = reinterpret_cast<float*>(ws + p.own_at); a.sums = reinterpret_cast<float*>(ws + p.own_sums_at);
     a.cum = reinterpret_cast<int*>(ws + p.cum_at);
