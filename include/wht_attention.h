@@ -43,7 +43,7 @@
  * Conventions for both entry points: device pointers; `stream` is a hipStream_t (NULL: the default stream); nothing is allocated or
  * synchronised; the arguments are validated before anything is enqueued; both may be captured into a HIP graph, which then replays
  * with the arrays' new values.  Results are bit-reproducible.  Outputs may not overlap inputs, except that the append's
- * q_out may be q itself.
+ * q_out may be q itself; nor themselves (strides that let them are refused, those of a cache that is appended to as well).
  */
 #ifndef WHT_ATTENTION_H
 #define WHT_ATTENTION_H

@@ -4,6 +4,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "../../include/wht_attention.h"
 
 #if defined(__HIPCC__)
@@ -154,6 +156,22 @@ inline bool good_rows(const wht_attention_rows_t* r, int heads, int head_dim, in
            (r->head_stride >= head_dim || heads == 1) && r->head_stride >= 0 && r->head_stride * size < (int64_t)1 << 31;
 }
 
+// What is written has a place of its own for every vector: of its dimensions, from the shortest stride on, each passes all of those before.
+struct Dimension { int64_t count, stride; };
+inline bool apart(Dimension a, Dimension b, Dimension c, int head_dim) {
+    auto swap_longer = [](Dimension& x, Dimension& y) { if (x.count > 1 && (y.count <= 1 || x.stride > y.stride)) { const Dimension t = x; x = y; y = t; } };
+    swap_longer(a, b);
+    swap_longer(b, c);
+    swap_longer(a, b);
+    double extent = head_dim;                                       // the products may pass 64 bits
+    for (const Dimension& d : {a, b, c}) {
+        if (d.count <= 1) continue;
+        if ((double)d.stride < extent) return false;
+        extent += (double)(d.count - 1) * (double)d.stride;
+    }
+    return true;
+}
+
 inline int check_cache(const wht_attention_cache_t* c, const wht_attention_batch_t* b, int32_t dtype) {
     if (!c || !b || !c->k || !c->v || !b->table || !b->lengths) return WHT_ERR_NULL_PTR;
     if (dtype != WHT_DTYPE_F32 && dtype != WHT_DTYPE_BF16) return WHT_ERR_BAD_DTYPE;
@@ -183,6 +201,8 @@ inline int check_append(const wht_attention_rows_t* q, const wht_attention_rows_
     if (position < 0 || position > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
     if (!good_rows(k, c->heads, c->head_dim, size) || !good_rows(v, c->heads, c->head_dim, size) || ((uintptr_t)rope & 15u) != 0) return WHT_ERR_MISALIGNED;
     if (q->data && (!good_rows(q, q_heads, c->head_dim, size) || !good_rows(q_out, q_heads, c->head_dim, size))) return WHT_ERR_MISALIGNED;
+    if (q->data && !apart({T, q_out->token_stride}, {q_heads, q_out->head_stride}, {1, 0}, c->head_dim)) return WHT_ERR_MISALIGNED;
+    if (!apart({c->pages, c->page_stride}, {c->heads, c->head_stride}, {c->page_size, c->token_stride}, c->head_dim)) return WHT_ERR_MISALIGNED;
     return WHT_OK;
 }
 
@@ -214,6 +234,7 @@ inline int check_paged(const wht_attention_rows_t* q, const wht_attention_rows_t
     if (((int64_t)b->B + 1) * (own / kBlockKeys + prefix / kBlockKeys + 2) > INT32_MAX / c->heads) return WHT_ERR_BAD_DIM;
     const int size = dtype == WHT_DTYPE_F32 ? 4 : 2;
     if (!good_rows(q, q_heads, c->head_dim, size) || !good_rows(out, q_heads, c->head_dim, size)) return WHT_ERR_MISALIGNED;
+    if (!apart({T, out->token_stride}, {q_heads, out->head_stride}, {1, 0}, c->head_dim)) return WHT_ERR_MISALIGNED;
     if (((uintptr_t)lse & 3u) != 0 || ((uintptr_t)prefix_table & 3u) != 0) return WHT_ERR_MISALIGNED;
     return WHT_OK;
 }

@@ -191,6 +191,26 @@ static void statuses() {
         CHECK(check_paged(&r0, &r0, nullptr, 3, 32, &c, &b, nullptr, 0, 1, (int64_t)1 << 20, 1.0f, 1) == WHT_ERR_BAD_DIM);
         CHECK(check_paged(&r0, &r0, nullptr, 3, 32, &c, &b, nullptr, 0, 1, 1 << 12, 1.0f, 1) == WHT_OK);
     }
+    // outputs over themselves: rows or heads at one place, one inside the other's
+    auto written = [&](int64_t T, int64_t token_stride, int64_t head_stride) {
+        const wht_attention_rows_t o{P, token_stride, head_stride};
+        return check_paged(&r0, &o, nullptr, T, 32, &c0, &b0, nullptr, 0, 1, 256, 1.0f, 1);
+    };
+    CHECK(written(3, 48 * 128, 128) == WHT_OK && written(3, 128, 3 * 128) == WHT_OK && written(3, 32 * 128, 128) == WHT_OK && written(1, 0, 128) == WHT_OK);
+    CHECK(written(3, 0, 128) == WHT_ERR_MISALIGNED && written(3, 128, 128) == WHT_ERR_MISALIGNED && written(3, 31 * 128, 128) == WHT_ERR_MISALIGNED);
+    CHECK(written(3, 128, 2 * 128) == WHT_ERR_MISALIGNED && written(3, 64, 3 * 128) == WHT_ERR_MISALIGNED);
+    {
+        const wht_attention_rows_t o{P, 0, 128};
+        CHECK(check_append(&r0, &r0, &r0, &o, 3, 32, &c0, &b0, F, 100, 128, 0, 1) == WHT_ERR_MISALIGNED);
+        CHECK(check_append(&none, &r0, &r0, &o, 3, 32, &c0, &b0, F, 100, 128, 0, 1) == WHT_OK);
+    }
+    CHECK(cache([](auto& c) { c.page_stride = 0; }) == WHT_ERR_MISALIGNED);
+    CHECK(cache([](auto& c) { c.page_stride = 0; c.pages = 1; }) == WHT_OK);
+    CHECK(cache([](auto& c) { c.head_stride = 0; }) == WHT_ERR_MISALIGNED);
+    CHECK(cache([](auto& c) { c.page_stride -= 128; }) == WHT_ERR_MISALIGNED);
+    CHECK(cache([](auto& c) { c.token_stride = 8 * 128; c.head_stride = 128; }) == WHT_OK);                                     // [pages][slots][heads]
+    CHECK(cache([](auto& c) { c.page_stride = 64 * 128; c.head_stride = 10 * 64 * 128; }) == WHT_OK);                            // [heads][pages][slots]
+    CHECK(cache([](auto& c) { c.page_stride = 64 * 128; c.head_stride = (int64_t)1 << 61; }) == WHT_OK);
     // a scale whose product with log2(e) is infinite would make NaN of every score of zero
     for (float s : {1e-45f, 1e-38f, 1.0f, 1e38f, 2.3e38f}) CHECK(paged(r0, 32, I, 100, 1, 256, s, 1) == WHT_OK && base2_scale(s) > 0.0f && base2_scale(s) < __builtin_inff());
     for (float s : {2.4e38f, 3.0e38f, 3.4e38f}) CHECK(paged(r0, 32, I, 100, 1, 256, s, 1) == WHT_ERR_BAD_DIM);

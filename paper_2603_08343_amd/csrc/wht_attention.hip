@@ -180,7 +180,7 @@ const char* wht_attention_status_string(int status) {
     case WHT_ERR_NULL_PTR:   return "a required pointer is NULL";
     case WHT_ERR_BAD_DIM:    return "a size is not taken: head_dim 64, 96 or 128; page_size a power of two, 8 to 1024; q_heads a multiple of heads, at most 1024; rotary a multiple of 16 up to head_dim; counts not negative and below 2^30; a page below 4 GiB; scale > 0 and at most 2.3e38";
     case WHT_ERR_BAD_DTYPE:  return "dtype must be WHT_DTYPE_F32 or WHT_DTYPE_BF16";
-    case WHT_ERR_MISALIGNED: return "tensors must be 16-byte aligned and their strides 16-byte steps of at least a row (heads: below 2 GiB)";
+    case WHT_ERR_MISALIGNED: return "tensors must be 16-byte aligned and their strides 16-byte steps of at least a row (heads: below 2 GiB); what is written must not overlap itself";
     case WHT_ERR_WORKSPACE:  return "workspace is NULL or smaller than wht_attention_workspace_bytes";
     case WHT_ERR_LAUNCH:     return "the HIP runtime refused a kernel launch";
     default:                 return "unknown status";

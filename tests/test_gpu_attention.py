@@ -613,3 +613,18 @@ def test_scores_so_large_that_a_rounding_of_them_is_large(dtype, heads, queries,
     tol_lse[exact] = (sums + 4 * check.F * want_lse.abs())[exact]
     check.same(lse, want_lse, tol_lse, "lse")
     check.same(out, want, tol, "out")
+
+
+def test_outputs_over_themselves_are_refused():
+    wht = _wht()
+    c = check.make(2, [1, 1], [20, 30], (4, 2, 64), 16, 10, seed=40)
+    for over in (torch.empty(1, 4, 64, dtype=BF16, device="cuda:0").expand(2, 4, 64), torch.empty(2, 1, 64, dtype=BF16, device="cuda:0").expand(2, 4, 64)):
+        with pytest.raises(wht.WhtAttentionError, match="overlap itself"):
+            _paged(c, out=over)
+        with pytest.raises(wht.WhtAttentionError, match="overlap itself"):
+            wht.wht_attention_append(c["q"], c["k"], c["v"], c["k_pages"], c["v_pages"], c["table"], c["lengths"], None, q_out=over)
+    n = c["k_pages"].shape[0]
+    shared = [c[t][:1].expand(n, -1, -1, -1) for t in ("k_pages", "v_pages")]
+    with pytest.raises(wht.WhtAttentionError, match="overlap itself"):
+        wht.wht_attention_append(None, c["k"], c["v"], *shared, c["table"], c["lengths"], None)
+    _paged({**c, "k_pages": shared[0], "v_pages": shared[1]})        # reading them is as good as ever
