@@ -94,6 +94,8 @@ def wht_attention_workspace_bytes(T, B, q_heads, heads, head_dim, max_q, max_len
 def wht_attention_rope_table(positions, rotary, base=10000.0, device="cuda"):
     """[positions, rotary / 2, 2] float32: cos and sin of position * base^(-2 i / rotary), from angles in 64 bits."""
     import torch
+    if rotary < 0 or rotary % 2 != 0:
+        raise ValueError(f"rotary must be even and not negative, got {rotary}")
     rates = base ** (-torch.arange(0, rotary, 2, dtype=torch.float64, device=device) / rotary)
     angles = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * rates
     return torch.stack((angles.cos(), angles.sin()), dim=2).float()

@@ -151,3 +151,11 @@ def test_older_rules_are_refused(source, monkeypatch):
     monkeypatch.setattr(os.path, "getmtime", lambda f: real(source) - 1.0 if f == build.ATTENTION_QUERY_LIB else real(f))
     with pytest.raises(RuntimeError, match="older than its source"):
         build.ensure_built()
+
+
+def test_rope_table_of_an_odd_width_is_refused():
+    """Its last pair would have one element, and the call would take it for a table one wider."""
+    for rotary in (15, 63, -2):
+        with pytest.raises(ValueError, match="rotary must be even"):
+            wht.wht_attention_rope_table(10, rotary, device="cpu")
+    assert wht.wht_attention_rope_table(10, 0, device="cpu").shape == (10, 0, 2)
