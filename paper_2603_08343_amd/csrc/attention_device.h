@@ -975,10 +975,9 @@ __device__ __forceinline__ void store4(unsigned char* p, f32x4 x) {
     }
 }
 
-// Rows that no tile covers: padding (zeros) and tokens from the max_q-th of their sequence on (NaN).
-constexpr int kFillGroups = 8;
+// Rows that no tile covers: padding (zeros) and tokens from the max_q-th of their sequence on (NaN).  A workgroup of each die takes a share.
 template <class T, int D>
-__device__ __forceinline__ void fill_rows(const AttentionArgs& a, int group) {
+__device__ __forceinline__ void fill_rows(const AttentionArgs& a, int die) {
     auto fill = [&](int lo, int hi, float value, float lse) {
         const int64_t n = (int64_t)(hi - lo) * a.q_heads * (D / 4);
         for (int64_t i = threadIdx.x; i < n; i += 256) {
@@ -988,13 +987,13 @@ __device__ __forceinline__ void fill_rows(const AttentionArgs& a, int group) {
             if (a.lse && i % (D / 4) == 0) a.lse[t * a.q_heads + h] = lse;
         }
     };
-    for (int b = group; b < a.batch.B; b += kFillGroups) {
+    for (int b = die; b < a.batch.B; b += kDies) {
         const Sequence s = sequence(a.batch, b);
         if (s.queries > a.max_q) fill(s.first + a.max_q, s.first + s.queries, __builtin_nanf(""), __builtin_nanf(""));
     }
     const int last = min(max(a.batch.q_starts ? a.batch.q_starts[a.batch.B] : a.batch.B, 0), a.batch.T);
     const int left = a.batch.T - last;
-    fill(last + (int)((int64_t)left * group / kFillGroups), last + (int)((int64_t)left * (group + 1) / kFillGroups), 0.0f, WHT_NEG_INF);
+    fill(last + (int)((int64_t)left * die / kDies), last + (int)((int64_t)left * (die + 1) / kDies), 0.0f, WHT_NEG_INF);
 }
 
 // STACKED: the rows of all sequences, against the prefix alone.
@@ -1006,7 +1005,7 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
     auto& list = shared.list;
     auto& odd = shared.odd;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int x = block & 7, y = block >> 3, groups = a.heads * a.splits;
+    const int x = block % kDies, y = block / kDies, groups = a.heads * a.splits;
     auto tiles_of = [&](int queries) { return (int)(((int64_t)queries * a.G + kTileRows - 1) / kTileRows); };
     int b = 0, cum = 0;
     Sequence s{0, a.batch.T, 0};

@@ -66,16 +66,17 @@ inline int64_t most_tiles(int64_t T, int64_t B, int64_t G, int64_t max_q) {
 // dies, the tiles of a group one after the other, so that its keys are in one L2 once.  A workgroup looks its tile up, so that sequences of few new tokens among longer ones launch no tiles without rows:
 // one prompt of 2000 tokens and 63 of one, each with 500 before, 32 and 8 heads of 128, 133 -> 87 us; 512 among 199 of one 275 -> 97; where all are alike
 // the look-up adds 0.5 us.  Of sequence b's groups those of die x: how many, and the k-th.
-WHT_HD int die_groups(int b, int per, int x) { return ((b + 1) * per - x + 7) / 8 - (b * per - x + 7) / 8; }
-WHT_HD int die_group(int b, int per, int x, int k) { return ((x - b * per) & 7) + 8 * k; }
+constexpr int kDies = 8;
+WHT_HD int die_groups(int b, int per, int x) { return ((b + 1) * per - x + kDies - 1) / kDies - (b * per - x + kDies - 1) / kDies; }
+WHT_HD int die_group(int b, int per, int x, int k) { return ((x - b * per) & (kDies - 1)) + kDies * k; }
 // The line of a die's tiles, counted up to more than a grid has, so that the sum of any numbers that q_starts may hold fits 32 bits (64 lanes' sums too): one
 // sequence has 2^23 rows of tiles at most.
 constexpr int kMostTiles = 1 << 24;
-static_assert(kMostTiles > kMostWorkgroups / 8, "counts are cut off where no workgroup looks");
+static_assert(kMostTiles > kMostWorkgroups / kDies, "counts are cut off where no workgroup looks");
 WHT_HD int add_tiles(int sum, int tiles) { return sum + tiles < kMostTiles ? sum + tiles : kMostTiles; }
 // Workgroups that a die needs at most.
 inline int64_t die_blocks(int64_t T, int64_t B, int64_t G, int64_t max_q, int64_t per) {
-    const int64_t packed = ceil_div64(per, 8) * (T * G / kTileRows + B), each = ceil_div64(B * per, 8) * ceil_div64((max_q < T ? max_q : T) * G, kTileRows);
+    const int64_t packed = ceil_div64(per, kDies) * (T * G / kTileRows + B), each = ceil_div64(B * per, kDies) * ceil_div64((max_q < T ? max_q : T) * G, kTileRows);
     return packed < each ? packed : each;
 }
 

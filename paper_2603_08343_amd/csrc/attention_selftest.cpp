@@ -60,14 +60,14 @@ static void deal(const std::vector<int>& queries, int heads, int splits, int G) 
     for (int q : queries) { T += q; max_q = q > max_q ? q : max_q; }
     const int64_t most = die_blocks(T, B, G, max_q, per);
     std::set<std::pair<int, int>> seen;
-    for (int x = 0; x < 8; ++x) {
+    for (int x = 0; x < kDies; ++x) {
         int64_t blocks = 0;
         for (int b = 0; b < B; ++b) {
             const int n = die_groups(b, per, x);
             CHECK(n >= 0);
             for (int k = 0; k < n; ++k) {
                 const int g = die_group(b, per, x, k);
-                CHECK(g >= 0 && g < per && (b * per + g) % 8 == x && seen.insert({b, g}).second);
+                CHECK(g >= 0 && g < per && (b * per + g) % kDies == x && seen.insert({b, g}).second);
                 blocks += ceil_div64((int64_t)queries[b] * G, kTileRows);
             }
         }
@@ -84,7 +84,7 @@ static void deal_to_overlapping(int B, int64_t T, int heads, int G) {
     const int splits = splits_for(most_tiles(T, B, G, T) * heads, 1 << 20), per = heads * splits, run = ceil_div(B, 64);
     auto tiles_at = [&](int i, int x) { return die_groups(i, per, x) * (i % 2 ? 0 : (int)ceil_div64(T * G, kTileRows)); };
     const int64_t most = die_blocks(T, B, G, T, per);
-    CHECK(most <= kMostWorkgroups / 8);
+    CHECK(most <= kMostWorkgroups / kDies);
     for (int x = 0; x < 8; x += 7) {
         int upto[64], last = 0;
         for (int lane = 0; lane < 64; ++lane) {

@@ -96,7 +96,7 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     if (p.front && !p.front_few) {
         f.use_prefix = 1; f.splits = p.front_splits;
         f.part = reinterpret_cast<float*>(ws + p.front_at); f.sums = reinterpret_cast<float*>(ws + p.front_sums_at);
-        front_blocks = 8 * die_blocks(T, 1, a.G, T, (int64_t)c->heads * f.splits);
+        front_blocks = kDies * die_blocks(T, 1, a.G, T, (int64_t)c->heads * f.splits);
     }
     a.use_prefix = !p.front && prefix > 0;
     a.front_item = p.front && p.front_few;
@@ -105,7 +105,7 @@ static int paged(const wht_attention_rows_t* q, const wht_attention_rows_t* out,
     a.splits = p.own_splits; a.rows_cap = p.own_cap;
     a.part = reinterpret_cast<float*>(ws + p.own_at); a.sums = reinterpret_cast<float*>(ws + p.own_sums_at);
     a.cum = reinterpret_cast<int*>(ws + p.cum_at);
-    const int64_t each = die_blocks(T, b->B, a.G, max_q, (int64_t)c->heads * a.splits), own_blocks = p.own_few ? kWorkgroups : (each + 1) * 8;
+    const int64_t each = die_blocks(T, b->B, a.G, max_q, (int64_t)c->heads * a.splits), own_blocks = p.own_few ? kWorkgroups : (each + 1) * kDies;
     if (front_blocks + own_blocks > kMostWorkgroups) return WHT_ERR_BAD_DIM;
     a.fill = (int)each;
     const int rc = with_type(dtype, c->head_dim, [&](auto t, auto d) {
