@@ -351,7 +351,8 @@ __device__ __forceinline__ int key_of(int i) { return (i >> 2) * 8 + ((threadIdx
 // many rows, where the vector units' time counts, that is 8: one of a wave's 32 rows has a new maximum in most steps, and each
 // one multiplies all the sums over.  Weights are up to 256 then, which float32 sums hold as exactly; but the largest of a row is no longer
 // 1, which bfloat16 holds exactly: the error of the outputs, with that of their own rounding, goes from 1.9e-3 to 2.3e-3 of their norm.
-// With few rows, bound by memory, it is 0.
+// Float32 products hold a weight of 256 as exactly as one of 1 (two prompts of 4096 at 32 and 8 x 128: 1.07e-6; with the base at the maximum itself, in elementary
+// operations, 1.04e-6).  With few rows, bound by memory, it is 0.
 //
 // A weight is exp2(s scale - base), one rounding, with base = top scale rounded: what that rounding is off by is a factor that all weights share, but for those that bfloat16
 // rounds and their sum, which is not rounded.  Of a maximum of 2^31 it may be 2^128 or 2^-128, and the weights infinite or zero.  From kFar on, where the factor may be 1 + 2e-5,
@@ -534,7 +535,7 @@ __device__ __forceinline__ void load_row(const unsigned char* p, bool there, u32
 // waves share evenly, whatever the sequences' lengths: a wave's share begins and ends anywhere in an item.  Every piece of an item leaves a
 // slot of partial results, numbered item + worker (each step along the line raises one of the two), which join_kernel puts together.
 // Gang: where a token's rows of neighbouring heads share 128-byte lines, the four waves of a workgroup are one worker that takes four heads' rows, whole lines
-// together, at the same time (200 sequences at 16 x 96, rows of 192 bytes one after the other: 525 MB fetched without it, of 406 MB that there are).
+// together, at the same time (200 sequences at 16 x 96, rows of 192 bytes one after the other: 537 MB fetched without it, 416 with it, of 406 that there are).
 
 template <class T, int D, bool MULTI, bool STREAM>
 struct FewRange {
@@ -733,7 +734,7 @@ __device__ __forceinline__ void few_rows(const AttentionArgs& a, int block, Shar
 // next steps' in flight.  A wave takes 32 keys at a time, as a pipeline: the products with the next 32 keys stand beside the exponentials of
 // these, those with their values beside the next ones' maximum, and every fragment is read from LDS as many products ahead as there are in one of the two,
 // into the registers of the one just used.  Per 32 keys 128 wide: 16 matrix instructions of 32 cycles, 60 vector instructions of 4 and 16 exponentials of 16.
-// Two prompts of 4096 tokens, 32 and 8 heads of 128: 297 us, 927 TFLOP/s (a library product of 8192 x 8192 x 8192 here: 1215).  What bounds it is no one
+// Two prompts of 4096 tokens, 32 and 8 heads of 128: 300 us, 916 TFLOP/s (a library product of 8192 x 8192 x 8192 here: 1215).  What bounds it is no one
 // of its parts: 8 x 128 tokens behind 16256 keys, 32 heads, take 327 us; without the loads into LDS 258, without the reads from it 237, without either
 // 185, without the products 209, without the exponentials 294.  A second workgroup on a compute unit gains 8 %.
 
@@ -1085,7 +1086,7 @@ __device__ __forceinline__ void many_rows(const AttentionArgs& a, int block, Sha
 
 // ------------------------------------------------------------------------------------------------
 // The kernels.  Where rows of all sequences meet the prefix (compute-bound) and each sequence's few rows its own keys (memory-bound), one launch does
-// both, so that a compute unit holds a workgroup of each.
+// both, so that a compute unit may hold a workgroup of each (where the first kind's leave room: AttentionPlan).
 
 template <class T, int D>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void many_rows_kernel(AttentionArgs a) {

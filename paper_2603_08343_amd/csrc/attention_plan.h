@@ -25,7 +25,7 @@ constexpr int kFewRows = 32;        // few-rows kernel: one tile of rows, every 
 constexpr int kTileRows = 128;      // many-rows kernel: 32 rows per wave, all waves take the same keys
 constexpr int kBlockKeys = 32;      // keys of one step of a wave in the few-rows kernel
 constexpr int kStepKeys = 64;       // keys of one step of a workgroup in the many-rows kernel
-constexpr int kWorkgroups = 512;    // two per compute unit
+constexpr int kWorkgroups = 512;    // two per compute unit; of float32 heads 96 and 128 wide, which take more than half of its LDS (103 and 137 KB), it holds one at a time
 constexpr int kWorkers = 4 * kWorkgroups;       // waves of the few-rows kernel's grid
 
 // A launch has below 2^32 threads along x.  Kernels that take a token or row each have this many workgroups there, and as many rows of them as it takes.
@@ -34,7 +34,9 @@ constexpr int64_t kMostWorkgroups = ((int64_t)1 << 32) / 256 - 1;       // of 25
 
 // What one call launches.  `front`: the rows of all sequences against the prefix; `own`: each sequence's rows against its own
 // keys -- or, where there is no front, against prefix and own keys as one range.  A front of few rows is one more sequence on the
-// few-rows kernel's line; one of many rows shares the launch with it, with a workgroup for every compute unit.
+// few-rows kernel's line; one of many rows shares the launch with it.  Its workgroups come first in the grid: where they are one a compute unit or fewer, the line
+// runs beside them; where splits_for makes them two (4 shares of 128 tiles and the like), they fill every place and the line begins as they end.  256 sequences at
+// 64 and 8 x 128 behind 32768 tokens, two / one a compute unit: with 1024 to 2048 tokens of their own 529 / 474 us, with 32 to 64 293 / 343.
 struct AttentionPlan {
     bool front, front_few, own_few;
     int front_splits, own_splits;           // many-rows kernel: workgroups that share a tile's keys
@@ -44,9 +46,12 @@ struct AttentionPlan {
     size_t front_at, own_at, front_sums_at, own_sums_at, cum_at, bytes;     // byte offsets in the workspace
 };
 
-// Workgroups that share a tile's keys, 256 keys each at least: so that every compute unit has one.  A second one there is worth 8 % (8 sequences of 128 new
+// Workgroups that share a tile's keys: so that every compute unit has one, and at most one for every 256 keys begun (a tile's own keys are cut evenly in steps of 64,
+// so that shares may be shorter: 257 keys of 8 tiles 192 and 65).  A second one there is worth 8 % (8 sequences of 128 new
 // tokens behind 16256, 32 heads of 128: 351 us with one, 325 with two), less than partial results of short ranges cost (1000 new tokens at
-// 32 x 128: 29 and 45 us), so that tiles are split for it where the shares are long.
+// 32 x 128: 29 and 45 us), so that tiles are split for it where the shares are long.  It goes by the longest that lengths can be, and is blind to the type, though a step
+// costs float32 16 times the matrix cycles.  With a table 32 times as wide as the sequences are long: 1000 new tokens at 32 x 128 30.3 -> 38.0 us, 4 x 200 at 16 x 64
+// 12.1 -> 16.0, two of 4096 at 32 and 8 x 128 296 -> 290.
 inline int splits_for(int64_t tiles, int64_t keys) {
     if (tiles <= 0) return 1;
     int64_t s = kWorkgroups / tiles;
@@ -88,7 +93,8 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
     // Several sequences of few rows each: their rows together read the prefix once.  Where a sequence's own rows fill tiles by themselves nothing is saved
     // by that, and prefix and own keys are one range; as where the prefix, read by every sequence, is two blocks for each worker or fewer:
     // apart / as one range, in us: 15 sequences behind 1 token, 16 heads of 128, 28.4 / 11.9; 8 behind 2048, 8 key heads, 22.1 / 20.1;
-    // 32 behind 1024 (four blocks) 18.2 / 29.2; 200 behind 64, 16 of 64 (three) 60.5 / 50.8.
+    // 32 behind 1024 (four blocks) 18.2 / 29.2.  Counting the prefix's blocks alone, it is wrong where the own keys are many and the prefix short beside them:
+    // 200 behind 64, 16 of 64 (three blocks) 60.5 / 50.8, which are taken apart.
     p.front = prefix > 0 && B > 1 && p.own_few && (int64_t)B * heads * ceil_div64(prefix, kBlockKeys) > 2 * kWorkers;
     p.front_few = T * G <= kFewRows;
     p.front_splits = p.own_splits = 1;
@@ -119,7 +125,8 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
 // The few-rows kernel's line: the blocks of all items one after the other, an equal share of them to a worker (a wave).  The pieces of an item
 // of n blocks from u0 on lie in the slots item + w of the workers w that it meets: first .. first + count - 1.  A piece writes `rows`
 // rows of results, 4 bytes an element, for the keys and values it reads: where there is more than a block for every worker, a share is a
-// block for every eight rows at least (8 sequences of 8 new tokens and 1500 of their own, 32 and 8 heads: 23.6 us; for sixteen: 25.4).
+// block for every eight rows at least.  For every four / eight / sixteen rows, in us, 32 and 8 x 128: 8 sequences of 8 new tokens and 750 to 1500 of their own
+// 28.3 / 23.6 / 24.9, 4 of 8 and 2000 to 4000 27.0 / 23.8 / 26.8, 32 of 8 and 750 to 1500 52.4 / 50.0 / 49.9, 8 of 4 and 750 to 1500 19.8 / 20.3 / 20.3.
 // With a gang of heads a worker is a workgroup, an item a group of heads, and every slot holds one piece for each of them.
 struct Slots { int64_t first; int count; };
 constexpr int kWorkersLog2 = 11;
@@ -148,7 +155,10 @@ inline bool streams(int32_t B, int32_t heads, int32_t head_dim, int64_t size, in
     return gang_log2 == 0 && ((double)B * max_length + prefix) * heads * head_dim * 2 * size >= 96e6;
 }
 
-// Waves that share a row's pieces where the few-rows kernel left them: more where few rows have to fill the chip.
+// Waves that share a row's pieces where the few-rows kernel left them: more where few rows have to fill the chip.  Both kernels with 16 / 4 / 1 of them, in us, 128 wide:
+// 32 rows of 256 pieces 30.6 / 32.3 / 45.7, 16 of 1000 22.0 / 33.5 / 91.3, 256 of 256 24.4 / 24.6 / 30.5, but of 32 pieces 19.0 / 18.3 / 18.9 and 32 of 4 10.3 / 10.1 / 9.7;
+// 512 of 64 25.2 / 23.9 / 26.1, 1024 of 64 31.3 / 26.1 / 26.7, but of 8 47.0 / 42.1 / 41.6; 2048 of 4 83.6 / 74.9 / 72.4; 3072 of 3 121.9 / 109.2 / 104.9.  How many
+// pieces a row has is not asked for, which costs up to 1.3 us where they are few and up to a tenth between 1024 and 2048 rows.
 inline int join_waves(int64_t rows) { return rows <= 256 ? 16 : rows <= 2048 ? 4 : 1; }
 
 // Argument checks, in the order of the status codes.
