@@ -157,7 +157,7 @@ inline bool streams(int32_t B, int32_t heads, int32_t head_dim, int64_t size, in
 
 // Waves that share a row's pieces where the few-rows kernel left them: more where few rows have to fill the chip.  Both kernels with 16 / 4 / 1 of them, in us, 128 wide:
 // 32 rows of 256 pieces 30.6 / 32.3 / 45.7, 16 of 1000 22.0 / 33.5 / 91.3, 256 of 256 24.4 / 24.6 / 30.5, but of 32 pieces 19.0 / 18.3 / 18.9 and 32 of 4 10.3 / 10.1 / 9.7;
-// 512 of 64 25.2 / 23.9 / 26.1, 1024 of 64 31.3 / 26.1 / 26.7, but of 8 47.0 / 42.1 / 41.6; 2048 of 4 83.6 / 74.9 / 72.4; 3072 of 3 121.9 / 109.2 / 104.9.  How many
+// 512 of 64 25.2 / 23.9 / 26.1, 1024 of 64 31.3 / 26.1 / 26.7, but of 8 47.0 / 42.1 / 41.6; 2048 of 4 83.6 / 74.9 / 72.4; 4096 of 2 157.2 / 140.1 / 134.3.  How many
 // pieces a row has is not asked for, which costs up to 1.3 us where they are few and up to a tenth between 1024 and 2048 rows.
 inline int join_waves(int64_t rows) { return rows <= 256 ? 16 : rows <= 2048 ? 4 : 1; }
 
