@@ -9,7 +9,7 @@ the layer the orthogonal transform itself at initialisation.
 """
 import torch
 
-from . import binding
+from . import attention4, binding, rotary
 
 
 class WhtAffineFunction(torch.autograd.Function):
@@ -75,3 +75,49 @@ class WhtAffine(torch.nn.Module):
 
     def extra_repr(self):
         return f"d={self.d}"
+
+
+class WhtRotaryFunction(torch.autograd.Function):
+    """Heads turned by positions of several axes; the gradient is turned back by the same angles."""
+
+    @staticmethod
+    def forward(ctx, x, rope, positions, axes, interleaved, inverse):
+        y = rotary.wht_rotary_rotate(_heads(x), rope, positions, axes, interleaved, inverse)
+        ctx.save_for_backward(rope, positions)              # their versions are checked: angles that have changed since raise
+        ctx.how = axes, interleaved, not inverse
+        return y.view(x.shape)
+
+    @staticmethod
+    def backward(ctx, dy):
+        return WhtRotaryFunction.apply(dy, *ctx.saved_tensors, *ctx.how), None, None, None, None, None
+
+
+def _heads(x):
+    """x [..., heads, head_dim] as [T, heads, head_dim] with steps of 16 bytes: a copy where its strides or its place are others."""
+    x = x.reshape(-1, *x.shape[-2:])
+    step = 16 // x.element_size()
+    plain = x.stride(2) == 1 and x.stride(1) % step == 0 and x.stride(0) % step == 0 and x.stride(1) >= x.shape[2] and x.data_ptr() % 16 == 0
+    return x if plain else x.clone(memory_format=torch.contiguous_format)
+
+
+def wht_rotary(x, rope, positions=None, axes=None, interleaved=False):
+    """Differentiable rotary.wht_rotary_rotate; x: [..., heads, head_dim] bfloat16|float32 on the GPU, positions int32 [...] or [..., axes].
+    Neither the table nor the positions have a gradient.  Plain calls go to the extension module's node of torch's C++ autograd
+    (csrc/attention_marshal.cpp), the others, and everything under a compiler's trace, to WhtRotaryFunction.
+
+    A capture into a graph is refused for a leaf whose gradient a living graph from outside the capture gathers: the backward pass would wait for that
+    graph's stream, which is not captured, and torch ends the process over it."""
+    if positions is not None and x.dim() != 3:
+        lead = positions.shape[:x.dim() - 2]
+        if lead != x.shape[:-2]:
+            raise ValueError(f"positions must be those of the tokens, {list(x.shape[:-2])}, got {list(positions.shape)}")
+        positions = positions.reshape(-1, *positions.shape[x.dim() - 2:]).contiguous()
+    if not torch.compiler.is_compiling():
+        native = attention4._native()
+        if torch.cuda.is_current_stream_capturing() and native.leaf_elsewhere(x):
+            raise RuntimeError("x is a leaf whose gradient a graph from outside the capture gathers on another stream: let go of that graph first "
+                               "(its outputs and losses), or capture with a detached x")
+        y = native.rotary(x, rope, positions, axes, interleaved)
+        if y is not None:
+            return y
+    return WhtRotaryFunction.apply(x, rope, positions, axes, interleaved, False)

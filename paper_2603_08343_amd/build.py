@@ -1,5 +1,5 @@
 """Compile the HIP libraries for gfx950 -- csrc/wht_affine.hip into libwht_affine.so, csrc/wht_attention.hip into
-libwht_attention.so -- and the tensor calls' marshalling (csrc/torch_marshal.cpp, csrc/attention_marshal.cpp)
+libwht_attention.so, csrc/wht_attention4.hip into libwht_attention4.so -- and the tensor calls' marshalling (csrc/torch_marshal.cpp, csrc/attention_marshal.cpp)
 into the extension modules _torch_marshal.so and _attention_marshal.so, in-tree.
 
 hipcc cross-compiles without a GPU; the extension modules take the host compiler and torch's headers.
@@ -39,6 +39,10 @@ ATTENTION_MARSHAL_LIB = os.path.join(HERE, "_attention_marshal.so")
 ATTENTION_QUERY_SRC = os.path.join(HERE, "csrc", "attention_query.cpp")         # its rules, for the tests
 ATTENTION_QUERY_LIB = os.path.join(HERE, "libwht_attention_query.so")
 
+# the cache in 4 bits, its attention, and rotary positions of several axes
+ATTENTION4_SRC = os.path.join(HERE, "csrc", "wht_attention4.hip")
+ATTENTION4_LIB = os.path.join(HERE, "libwht_attention4.so")
+
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # packed float32 VALU forms are kept out of the generated code on the test machines.  The
@@ -52,6 +56,9 @@ HIPCC_FLAGS = [
 HEADER = os.path.join(os.path.dirname(HERE), "include", "wht_affine.h")
 ATTENTION_HEADER = os.path.join(os.path.dirname(HERE), "include", "wht_attention.h")
 ATTENTION_SOURCES = [ATTENTION_SRC, ATTENTION_HEADER, HEADER] + [os.path.join(HERE, "csrc", f) for f in ("attention_device.h", "attention_plan.h")]
+ATTENTION4_HEADERS = [os.path.join(os.path.dirname(HERE), "include", f) for f in ("wht_attention4.h", "wht_rotary.h")]
+ATTENTION4_SOURCES = ([ATTENTION4_SRC, *ATTENTION4_HEADERS, *ATTENTION_SOURCES[1:]]
+                      + [os.path.join(HERE, "csrc", f) for f in ("attention4_device.h", "append4_device.h", "rotary_device.h", "attention4_plan.h")])
 SOURCES = [SRC, HEADER] + [os.path.join(HERE, "csrc", f) for f in ("wht_device.h", "wht_plan.h", "wht_route.h", "wht_validate.h")]
 
 
@@ -63,6 +70,7 @@ def build(verbose: bool = False, extra=()) -> str:
     _compile_rules(ROUTE_SRC, ROUTE_LIB, verbose)
     _compile_rules(ATTENTION_QUERY_SRC, ATTENTION_QUERY_LIB, verbose)
     _compile(ATTENTION_SRC, ATTENTION_LIB, verbose, extra)
+    _compile(ATTENTION4_SRC, ATTENTION4_LIB, verbose, extra)
     return _compile(SRC, LIB, verbose, extra)
 
 
@@ -104,20 +112,23 @@ def _compile(src: str, lib: str, verbose: bool, extra=()) -> str:
 def ensure_built(verbose: bool = False) -> str:
     """For harnesses (tests, smoke check, benchmark): compile only if nothing has been built yet.
     The binding itself never builds: a missing library is an error there."""
-    if not all(os.path.exists(lib) for lib in (LIB, COPY_LIB, POISON_LIB, MARSHAL_LIB, ROUTE_LIB, ATTENTION_LIB, ATTENTION_MARSHAL_LIB, ATTENTION_QUERY_LIB)):
+    if not all(os.path.exists(lib) for lib in (LIB, COPY_LIB, POISON_LIB, MARSHAL_LIB, ROUTE_LIB, ATTENTION_LIB, ATTENTION_MARSHAL_LIB, ATTENTION_QUERY_LIB,
+                                               ATTENTION4_LIB)):
         build(verbose=verbose)
     elif any(os.path.getmtime(f) > os.path.getmtime(MARSHAL_LIB) for f in (MARSHAL_SRC, HEADER)):
         raise RuntimeError(f"{MARSHAL_LIB} is older than its source: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > os.path.getmtime(ROUTE_LIB)
              for f in (ROUTE_SRC, os.path.join(HERE, "csrc", "wht_route.h"), os.path.join(HERE, "csrc", "wht_validate.h"), HEADER)):
         raise RuntimeError(f"{ROUTE_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
-    elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_MARSHAL_LIB) for f in (ATTENTION_MARSHAL_SRC, ATTENTION_HEADER, HEADER)):
+    elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_MARSHAL_LIB) for f in (ATTENTION_MARSHAL_SRC, ATTENTION_HEADER, *ATTENTION4_HEADERS, HEADER)):
         raise RuntimeError(f"{ATTENTION_MARSHAL_LIB} is older than its source: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_QUERY_LIB)
              for f in (ATTENTION_QUERY_SRC, os.path.join(HERE, "csrc", "attention_plan.h"), ATTENTION_HEADER, HEADER)):
         raise RuntimeError(f"{ATTENTION_QUERY_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_LIB) for f in ATTENTION_SOURCES):
         raise RuntimeError(f"{ATTENTION_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
+    elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION4_LIB) for f in ATTENTION4_SOURCES):
+        raise RuntimeError(f"{ATTENTION4_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > min(os.path.getmtime(LIB), os.path.getmtime(POISON_LIB))
              for f in SOURCES if os.path.exists(f)):
         # a stale binary would be validated and recorded under the new sources' name

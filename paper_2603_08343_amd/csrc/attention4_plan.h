@@ -1,0 +1,89 @@
+// Argument checks of the cache in 4 bits (include/wht_attention4.h) and of rotary positions of several axes (include/wht_rotary.h).
+// Calls are cut as attention_plan.h says.  Compiles without HIP.
+#pragma once
+#include "../../include/wht_attention4.h"
+#include "attention_plan.h"
+
+namespace wht {
+
+constexpr int kMaxPairs = WHT_ROTARY_MAX_HEAD / 2;
+
+// rotary > 0: whether every pair's axis is one of those that positions have.
+inline bool good_axes(const uint8_t* pair_axes, int rotary, int axes) {
+    for (int i = 0; pair_axes && i < rotary / 2; ++i)
+        if (pair_axes[i] >= axes) return false;
+    return true;
+}
+
+inline int check_rotary(const wht_attention_rows_t* x, const wht_attention_rows_t* out, int64_t T, int32_t heads, int32_t head_dim, const float* rope,
+                        int64_t rope_rows, int32_t rotary, const int32_t* positions, int32_t axes, const uint8_t* pair_axes, int32_t dtype) {
+    if (!x || !out || !x->data || !out->data || !rope) return WHT_ERR_NULL_PTR;
+    if (dtype != WHT_DTYPE_F32 && dtype != WHT_DTYPE_BF16) return WHT_ERR_BAD_DTYPE;
+    if (T < 0 || T > (int64_t)1 << 30 || heads < 1 || heads > 1024 || head_dim < 16 || head_dim > WHT_ROTARY_MAX_HEAD || head_dim % 16 != 0) return WHT_ERR_BAD_DIM;
+    if (rotary < 16 || rotary % 16 != 0 || rotary > head_dim || rope_rows < 0 || rope_rows > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
+    if (axes < 1 || axes > WHT_ROTARY_MAX_AXES || (!positions && axes != 1) || !good_axes(pair_axes, rotary, axes)) return WHT_ERR_BAD_DIM;
+    const int size = dtype == WHT_DTYPE_F32 ? 4 : 2;
+    if (!good_rows(x, heads, head_dim, size) || !good_rows(out, heads, head_dim, size) || ((uintptr_t)rope & 15u) != 0 || ((uintptr_t)positions & 3u) != 0) return WHT_ERR_MISALIGNED;
+    if (!apart({T, out->token_stride}, {heads, out->head_stride}, {1, 0}, head_dim)) return WHT_ERR_MISALIGNED;
+    return WHT_OK;
+}
+
+inline int check_cache4(const wht_attention_cache4_t* c, const wht_attention_batch_t* b, int32_t dtype) {
+    if (!c || !b || !c->k || !c->v || !c->k_scales || !c->v_scales || !b->table || !b->lengths) return WHT_ERR_NULL_PTR;
+    if (dtype != WHT_DTYPE_F32 && dtype != WHT_DTYPE_BF16) return WHT_ERR_BAD_DTYPE;
+    if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return WHT_ERR_BAD_DIM;
+    if (c->page_size < WHT_ATTENTION_MIN_PAGE || c->page_size > WHT_ATTENTION_MAX_PAGE || (c->page_size & (c->page_size - 1)) != 0) return WHT_ERR_BAD_DIM;
+    if (c->heads < 1 || c->heads > 1024 || c->pages < 1 || b->B < 0 || b->width < 1 || b->table_stride < 0) return WHT_ERR_BAD_DIM;
+    if ((int64_t)b->width * c->page_size > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
+    // a page's number is multiplied by its stride in bytes (both 32 bits), and a row's place in its page stays below 31
+    auto fits = [&](int64_t page, int64_t head, int64_t token, int row) {
+        return page >= 0 && page < (int64_t)1 << 32 && token >= row && token < (int64_t)1 << 31 && (c->page_size - 1) * token < (int64_t)1 << 31 && head >= 0 && head < (int64_t)1 << 31;
+    };
+    if (!fits(c->page_stride, c->head_stride, c->token_stride, c->head_dim / 2) ||
+        !fits(c->scale_page_stride, c->scale_head_stride, c->scale_token_stride, c->head_dim / 32)) return WHT_ERR_BAD_DIM;
+    if (((uintptr_t)c->k & 15u) != 0 || ((uintptr_t)c->v & 15u) != 0 || c->page_stride % 16 != 0 || c->head_stride % 16 != 0 || c->token_stride % 16 != 0) return WHT_ERR_MISALIGNED;
+    if (((uintptr_t)b->table & 3u) != 0 || ((uintptr_t)b->lengths & 3u) != 0 || ((uintptr_t)b->q_starts & 3u) != 0) return WHT_ERR_MISALIGNED;
+    return WHT_OK;
+}
+
+inline int check_append4(const wht_attention_rows_t* q, const wht_attention_rows_t* k, const wht_attention_rows_t* v, const wht_attention_rows_t* q_out,
+                         const wht_attention_rows_t* k_out, const wht_attention_rows_t* v_out, int64_t T, int32_t q_heads, const wht_attention_cache4_t* c,
+                         const wht_attention_batch_t* b, const float* rope, int64_t rope_rows, int32_t rotary, int64_t position, const int32_t* positions,
+                         int32_t axes, const uint8_t* pair_axes, int32_t dtype) {
+    if (!q || !k || !v || !q_out || !k_out || !v_out || !k->data || !v->data || (q->data && !q_out->data) || (rotary != 0 && !rope)) return WHT_ERR_NULL_PTR;
+    if (!k_out->data != !v_out->data) return WHT_ERR_NULL_PTR;
+    if (int rc = check_cache4(c, b, dtype)) return rc;
+    const int size = dtype == WHT_DTYPE_F32 ? 4 : 2;
+    if (T < 0 || T > (int64_t)1 << 30 || (q->data && (q_heads < 1 || q_heads > 1024))) return WHT_ERR_BAD_DIM;
+    if (rotary < 0 || rotary % 16 != 0 || rotary > c->head_dim || rope_rows < 0 || rope_rows > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
+    if (position < 0 || position > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
+    if (axes < 1 || axes > WHT_ROTARY_MAX_AXES || (!positions && axes != 1) || !good_axes(pair_axes, rotary, axes)) return WHT_ERR_BAD_DIM;
+    if (!good_rows(k, c->heads, c->head_dim, size) || !good_rows(v, c->heads, c->head_dim, size) || ((uintptr_t)rope & 15u) != 0 || ((uintptr_t)positions & 3u) != 0) return WHT_ERR_MISALIGNED;
+    if (q->data && (!good_rows(q, q_heads, c->head_dim, size) || !good_rows(q_out, q_heads, c->head_dim, size))) return WHT_ERR_MISALIGNED;
+    if (q->data && !apart({T, q_out->token_stride}, {q_heads, q_out->head_stride}, {1, 0}, c->head_dim)) return WHT_ERR_MISALIGNED;
+    if (k_out->data)
+        for (const wht_attention_rows_t* r : {k_out, v_out})
+            if (!good_rows(r, c->heads, c->head_dim, size) || !apart({T, r->token_stride}, {c->heads, r->head_stride}, {1, 0}, c->head_dim)) return WHT_ERR_MISALIGNED;
+    if (!apart({c->pages, c->page_stride}, {c->heads, c->head_stride}, {c->page_size, c->token_stride}, c->head_dim / 2) ||
+        !apart({c->pages, c->scale_page_stride}, {c->heads, c->scale_head_stride}, {c->page_size, c->scale_token_stride}, c->head_dim / 32)) return WHT_ERR_MISALIGNED;
+    return WHT_OK;
+}
+
+inline int check_paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out, const float* lse, int64_t T, int32_t q_heads,
+                        const wht_attention_cache4_t* c, const wht_attention_batch_t* b, const int32_t* prefix_table, int64_t prefix,
+                        int32_t max_q, int64_t max_length, float scale, int32_t dtype) {
+    if (!q || !out || !q->data || !out->data || (prefix > 0 && !prefix_table)) return WHT_ERR_NULL_PTR;
+    if (int rc = check_cache4(c, b, dtype)) return rc;
+    if (int rc = check_sizes(T, b->B, q_heads, c->heads, c->head_dim, max_q, max_length, prefix, dtype)) return rc;
+    if (!(scale > 0.0f) || !(base2_scale(scale) < __builtin_inff())) return WHT_ERR_BAD_DIM;
+    // the few-rows kernel counts the blocks of its line in 31 bits
+    const int64_t own = (int64_t)b->width * c->page_size < max_length ? (int64_t)b->width * c->page_size : max_length;
+    if (((int64_t)b->B + 1) * (own / kBlockKeys + prefix / kBlockKeys + 2) > INT32_MAX / c->heads) return WHT_ERR_BAD_DIM;
+    const int size = dtype == WHT_DTYPE_F32 ? 4 : 2;
+    if (!good_rows(q, q_heads, c->head_dim, size) || !good_rows(out, q_heads, c->head_dim, size)) return WHT_ERR_MISALIGNED;
+    if (!apart({T, out->token_stride}, {q_heads, out->head_stride}, {1, 0}, c->head_dim)) return WHT_ERR_MISALIGNED;
+    if (((uintptr_t)lse & 3u) != 0 || ((uintptr_t)prefix_table & 3u) != 0) return WHT_ERR_MISALIGNED;
+    return WHT_OK;
+}
+
+}  // namespace wht

@@ -1130,7 +1130,22 @@ __device__ __forceinline__ Parts slots(const JoinArgs& a, int b, int head, int n
     return {a.own_part, a.own_sums, ((p.first << a.gang_log2) + (head - (group << a.gang_log2))) * a.own_cap + row, (int64_t)a.own_cap << a.gang_log2, p.count};
 }
 
-template <class T, int D, int WAVES>
+// H (of 32) / 8 of a row's outputs, four to a lane.
+__device__ __forceinline__ f32x4 transform_outputs(f32x4 x) {
+    x = f32x4{x[0] + x[1], x[0] - x[1], x[2] + x[3], x[2] - x[3]};
+    x = f32x4{x[0] + x[2], x[1] + x[3], x[0] - x[2], x[1] - x[3]};
+#pragma unroll
+    for (int h = 1; h < 8; h <<= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float other = __shfl_xor(x[i], h);
+            x[i] = threadIdx.x & h ? other - x[i] : x[i] + other;
+        }
+    return x * 0.125f;
+}
+
+// TRANSFORM: of the cache in 4 bits, whose values may be transformed.
+template <class T, int D, int WAVES, bool TRANSFORM = false>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(JoinArgs a) {
     constexpr int kLanes = D / 4, kAtOnce = 64 / kLanes, kUnroll = 4;
     struct Share { float m, l; f32x4 o[kLanes]; };
@@ -1222,13 +1237,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Joi
     if (empty) { l = 0.0f; m = WHT_NEG_INF; o = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }              // padding
     if (value != 0.0f) l = value;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if constexpr (TRANSFORM) o = transform_outputs(o);
     if (lane < kLanes) store4<T>(a.out + t * a.out_ts + qh * a.out_hs + lane * 4 * sizeof(T), value != 0.0f ? f32x4{value, value, value, value} : o * inv);
     if (a.lse && lane == 0) a.lse[r] = l == 0.0f ? WHT_NEG_INF : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // The same where every row has its pieces at the same places: the shares that a tile's keys were split into.  D / 4 lanes take a row, so that a wave has two
 // or more; which row it is matters only for what is written, and is looked up beside the loads.
-template <class T, int D>
+template <class T, int D, bool TRANSFORM = false>
 __global__ __launch_bounds__(256) void join_splits_kernel(JoinArgs a) {
     constexpr int kLanes = D / 4, kRows = 256 / kLanes, kUnroll = 4;
     const int64_t rows = (int64_t)a.batch.T * a.q_heads, r = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
@@ -1263,6 +1279,7 @@ __global__ __launch_bounds__(256) void join_splits_kernel(JoinArgs a) {
         }
     }
     int b = sequence_of(a.batch, t0);                               // of the block's first row; the others' is that or one soon after
+    if constexpr (TRANSFORM) o = transform_outputs(o);
     if (!there) return;
     float value = 0.0f;
     while (b >= 0 && b < a.batch.B) {
