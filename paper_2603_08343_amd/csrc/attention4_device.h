@@ -75,23 +75,19 @@ struct Few4 {
 
     static __device__ __forceinline__ int scale_index(int i) { return ((int)(threadIdx.x >> 4 & 3) * kElements + i * 8) / 32; }
 
-    static __device__ __forceinline__ void load(Part& p, const unsigned char* codes, const unsigned char* scales, const int64_t (&code_at)[2], const int64_t (&scale_at)[2]) {
-        const int g = threadIdx.x >> 4 & 3;
+    // Of key or value k of the two: `codes` and `scales` on from places that all lanes share, by what is the lane's own.
+    static __device__ __forceinline__ void load(Part& p, int k, const unsigned char* codes, const unsigned char* scales, unsigned code_off, unsigned scale_off) {
+        const unsigned char* from = codes + code_off;
+        if constexpr (D == 128) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(from);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const unsigned char* from = code_at[k] >= 0 ? codes + code_at[k] + g * (kElements / 2) : zero_chunk;
-            if constexpr (D == 128) {
-                const u32x4 x = *reinterpret_cast<const u32x4*>(from);
+            for (int i = 0; i < 4; ++i) p.code[k][i] = x[i];
+        } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p.code[k][i] = x[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) p.code[k][i] = reinterpret_cast<const unsigned*>(from)[i];
-            }
-            const unsigned char* at = code_at[k] >= 0 ? scales + scale_at[k] + scale_index(0) : zero_chunk;
-            p.scale[k][0] = *at;
-            if constexpr (kScales == 2) p.scale[k][1] = code_at[k] >= 0 ? *(at - scale_index(0) + scale_index(kWords - 1)) : 0;
+            for (int i = 0; i < kWords; ++i) p.code[k][i] = reinterpret_cast<const unsigned*>(from)[i];
         }
+        p.scale[k][0] = scales[scale_off];
+        if constexpr (kScales == 2) p.scale[k][1] = scales[scale_off + (unsigned)(scale_index(kWords - 1) - scale_index(0))];
     }
     static __device__ __forceinline__ float scale_at(const unsigned (&scale)[kScales], int i) {
         if constexpr (kScales == 1) return scale_of(scale[0]);
@@ -150,153 +146,181 @@ struct Few4 {
         return v;
     }
 
-    // One block of 32 keys from key0 on; limit: how many keys each tile's row of this lane sees, uneven: rows see different ones of them.
-    template <bool MULTI>
-    static __device__ __forceinline__ void block(const Part& kp, const Part& vp, unsigned buf, const bf16x8 (&q)[TILES][kTermsOf][kWords], int key0,
-                                                 const int (&limit)[TILES], const bool (&there)[2], bool masked, bool uneven, float scale, Odd& odd, State (&st)[TILES]) {
-        const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-        f32x4 s[TILES][2];
-#pragma unroll
-        for (int n = 0; n < TILES; ++n)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) s[n][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) {
-                const bf16x8 x = decode(kp.code[k][i], scale_at(kp.scale[k], i));
-#pragma unroll
-                for (int n = 0; n < TILES; ++n)
-#pragma unroll
-                    for (int e = kTermsOf - 1; e >= 0; --e) s[n][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[n][e][i], s[n][k], 0, 0, 0);
-            }
-
-        // Values to LDS.  A value that is not a number is in all 32 of its block; a key that a row does not see has a weight of zero, and zero times NaN is
-        // NaN: where rows see different keys such blocks stay out of the product, and rows that see one get it by itself.
-        bool any_odd = false;
-        if constexpr (MULTI) {
-            if (uneven) {
-                bool mine = false;
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int i = 0; i < kScales; ++i) mine |= vp.scale[k][i] >= 253;
-                any_odd = __any(mine);
-                if (any_odd) {
-                    if (lane < D / 8) odd.first[lane] = INT_MAX;
-                    reads_done();
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int i = 0; i < kWords; ++i)
-                            if (!(fabsf(scale_at(vp.scale[k], i)) < __builtin_inff())) atomicMin(&odd.first[g * kWords + i], key0 + 16 * k + c);
-                    reads_done();
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) {
-                float f = scale_at(vp.scale[k], i);
-                unsigned code = vp.code[k][i];
-                if (MULTI && any_odd && !(fabsf(f) < __builtin_inff())) { f = 1.0f; code = 0; }
-                const int row = 16 * k + c;
-                *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(buf + row * L::kRowBytes + L::v_place(row, g * kWords + i) * 16) = __builtin_bit_cast(u32x4, decode(code, f));
-            }
-
-        bf16x8 w[TILES][kTermsOf];
-#pragma unroll
-        for (int n = 0; n < TILES; ++n) {
-            if (masked) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = 16 * k + 4 * g + i;
-                        // whether the key's page names memory is known where its row was loaded
-                        const bool loaded = __shfl((int)there[k], 4 * g + i) != 0;
-                        s[n][k][i] = key0 + key < limit[n] && loaded ? s[n][k][i] : WHT_NEG_INF;
-                    }
-            }
-            rebase(scale, s[n], st[n]);
-            float sum = 0.0f;
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][k][i], scale, -st[n].base));
-                    sum += p;
-                    bf16 t[kTermsOf];
-                    split<kTermsOf>(p, t);
-#pragma unroll
-                    for (int e = 0; e < kTermsOf; ++e) w[n][e][k * 4 + i] = t[e];
-                }
-            st[n].l += sum;
-        }
-        reads_done();                                               // the wave's own writes
-#pragma unroll
-        for (int d = 0; d < kBlocks; ++d) {
-            const bf16x8 v = values(buf, d);
-#pragma unroll
-            for (int n = 0; n < TILES; ++n)
-#pragma unroll
-                for (int e = kTermsOf - 1; e >= 0; --e) st[n].o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[n][e], st[n].o[d], 0, 0, 0);
-        }
-        if (MULTI && any_odd) {
-#pragma unroll
-            for (int d = 0; d < kBlocks; ++d) {
-                const int first = odd.first[d * 2 + (g >> 1)];
-#pragma unroll
-                for (int n = 0; n < TILES; ++n)
-                    if (first < limit[n]) st[n].o[d] += __builtin_nanf("");
-            }
-        }
-        reads_done();                                               // before the next block's values overwrite these
-    }
-
     // Blocks [n0, n1) of `table`'s tokens, of which there are `keys`; limit: how many of them this lane's rows see, all_see: how many every row sees.
-    template <bool MULTI>
+    // Codes of two blocks are on their way while a third is worked on.
+    // NARROW: pages of 8 tokens, so that 16 keys are of two.
+    template <bool MULTI, bool NARROW>
     static __device__ __forceinline__ void run(const Attention4Args& args, const int* table, int n0, int n1, int keys, const int (&limit)[TILES], int all_see,
                                                int head, unsigned buf, const bf16x8 (&q)[TILES][kTermsOf][kWords], Odd& odd, State (&st)[TILES]) {
         const AttentionArgs& a = args.base;
-        const int lane = threadIdx.x & 63, c = lane & 15;
+        const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, shift = a.page_shift;
         const unsigned char *kc = a.k + head * a.head_stride, *vc = a.v + head * a.head_stride, *ks = args.ks + head * args.s_head_stride, *vs = args.vs + head * args.s_head_stride;
+        const unsigned code_off = c * a.token_stride + g * (kElements / 2), scale_off = c * args.s_token_stride + scale_index(0);
         const int last = min(n1 * kBlockKeys, keys);
         int key0 = n0 * kBlockKeys;
         while (key0 < last) {
             // 64 pages at a time, one per lane
-            const int first = key0 >> a.page_shift, end = min((int64_t)last, (int64_t)(first + 64) << a.page_shift);
+            const int first = key0 >> shift, end = min((int64_t)last, (int64_t)(first + 64) << shift);
             int page = -1;
-            const bool listed = ((int64_t)(first + lane) << a.page_shift) < end;
+            const bool listed = ((int64_t)(first + lane) << shift) < end;
             if (listed) page = table[first + lane];
             if (page >= a.pages) page = -1;
             const bool bad = __any(listed && page < 0);
-            auto fetch = [&](int from, Part& k, Part& v, bool (&there)[2]) {
-                int64_t code_at[2], scale_at[2];
+            const int named = max(page, 0);                         // keys that are not there are read from a page that is, and not used
+            auto fetch = [&](int from, Part& k, Part& v) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int key = from + 16 * i + c, slot = key & ((1 << a.page_shift) - 1);
-                    const int at = __shfl(page, min((key >> a.page_shift) - first, 63));
-                    there[i] = at >= 0 && key < end;
-                    code_at[i] = there[i] ? (int64_t)((uint64_t)(unsigned)at * a.page_stride + (unsigned)slot * a.token_stride) : -1;
-                    scale_at[i] = (int64_t)((uint64_t)(unsigned)at * args.s_page_stride + (unsigned)slot * args.s_token_stride);
+                    const int key = from + 16 * i, slot = key & ((1 << shift) - 1);
+                    if constexpr (!NARROW) {
+                        const unsigned at = __builtin_amdgcn_readlane(named, min((key >> shift) - first, 63));
+                        const uint64_t codes = (uint64_t)at * a.page_stride + (unsigned)slot * a.token_stride, scales = (uint64_t)at * args.s_page_stride + (unsigned)slot * args.s_token_stride;
+                        load(k, i, kc + codes, ks + scales, code_off, scale_off);
+                        load(v, i, vc + codes, vs + scales, code_off, scale_off);
+                    } else {
+                        const int mine = key + c, place = mine & ((1 << shift) - 1);
+                        const unsigned at = __shfl(named, min((mine >> shift) - first, 63));
+                        const uint64_t codes = (uint64_t)at * a.page_stride + (unsigned)place * a.token_stride, scales = (uint64_t)at * args.s_page_stride + (unsigned)place * args.s_token_stride;
+                        load(k, i, kc + codes, ks + scales, code_off - c * a.token_stride, scale_off - c * args.s_token_stride);
+                        load(v, i, vc + codes, vs + scales, code_off - c * a.token_stride, scale_off - c * args.s_token_stride);
+                    }
                 }
-                load(k, kc, ks, code_at, scale_at);
-                load(v, vc, vs, code_at, scale_at);
             };
-            Part k, v, k2, v2;
-            bool there[2], there2[2];
-            fetch(key0, k, v, there);
+            auto there = [&](int key) {                             // by all lanes
+                const int at = __shfl(page, min((key >> shift) - first, 63));
+                return key < end && at >= 0;
+            };
+
+            // 32 keys from `from` on; what is two blocks further on is fetched as soon as this one's codes are used
+            auto block = [&](int from, Part& kp, Part& vp) {
+                f32x4 s[TILES][2];
+#pragma unroll
+                for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) s[n][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) {
+                        const bf16x8 x = decode(kp.code[k][i], scale_at(kp.scale[k], i));
+#pragma unroll
+                        for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                            for (int e = kTermsOf - 1; e >= 0; --e) s[n][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[n][e][i], s[n][k], 0, 0, 0);
+                    }
+                const int next = from + kBlockKeys;
+                if (bad || next > end) {                            // values of keys that are not there: zeros
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const bool known = there(from + 16 * k + c);
+#pragma unroll
+                        for (int i = 0; i < kWords; ++i) vp.code[k][i] = known ? vp.code[k][i] : 0;
+#pragma unroll
+                        for (int i = 0; i < kScales; ++i) vp.scale[k][i] = known ? vp.scale[k][i] : 127;
+                    }
+                }
+                // A value that is not a number is in all 32 of its block; a key that a row does not see has a weight of zero, and zero times NaN is NaN: where
+                // rows see different keys such blocks stay out of the product, and rows that see one get it by itself.
+                bool any_odd = false;
+                if constexpr (MULTI) {
+                    if (all_see < min(next, keys)) {
+                        bool mine = false;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+#pragma unroll
+                            for (int i = 0; i < kScales; ++i) mine |= vp.scale[k][i] >= 253;
+                        any_odd = __any(mine);
+                        if (any_odd) {
+                            if (lane < D / 8) odd.first[lane] = INT_MAX;
+                            reads_done();
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                                for (int i = 0; i < kWords; ++i)
+                                    if (!(fabsf(scale_at(vp.scale[k], i)) < __builtin_inff())) {
+                                        atomicMin(&odd.first[g * kWords + i], from + 16 * k + c);
+                                        vp.code[k][i] = 0;
+                                    }
+#pragma unroll
+                                for (int i = 0; i < kScales; ++i)
+                                    if (vp.scale[k][i] >= 253) vp.scale[k][i] = 127;
+                            }
+                            reads_done();
+                        }
+                    }
+                }
+                // a wave's reads and writes of LDS happen in their order: no waits
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) {
+                        const int row = 16 * k + c;
+                        *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(buf + row * L::kRowBytes + L::v_place(row, g * kWords + i) * 16) =
+                            __builtin_bit_cast(u32x4, decode(vp.code[k][i], scale_at(vp.scale[k], i)));
+                    }
+                if (next + kBlockKeys < end) fetch(next + kBlockKeys, kp, vp);
+
+                bf16x8 w[TILES][kTermsOf];
+#pragma unroll
+                for (int n = 0; n < TILES; ++n) {
+                    if (bad) {
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) s[n][k][i] = there(from + 16 * k + 4 * g + i) ? s[n][k][i] : WHT_NEG_INF;
+                    }
+                    if (next > all_see) {
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) s[n][k][i] = from + 16 * k + 4 * g + i < limit[n] ? s[n][k][i] : WHT_NEG_INF;
+                    }
+                    rebase(a.scale, s[n], st[n]);
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][k][i], a.scale, -st[n].base));
+                            sum += p;
+                            bf16 t[kTermsOf];
+                            split<kTermsOf>(p, t);
+#pragma unroll
+                            for (int e = 0; e < kTermsOf; ++e) w[n][e][k * 4 + i] = t[e];
+                        }
+                    st[n].l += sum;
+                }
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int d = 0; d < kBlocks; ++d) {
+                    const bf16x8 v = values(buf, d);
+#pragma unroll
+                    for (int n = 0; n < TILES; ++n)
+#pragma unroll
+                        for (int e = kTermsOf - 1; e >= 0; --e) st[n].o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[n][e], st[n].o[d], 0, 0, 0);
+                }
+                if (MULTI && any_odd) {
+#pragma unroll
+                    for (int d = 0; d < kBlocks; ++d) {
+                        const int seen = odd.first[d * 2 + (g >> 1)];
+#pragma unroll
+                        for (int n = 0; n < TILES; ++n)
+                            if (seen < limit[n]) st[n].o[d] += __builtin_nanf("");
+                    }
+                    reads_done();
+                }
+                asm volatile("" ::: "memory");
+            };
+
+            Part k[2], v[2];
+            fetch(key0, k[0], v[0]);
+            if (key0 + kBlockKeys < end) fetch(key0 + kBlockKeys, k[1], v[1]);
             while (true) {
-                const int next = key0 + kBlockKeys;
-                const bool more = next < end;
-                if (more) fetch(next, k2, v2, there2);
-                block<MULTI>(k, v, buf, q, key0, limit, there, bad || next > all_see, all_see < min(next, keys), a.scale, odd, st);
-                key0 = next;
-                if (!more) break;
-                k = k2; v = v2;
-                there[0] = there2[0]; there[1] = there2[1];
+                block(key0, k[0], v[0]);
+                key0 += kBlockKeys;
+                if (key0 >= end) break;
+                block(key0, k[1], v[1]);
+                key0 += kBlockKeys;
+                if (key0 >= end) break;
             }
         }
     }
@@ -382,8 +406,9 @@ __device__ __forceinline__ void few_rows4(const Attention4Args& args, int block,
         for (int part = FRONT ? 1 : 0; part < 2; ++part) {          // the prefix, the sequence
             const int lo = part ? max(n0 - front, 0) : n0, hi = part ? n1 - front : min(n1, front);
             if (lo >= hi) continue;
-            F::template run<MULTI>(args, part ? a.batch.table + b * a.batch.table_stride : a.prefix_table, lo, hi, part ? keys : a.prefix, part ? limit : whole,
-                                   part ? all_see : a.prefix, head, buf, q, shared.odd[wave], st);
+            const int* table = part ? a.batch.table + b * a.batch.table_stride : a.prefix_table;
+            if (a.page_shift >= 4) F::template run<MULTI, false>(args, table, lo, hi, part ? keys : a.prefix, part ? limit : whole, part ? all_see : a.prefix, head, buf, q, shared.odd[wave], st);
+            else F::template run<MULTI, true>(args, table, lo, hi, part ? keys : a.prefix, part ? limit : whole, part ? all_see : a.prefix, head, buf, q, shared.odd[wave], st);
         }
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {
