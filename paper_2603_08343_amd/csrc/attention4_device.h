@@ -64,6 +64,16 @@ struct Few4 {
     static constexpr int kBlocks = D / 16, kTermsOf = kTerms<T>;
     using L = Head<bf16, D>;
     static constexpr int kWaveBytes = 32 * L::kRowBytes;
+    static constexpr int kAhead = 2;                                // blocks whose codes are in registers or on their way
+
+    // Where 16-byte chunk `chunk` of row `row` of the values stands in its row in LDS.  A wave writes a chunk of 16 rows at a time, which take all 16 groups
+    // of four banks, and reads 32 bytes of eight rows, which take all eight of 32 bytes.
+    static __device__ __forceinline__ int place(int row, int chunk) {
+        const int low = (row >> 3) & 1;
+        if constexpr (D == 128) return chunk ^ ((row & 3) << 2 | ((row >> 2) & 1) << 1 | low);
+        else if constexpr (D == 64) return chunk ^ (((row >> 2) & 1) << 2 | ((row >> 1) & 1) << 1 | low);
+        else return chunk ^ (((row >> 2) & 1) << 1 | low);
+    }
 
     // Codes and scale bytes of a lane's part of two keys or values.
     struct Part { unsigned code[2][kWords]; unsigned scale[2][kScales]; };
@@ -134,7 +144,7 @@ struct Few4 {
     // 8 keys by 16 columns of the values in LDS, transposed, from column 16 d on.
     static __device__ __forceinline__ bf16x8 values(unsigned buf, int d) {
         const int lane = threadIdx.x & 63, g = lane >> 4, in = lane & 15, row = g * 4 + (in >> 2), c = d * 2 + ((in & 3) >> 1);
-        const unsigned at = buf + row * L::kRowBytes + L::v_place(row, c) * 16 + (in & 1) * 8;
+        const unsigned at = buf + row * L::kRowBytes + place(row, c) * 16 + (in & 1) * 8;
         bf16x8 v;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -148,7 +158,7 @@ struct Few4 {
 
     // Blocks [n0, n1) of `table`'s tokens, of which there are `keys`; limit: how many of them this lane's rows see, all_see: how many every row sees.
     // Codes of two blocks are on their way while a third is worked on.
-    // NARROW: pages of 8 tokens, so that 16 keys are of two.
+    // NARROW: pages of 8 tokens.
     template <bool MULTI, bool NARROW>
     static __device__ __forceinline__ void run(const Attention4Args& args, const int* table, int n0, int n1, int keys, const int (&limit)[TILES], int all_see,
                                                int head, unsigned buf, const bf16x8 (&q)[TILES][kTermsOf][kWords], Odd& odd, State (&st)[TILES]) {
@@ -167,21 +177,30 @@ struct Few4 {
             if (page >= a.pages) page = -1;
             const bool bad = __any(listed && page < 0);
             const int named = max(page, 0);                         // keys that are not there are read from a page that is, and not used
+            // of 16 (pages of 8 tokens: 8) keys the page, and where its rows are, are the same for all lanes
+            auto row_of = [&](int key, uint64_t& codes, uint64_t& scales) {
+                const unsigned at = __builtin_amdgcn_readlane(named, min((key >> shift) - first, 63)), slot = key & ((1 << shift) - 1);
+                codes = (uint64_t)at * a.page_stride + slot * a.token_stride;
+                scales = (uint64_t)at * args.s_page_stride + slot * args.s_token_stride;
+            };
             auto fetch = [&](int from, Part& k, Part& v) {
+                uint64_t codes[2], scales[2];
+                row_of(from, codes[0], scales[0]);
+                row_of(from + 16, codes[1], scales[1]);
+                if constexpr (!NARROW) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int key = from + 16 * i, slot = key & ((1 << shift) - 1);
-                    if constexpr (!NARROW) {
-                        const unsigned at = __builtin_amdgcn_readlane(named, min((key >> shift) - first, 63));
-                        const uint64_t codes = (uint64_t)at * a.page_stride + (unsigned)slot * a.token_stride, scales = (uint64_t)at * args.s_page_stride + (unsigned)slot * args.s_token_stride;
-                        load(k, i, kc + codes, ks + scales, code_off, scale_off);
-                        load(v, i, vc + codes, vs + scales, code_off, scale_off);
-                    } else {
-                        const int mine = key + c, place = mine & ((1 << shift) - 1);
-                        const unsigned at = __shfl(named, min((mine >> shift) - first, 63));
-                        const uint64_t codes = (uint64_t)at * a.page_stride + (unsigned)place * a.token_stride, scales = (uint64_t)at * args.s_page_stride + (unsigned)place * args.s_token_stride;
-                        load(k, i, kc + codes, ks + scales, code_off - c * a.token_stride, scale_off - c * args.s_token_stride);
-                        load(v, i, vc + codes, vs + scales, code_off - c * a.token_stride, scale_off - c * args.s_token_stride);
+                    for (int i = 0; i < 2; ++i) {
+                        load(k, i, kc + codes[i], ks + scales[i], code_off, scale_off);
+                        load(v, i, vc + codes[i], vs + scales[i], code_off, scale_off);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint64_t more_codes, more_scales;
+                        row_of(from + 16 * i + 8, more_codes, more_scales);
+                        const uint64_t at = c < 8 ? codes[i] : more_codes - 8 * a.token_stride, scale = c < 8 ? scales[i] : more_scales - 8 * args.s_token_stride;
+                        load(k, i, kc + at, ks + scale, code_off, scale_off);
+                        load(v, i, vc + at, vs + scale, code_off, scale_off);
                     }
                 }
             };
@@ -254,10 +273,10 @@ struct Few4 {
 #pragma unroll
                     for (int i = 0; i < kWords; ++i) {
                         const int row = 16 * k + c;
-                        *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(buf + row * L::kRowBytes + L::v_place(row, g * kWords + i) * 16) =
+                        *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(buf + row * L::kRowBytes + place(row, g * kWords + i) * 16) =
                             __builtin_bit_cast(u32x4, decode(vp.code[k][i], scale_at(vp.scale[k], i)));
                     }
-                if (next + kBlockKeys < end) fetch(next + kBlockKeys, kp, vp);
+                if (from + kAhead * kBlockKeys < end) fetch(from + kAhead * kBlockKeys, kp, vp);
 
                 bf16x8 w[TILES][kTermsOf];
 #pragma unroll
@@ -311,16 +330,17 @@ struct Few4 {
                 asm volatile("" ::: "memory");
             };
 
-            Part k[2], v[2];
-            fetch(key0, k[0], v[0]);
-            if (key0 + kBlockKeys < end) fetch(key0 + kBlockKeys, k[1], v[1]);
-            while (true) {
-                block(key0, k[0], v[0]);
-                key0 += kBlockKeys;
-                if (key0 >= end) break;
-                block(key0, k[1], v[1]);
-                key0 += kBlockKeys;
-                if (key0 >= end) break;
+            Part k[kAhead], v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (i == 0 || key0 + i * kBlockKeys < end) fetch(key0 + i * kBlockKeys, k[i], v[i]);
+            while (key0 < end) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    if (key0 >= end) break;
+                    block(key0, k[i], v[i]);
+                    key0 += kBlockKeys;
+                }
             }
         }
     }
@@ -333,7 +353,7 @@ struct FewShared {
 };
 
 // The line is that of few_rows() in attention_device.h.  FRONT: the prefix is the launch's other workgroups' work.
-template <class T, int D, int TILES, bool MULTI, bool FRONT>
+template <class T, int D, int TILES, bool MULTI, bool FRONT, bool NARROW>
 __device__ __forceinline__ void few_rows4(const Attention4Args& args, int block, FewShared<T, D, TILES>& shared) {
     using F = Few4<T, D, TILES>;
     const AttentionArgs& a = args.base;
@@ -360,7 +380,7 @@ __device__ __forceinline__ void few_rows4(const Attention4Args& args, int block,
         for (int b = b0; b < b1; ++b) { a.cum[b] = n; n += line_blocks(a, b, line_sequence(a, b)); }
         if (lane == 0) a.cum[B] = all;
     }
-    const int total = all * groups, per = line_share(total, a.rows_cap, a.gang_log2);
+    const int total = all * groups, per = line_share(total, a.rows_cap, a.gang_log2, kWorkers4Log2);
     int u = min((int64_t)total, (int64_t)worker * per);
     const int end = min(total, u + per);
     if (u >= end) return;
@@ -407,8 +427,7 @@ __device__ __forceinline__ void few_rows4(const Attention4Args& args, int block,
             const int lo = part ? max(n0 - front, 0) : n0, hi = part ? n1 - front : min(n1, front);
             if (lo >= hi) continue;
             const int* table = part ? a.batch.table + b * a.batch.table_stride : a.prefix_table;
-            if (a.page_shift >= 4) F::template run<MULTI, false>(args, table, lo, hi, part ? keys : a.prefix, part ? limit : whole, part ? all_see : a.prefix, head, buf, q, shared.odd[wave], st);
-            else F::template run<MULTI, true>(args, table, lo, hi, part ? keys : a.prefix, part ? limit : whole, part ? all_see : a.prefix, head, buf, q, shared.odd[wave], st);
+            F::template run<MULTI, NARROW>(args, table, lo, hi, part ? keys : a.prefix, part ? limit : whole, part ? all_see : a.prefix, head, buf, q, shared.odd[wave], st);
         }
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {
@@ -765,7 +784,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void many_rows4_kern
     many_rows4<T, D, false>(a, blockIdx.x, shared);
 }
 
-template <class T, int D, int TILES, bool MULTI, bool FRONT>
+template <class T, int D, int TILES, bool MULTI, bool FRONT, bool NARROW>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows4_kernel(Attention4Args a, Attention4Args front, int front_blocks) {
     if constexpr (FRONT) {
         __shared__ union Both {
@@ -774,10 +793,10 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows4_kerne
         } shared;
         const int block = blockIdx.x;
         if (block < front_blocks) many_rows4<T, D, true>(front, block, shared.many);
-        else few_rows4<T, D, TILES, MULTI, true>(a, block - front_blocks, shared.few);
+        else few_rows4<T, D, TILES, MULTI, true, NARROW>(a, block - front_blocks, shared.few);
     } else {
         __shared__ FewShared<T, D, TILES> shared;
-        few_rows4<T, D, TILES, MULTI, false>(a, blockIdx.x, shared);
+        few_rows4<T, D, TILES, MULTI, false, NARROW>(a, blockIdx.x, shared);
     }
 }
 

@@ -6,6 +6,10 @@
 
 namespace wht {
 
+// Waves of the few-rows kernel's grid.
+constexpr int kWorkers4Log2 = 11;
+constexpr int kWorkgroups4 = 1 << (kWorkers4Log2 - 2);
+
 constexpr int kMaxPairs = WHT_ROTARY_MAX_HEAD / 2;
 
 // rotary > 0: whether every pair's axis is one of those that positions have.
