@@ -66,13 +66,12 @@ struct Few4 {
     static constexpr int kWaveBytes = 32 * L::kRowBytes;
     static constexpr int kAhead = 2;                                // blocks whose codes are in registers or on their way
 
-    // Where 16-byte chunk `chunk` of row `row` of the values stands in its row in LDS.  A wave writes a chunk of 16 rows at a time, which take all 16 groups
-    // of four banks, and reads 32 bytes of eight rows, which take all eight of 32 bytes.
+    // Where 16-byte chunk `chunk` of row `row` of the values stands in its row in LDS.  A write takes eight rows' chunks at a time, which have to fill 128
+    // bytes, a transposing read 32 bytes of eight rows, which have to fill 256: no bank conflicts.
     static __device__ __forceinline__ int place(int row, int chunk) {
-        const int low = (row >> 3) & 1;
-        if constexpr (D == 128) return chunk ^ ((row & 3) << 2 | ((row >> 2) & 1) << 1 | low);
-        else if constexpr (D == 64) return chunk ^ (((row >> 2) & 1) << 2 | ((row >> 1) & 1) << 1 | low);
-        else return chunk ^ (((row >> 2) & 1) << 1 | low);
+        if constexpr (D == 128) return chunk ^ ((row & 3) << 1 | ((row >> 2) & 1) * 9);
+        else if constexpr (D == 64) return chunk ^ (row & 7);
+        else return chunk ^ (((row >> 2) & 1) << 1 | ((row >> 1) & 1));
     }
 
     // Codes and scale bytes of a lane's part of two keys or values.
