@@ -84,16 +84,23 @@ struct Few4 {
 
     static __device__ __forceinline__ int scale_index(int i) { return ((int)(threadIdx.x >> 4 & 3) * kElements + i * 8) / 32; }
 
+    // A word of codes; PAST: read once, not kept in the caches.
+    template <class V, bool PAST>
+    static __device__ __forceinline__ V words(const unsigned char* from) {
+        if constexpr (PAST) return __builtin_nontemporal_load(reinterpret_cast<const V*>(from));
+        else return *reinterpret_cast<const V*>(from);
+    }
     // Of key or value k of the two: `codes` and `scales` on from places that all lanes share, by what is the lane's own.
+    template <bool PAST>
     static __device__ __forceinline__ void load(Part& p, int k, const unsigned char* codes, const unsigned char* scales, unsigned code_off, unsigned scale_off) {
         const unsigned char* from = codes + code_off;
         if constexpr (D == 128) {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(from);
+            const u32x4 x = words<u32x4, PAST>(from);
 #pragma unroll
             for (int i = 0; i < 4; ++i) p.code[k][i] = x[i];
         } else {
 #pragma unroll
-            for (int i = 0; i < kWords; ++i) p.code[k][i] = reinterpret_cast<const unsigned*>(from)[i];
+            for (int i = 0; i < kWords; ++i) p.code[k][i] = words<unsigned, PAST>(from + i * 4);
         }
         p.scale[k][0] = scales[scale_off];
         if constexpr (kScales == 2) p.scale[k][1] = scales[scale_off + (unsigned)(scale_index(kWords - 1) - scale_index(0))];
@@ -157,8 +164,8 @@ struct Few4 {
 
     // Blocks [n0, n1) of `table`'s tokens, of which there are `keys`; limit: how many of them this lane's rows see, all_see: how many every row sees.
     // Codes of two blocks are on their way while a third is worked on.
-    // NARROW: pages of 8 tokens.
-    template <bool MULTI, bool NARROW>
+    // NARROW: pages of 8 tokens; STREAM: codes are read past the caches.
+    template <bool MULTI, bool NARROW, bool STREAM>
     static __device__ __forceinline__ void run(const Attention4Args& args, const int* table, int n0, int n1, int keys, const int (&limit)[TILES], int all_see,
                                                int head, unsigned buf, const bf16x8 (&q)[TILES][kTermsOf][kWords], Odd& odd, State (&st)[TILES]) {
         const AttentionArgs& a = args.base;
@@ -189,8 +196,8 @@ struct Few4 {
                 if constexpr (!NARROW) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        load(k, i, kc + codes[i], ks + scales[i], code_off, scale_off);
-                        load(v, i, vc + codes[i], vs + scales[i], code_off, scale_off);
+                        load<STREAM>(k, i, kc + codes[i], ks + scales[i], code_off, scale_off);
+                        load<STREAM>(v, i, vc + codes[i], vs + scales[i], code_off, scale_off);
                     }
                 } else {
 #pragma unroll
@@ -198,8 +205,8 @@ struct Few4 {
                         uint64_t more_codes, more_scales;
                         row_of(from + 16 * i + 8, more_codes, more_scales);
                         const uint64_t at = c < 8 ? codes[i] : more_codes - 8 * a.token_stride, scale = c < 8 ? scales[i] : more_scales - 8 * args.s_token_stride;
-                        load(k, i, kc + at, ks + scale, code_off, scale_off);
-                        load(v, i, vc + at, vs + scale, code_off, scale_off);
+                        load<STREAM>(k, i, kc + at, ks + scale, code_off, scale_off);
+                        load<STREAM>(v, i, vc + at, vs + scale, code_off, scale_off);
                     }
                 }
             };
@@ -352,7 +359,7 @@ struct FewShared {
 };
 
 // The line is that of few_rows() in attention_device.h.  FRONT: the prefix is the launch's other workgroups' work.
-template <class T, int D, int TILES, bool MULTI, bool FRONT, bool NARROW>
+template <class T, int D, int TILES, bool MULTI, bool FRONT, bool NARROW, bool STREAM>
 __device__ __forceinline__ void few_rows4(const Attention4Args& args, int block, FewShared<T, D, TILES>& shared) {
     using F = Few4<T, D, TILES>;
     const AttentionArgs& a = args.base;
@@ -379,7 +386,7 @@ __device__ __forceinline__ void few_rows4(const Attention4Args& args, int block,
         for (int b = b0; b < b1; ++b) { a.cum[b] = n; n += line_blocks(a, b, line_sequence(a, b)); }
         if (lane == 0) a.cum[B] = all;
     }
-    const int total = all * groups, per = line_share(total, a.rows_cap, a.gang_log2, kWorkers4Log2);
+    const int total = all * groups, per = line_share<kWorkers4>(total, a.rows_cap, a.gang_log2);
     int u = min((int64_t)total, (int64_t)worker * per);
     const int end = min(total, u + per);
     if (u >= end) return;
@@ -426,7 +433,7 @@ __device__ __forceinline__ void few_rows4(const Attention4Args& args, int block,
             const int lo = part ? max(n0 - front, 0) : n0, hi = part ? n1 - front : min(n1, front);
             if (lo >= hi) continue;
             const int* table = part ? a.batch.table + b * a.batch.table_stride : a.prefix_table;
-            F::template run<MULTI, NARROW>(args, table, lo, hi, part ? keys : a.prefix, part ? limit : whole, part ? all_see : a.prefix, head, buf, q, shared.odd[wave], st);
+            F::template run<MULTI, NARROW, STREAM>(args, table, lo, hi, part ? keys : a.prefix, part ? limit : whole, part ? all_see : a.prefix, head, buf, q, shared.odd[wave], st);
         }
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {
@@ -783,7 +790,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void many_rows4_kern
     many_rows4<T, D, false>(a, blockIdx.x, shared);
 }
 
-template <class T, int D, int TILES, bool MULTI, bool FRONT, bool NARROW>
+template <class T, int D, int TILES, bool MULTI, bool FRONT, bool NARROW, bool STREAM>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows4_kernel(Attention4Args a, Attention4Args front, int front_blocks) {
     if constexpr (FRONT) {
         __shared__ union Both {
@@ -792,10 +799,10 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows4_kerne
         } shared;
         const int block = blockIdx.x;
         if (block < front_blocks) many_rows4<T, D, true>(front, block, shared.many);
-        else few_rows4<T, D, TILES, MULTI, true, NARROW>(a, block - front_blocks, shared.few);
+        else few_rows4<T, D, TILES, MULTI, true, NARROW, STREAM>(a, block - front_blocks, shared.few);
     } else {
         __shared__ FewShared<T, D, TILES> shared;
-        few_rows4<T, D, TILES, MULTI, false, NARROW>(a, blockIdx.x, shared);
+        few_rows4<T, D, TILES, MULTI, false, NARROW, STREAM>(a, blockIdx.x, shared);
     }
 }
 

@@ -7,8 +7,13 @@
 namespace wht {
 
 // Waves of the few-rows kernel's grid.
-constexpr int kWorkers4Log2 = 11;
-constexpr int kWorkgroups4 = 1 << (kWorkers4Log2 - 2);
+constexpr int kWorkgroups4 = 512;
+constexpr int kWorkers4 = 4 * kWorkgroups4;
+
+// Whether the few-rows kernel reads a call's own codes past the caches: by the rule of streams() in attention_plan.h, with a row's bytes here.
+inline bool streams4(int32_t B, int32_t heads, int32_t head_dim, int64_t max_length, int64_t prefix, int32_t gang_log2) {
+    return gang_log2 == 0 && ((double)B * max_length + prefix) * heads * (head_dim / 2 + head_dim / 32) * 2 >= 96e6;
+}
 
 constexpr int kMaxPairs = WHT_ROTARY_MAX_HEAD / 2;
 

@@ -1124,10 +1124,10 @@ struct JoinArgs {
 struct Parts { const float *part, *sums; int64_t at, step; int n; };        // rows at, at + step, ...
 
 // The pieces that the few-rows kernel left of the line's b-th sequence, n blocks long, and a head; total: blocks of all sequences.
-template <int WORKERS_LOG2>
+template <int WORKERS>
 __device__ __forceinline__ Parts slots(const JoinArgs& a, int b, int head, int n, int total, int row) {
     const int groups = a.heads >> a.gang_log2, group = head >> a.gang_log2;
-    const Slots p = item_slots(b * groups + group, a.cum[b] * groups + group * n, n, total * groups, a.own_cap, a.gang_log2, WORKERS_LOG2);
+    const Slots p = item_slots<WORKERS>(b * groups + group, a.cum[b] * groups + group * n, n, total * groups, a.own_cap, a.gang_log2);
     return {a.own_part, a.own_sums, ((p.first << a.gang_log2) + (head - (group << a.gang_log2))) * a.own_cap + row, (int64_t)a.own_cap << a.gang_log2, p.count};
 }
 
@@ -1146,7 +1146,7 @@ __device__ __forceinline__ f32x4 transform_outputs(f32x4 x) {
 }
 
 // TRANSFORM: of the cache in 4 bits, whose values may be transformed.
-template <class T, int D, int WAVES, bool TRANSFORM = false, int WORKERS_LOG2 = kWorkersLog2>
+template <class T, int D, int WAVES, bool TRANSFORM = false, int WORKERS = kWorkers>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(JoinArgs a) {
     constexpr int kLanes = D / 4, kAtOnce = 64 / kLanes, kUnroll = 4;
     struct Share { float m, l; f32x4 o[kLanes]; };
@@ -1210,8 +1210,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void join_kernel(Joi
         if (j < 0 || j >= s.queries || j >= a.max_q) value = __builtin_nanf("");
         else {
             const int total = a.cum[a.batch.B + (a.front && a.front_few)];
-            if (a.front && a.front_few) add(slots<WORKERS_LOG2>(a, a.batch.B, head, ceil_div(a.prefix, kBlockKeys), total, t * a.G + g));
-            add(slots<WORKERS_LOG2>(a, b, head, (a.own_prefix ? ceil_div(a.prefix, kBlockKeys) : 0) + ceil_div(s.length, kBlockKeys), total, j * a.G + g));
+            if (a.front && a.front_few) add(slots<WORKERS>(a, a.batch.B, head, ceil_div(a.prefix, kBlockKeys), total, t * a.G + g));
+            add(slots<WORKERS>(a, b, head, (a.own_prefix ? ceil_div(a.prefix, kBlockKeys) : 0) + ceil_div(s.length, kBlockKeys), total, j * a.G + g));
         }
     }
     const f32x4 mine = o;

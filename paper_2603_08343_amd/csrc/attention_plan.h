@@ -85,10 +85,8 @@ inline int64_t die_blocks(int64_t T, int64_t B, int64_t G, int64_t max_q, int64_
     return packed < each ? packed : each;
 }
 
-constexpr int kWorkersLog2 = 11;
-static_assert(kWorkers == 1 << kWorkersLog2, "shares are counted by shifting");
 inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t head_dim, int32_t max_q,
-                                    int64_t max_length, int64_t prefix, int workers_log2 = kWorkersLog2) {
+                                    int64_t max_length, int64_t prefix, int workers = kWorkers) {
     AttentionPlan p{};
     const int64_t G = q_heads / heads;
     p.own_few = max_q * G <= kFewRows;
@@ -107,7 +105,7 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
         }
     }
     p.own_cap = p.front && p.front_few ? (int32_t)(T * G) : max_q * (int32_t)G;
-    if (p.own_few) p.own_rows = (((size_t)B + 1) * heads + ((size_t)1 << workers_log2)) * (size_t)p.own_cap;
+    if (p.own_few) p.own_rows = (((size_t)B + 1) * heads + (size_t)workers) * (size_t)p.own_cap;
     else {
         p.own_splits = splits_for(most_tiles(T, B, G, max_q) * heads, max_length + prefix);
         if (p.own_splits > 1) p.own_rows = (size_t)p.own_splits * (size_t)(T * q_heads);
@@ -131,13 +129,16 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
 // 28.3 / 23.6 / 24.9, 4 of 8 and 2000 to 4000 27.0 / 23.8 / 26.8, 32 of 8 and 750 to 1500 52.4 / 50.0 / 49.9, 8 of 4 and 750 to 1500 19.8 / 20.3 / 20.3.
 // With a gang of heads a worker is a workgroup, an item a group of heads, and every slot holds one piece for each of them.
 struct Slots { int64_t first; int count; };
-WHT_HD int line_share(int total, int rows, int gang_log2, int all_workers_log2 = kWorkersLog2) {
-    const int workers_log2 = all_workers_log2 - gang_log2, even = (total + (1 << workers_log2) - 1) >> workers_log2, least = even > 1 ? (rows + 7) >> 3 : 1;
+template <int WORKERS = kWorkers>
+WHT_HD int line_share(int total, int rows, int gang_log2) {
+    constexpr unsigned kAll = WORKERS;                              // a power of two is a shift
+    const int even = (int)((((uint64_t)(unsigned)total << gang_log2) + kAll - 1) / kAll), least = even > 1 ? (rows + 7) >> 3 : 1;
     return even > least ? even : least;
 }
-WHT_HD Slots item_slots(int item, int u0, int n, int total, int rows, int gang_log2, int all_workers_log2 = kWorkersLog2) {
+template <int WORKERS = kWorkers>
+WHT_HD Slots item_slots(int item, int u0, int n, int total, int rows, int gang_log2) {
     if (n == 0) return {0, 0};
-    const int per = line_share(total, rows, gang_log2, all_workers_log2), w0 = u0 / per, w1 = (u0 + n - 1) / per;
+    const int per = line_share<WORKERS>(total, rows, gang_log2), w0 = u0 / per, w1 = (u0 + n - 1) / per;
     return {(int64_t)item + w0, w1 - w0 + 1};
 }
 // Four heads side by side: where a row is no whole number of 128-byte lines, and the next head's row follows it in memory.

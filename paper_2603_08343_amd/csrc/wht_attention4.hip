@@ -140,6 +140,7 @@ static int paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out
     a.use_prefix = !p.front && prefix > 0;
     a.front_item = p.front && p.front_few;
     a.gang_log2 = gang_log2_of(c->heads, c->head_dim / 2, a.head_stride);
+    const bool past = streams4(b->B, c->heads, c->head_dim, a.batch.most, a.use_prefix ? prefix : 0, a.gang_log2);
     a.splits = p.own_splits; a.rows_cap = p.own_cap;
     a.part = reinterpret_cast<float*>(ws + p.own_at); a.sums = reinterpret_cast<float*>(ws + p.own_sums_at);
     a.cum = reinterpret_cast<int*>(ws + p.cum_at);
@@ -152,17 +153,17 @@ static int paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out
         const dim3 grid((unsigned)(front_blocks + own_blocks)), block(256);
         if (!p.own_few) hipLaunchKernelGGL((many_rows4_kernel<E, D>), grid, block, 0, stream, args);
         else
-            with_flags([&](auto two, auto multi, auto front) {
+            with_flags([&](auto two, auto multi, auto front, auto past) {
                 constexpr int kTiles = decltype(two)::value ? 2 : 1;
-                constexpr bool kMulti = decltype(multi)::value, kFront = decltype(front)::value;
+                constexpr bool kMulti = decltype(multi)::value, kFront = decltype(front)::value, kPast = decltype(past)::value && sizeof(E) == 2;
                 if constexpr (kTiles == 2 && kMulti) {
                     if (a.page_shift < 4) {                         // the one kernel for pages of 8 tokens
-                        hipLaunchKernelGGL((few_rows4_kernel<E, D, kTiles, kMulti, kFront, true>), grid, block, 0, stream, args, f, (int)front_blocks);
+                        hipLaunchKernelGGL((few_rows4_kernel<E, D, kTiles, kMulti, kFront, true, false>), grid, block, 0, stream, args, f, (int)front_blocks);
                         return;
                     }
                 }
-                hipLaunchKernelGGL((few_rows4_kernel<E, D, kTiles, kMulti, kFront, false>), grid, block, 0, stream, args, f, (int)front_blocks);
-            }, a.page_shift < 4 || p.own_cap > kSmallTile, a.page_shift < 4 || max_q > 1, front_blocks > 0);        // max_q = 1: a sequence's rows all see the same keys
+                hipLaunchKernelGGL((few_rows4_kernel<E, D, kTiles, kMulti, kFront, false, kPast>), grid, block, 0, stream, args, f, (int)front_blocks);
+            }, a.page_shift < 4 || p.own_cap > kSmallTile, a.page_shift < 4 || max_q > 1, front_blocks > 0, past);  // max_q = 1: a sequence's rows all see the same keys
         return launched();
     });
     if (rc) return rc;
@@ -182,9 +183,9 @@ static int paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out
         with_flags([&](auto turn) {
             constexpr bool kTurn = decltype(turn)::value;
             if (!p.own_few) hipLaunchKernelGGL((join_splits_kernel<E, D, kTurn>), dim3((unsigned)ceil_div64(rows, 256 / (D / 4))), dim3(256), 0, stream, j);
-            else if (join_waves(rows) == 16) hipLaunchKernelGGL((join_kernel<E, D, 16, kTurn, kWorkers4Log2>), dim3((unsigned)rows), dim3(1024), 0, stream, j);
-            else if (join_waves(rows) == 4) hipLaunchKernelGGL((join_kernel<E, D, 4, kTurn, kWorkers4Log2>), dim3((unsigned)rows), dim3(256), 0, stream, j);
-            else hipLaunchKernelGGL((join_kernel<E, D, 1, kTurn, kWorkers4Log2>), grid_of(ceil_div64(rows, 4)), dim3(256), 0, stream, j);
+            else if (join_waves(rows) == 16) hipLaunchKernelGGL((join_kernel<E, D, 16, kTurn, kWorkers4>), dim3((unsigned)rows), dim3(1024), 0, stream, j);
+            else if (join_waves(rows) == 4) hipLaunchKernelGGL((join_kernel<E, D, 4, kTurn, kWorkers4>), dim3((unsigned)rows), dim3(256), 0, stream, j);
+            else hipLaunchKernelGGL((join_kernel<E, D, 1, kTurn, kWorkers4>), grid_of(ceil_div64(rows, 4)), dim3(256), 0, stream, j);
         }, transform != 0);
         return launched();
     });
@@ -231,7 +232,7 @@ size_t wht_attention4_workspace_bytes(int64_t T, int32_t B, int32_t q_heads, int
                                       int64_t prefix_length, int32_t dtype) {
     using namespace wht;
     if (check_sizes(T, B, q_heads, heads, head_dim, max_q, max_length, prefix_length, dtype) != WHT_OK || T == 0) return 0;
-    return plan_attention(T, B, q_heads, heads, head_dim, max_q, max_length, prefix_length, kWorkers4Log2).bytes;
+    return plan_attention(T, B, q_heads, heads, head_dim, max_q, max_length, prefix_length, kWorkers4).bytes;
 }
 
 int wht_attention_paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out, float* lse, int64_t T, int32_t q_heads,
@@ -241,7 +242,7 @@ int wht_attention_paged4(const wht_attention_rows_t* q, const wht_attention_rows
     using namespace wht;
     if (int rc = check_paged4(q, out, lse, T, q_heads, cache, batch, prefix_table, prefix_length, max_q, max_length, scale, dtype)) return rc;
     if (T == 0) return WHT_OK;
-    const AttentionPlan p = plan_attention(T, batch->B, q_heads, cache->heads, cache->head_dim, max_q, max_length, prefix_length, kWorkers4Log2);
+    const AttentionPlan p = plan_attention(T, batch->B, q_heads, cache->heads, cache->head_dim, max_q, max_length, prefix_length, kWorkers4);
     if (p.bytes > 0 && (!workspace || workspace_bytes < p.bytes)) return WHT_ERR_WORKSPACE;
     if (((uintptr_t)workspace & 15u) != 0) return WHT_ERR_MISALIGNED;
     return paged4(q, out, lse, T, q_heads, cache, batch, prefix_table, prefix_length, max_q, max_length, scale, transform, dtype, p,
