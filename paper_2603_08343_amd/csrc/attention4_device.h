@@ -386,7 +386,7 @@ __device__ __forceinline__ void few_rows4(const Attention4Args& args, int block,
         for (int b = b0; b < b1; ++b) { a.cum[b] = n; n += line_blocks(a, b, line_sequence(a, b)); }
         if (lane == 0) a.cum[B] = all;
     }
-    const int total = all * groups, per = line_share<kWorkers4>(total, a.rows_cap, a.gang_log2);
+    const int total = all * groups, per = line_share<4 * workgroups4(sizeof(T) == 4, D, TILES, FRONT)>(total, a.rows_cap, a.gang_log2);
     int u = min((int64_t)total, (int64_t)worker * per);
     const int end = min(total, u + per);
     if (u >= end) return;
@@ -791,7 +791,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void many_rows4_kern
 }
 
 template <class T, int D, int TILES, bool MULTI, bool FRONT, bool NARROW, bool STREAM>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void few_rows4_kernel(Attention4Args a, Attention4Args front, int front_blocks) {
+__global__ __launch_bounds__(256, (sizeof(T) == 4 ? 1 : workgroups4(false, D, TILES, FRONT) / 256)) void few_rows4_kernel(Attention4Args a, Attention4Args front, int front_blocks) {
     if constexpr (FRONT) {
         __shared__ union Both {
             FewShared<T, D, TILES> few;

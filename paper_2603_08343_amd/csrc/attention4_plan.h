@@ -6,9 +6,11 @@
 
 namespace wht {
 
-// Waves of the few-rows kernel's grid.
-constexpr int kWorkgroups4 = 512;
-constexpr int kWorkers4 = 4 * kWorkgroups4;
+// The few-rows kernel's workgroups, of four workers: three on a compute unit where a worker's registers allow it, else two.  Heads of 128 need more of
+// them for the rows they sum up, and have more to do between two loads.  Two / three, in us: 48 sequences of 2 to 5 new tokens and up to 6000 of their own at
+// 16 x 96 77 / 71; 256 of up to 8192 at 32 and 8 x 128 204 / 212, one of 65001 22.3 / 25.7.
+constexpr int workgroups4(bool f32, int head_dim, int tiles, bool front) { return f32 || head_dim == 128 || tiles == 2 || front ? 512 : 768; }
+constexpr int kMostWorkers4 = 4 * 768;
 
 // Whether the few-rows kernel reads a call's own codes past the caches: by the rule of streams() in attention_plan.h, with a row's bytes here.
 inline bool streams4(int32_t B, int32_t heads, int32_t head_dim, int64_t max_length, int64_t prefix, int32_t gang_log2) {

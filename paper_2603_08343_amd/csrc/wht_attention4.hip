@@ -144,7 +144,9 @@ static int paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out
     a.splits = p.own_splits; a.rows_cap = p.own_cap;
     a.part = reinterpret_cast<float*>(ws + p.own_at); a.sums = reinterpret_cast<float*>(ws + p.own_sums_at);
     a.cum = reinterpret_cast<int*>(ws + p.cum_at);
-    const int64_t each = die_blocks(T, b->B, a.G, max_q, (int64_t)c->heads * a.splits), own_blocks = p.own_few ? kWorkgroups4 : (each + 1) * kDies;
+    const bool two_tiles = a.page_shift < 4 || p.own_cap > kSmallTile;
+    const int workgroups = workgroups4(dtype == WHT_DTYPE_F32, c->head_dim, two_tiles ? 2 : 1, front_blocks > 0);
+    const int64_t each = die_blocks(T, b->B, a.G, max_q, (int64_t)c->heads * a.splits), own_blocks = p.own_few ? workgroups : (each + 1) * kDies;
     if (front_blocks + own_blocks > kMostWorkgroups) return WHT_ERR_BAD_DIM;
     a.fill = (int)each;
     const int rc = with_type(dtype, c->head_dim, [&](auto t, auto d) {
@@ -163,7 +165,7 @@ static int paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out
                     }
                 }
                 hipLaunchKernelGGL((few_rows4_kernel<E, D, kTiles, kMulti, kFront, false, kPast>), grid, block, 0, stream, args, f, (int)front_blocks);
-            }, a.page_shift < 4 || p.own_cap > kSmallTile, a.page_shift < 4 || max_q > 1, front_blocks > 0, past);  // max_q = 1: a sequence's rows all see the same keys
+            }, two_tiles, a.page_shift < 4 || max_q > 1, front_blocks > 0, past);  // max_q = 1: a sequence's rows all see the same keys
         return launched();
     });
     if (rc) return rc;
@@ -180,13 +182,14 @@ static int paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out
         using E = decltype(t);
         constexpr int D = decltype(d)::value;
         const int64_t rows = T * q_heads;
-        with_flags([&](auto turn) {
+        with_flags([&](auto turn, auto more) {
             constexpr bool kTurn = decltype(turn)::value;
+            constexpr int kWorkersOf = decltype(more)::value && D != 128 && sizeof(E) == 2 ? kMostWorkers4 : kWorkers;
             if (!p.own_few) hipLaunchKernelGGL((join_splits_kernel<E, D, kTurn>), dim3((unsigned)ceil_div64(rows, 256 / (D / 4))), dim3(256), 0, stream, j);
-            else if (join_waves(rows) == 16) hipLaunchKernelGGL((join_kernel<E, D, 16, kTurn, kWorkers4>), dim3((unsigned)rows), dim3(1024), 0, stream, j);
-            else if (join_waves(rows) == 4) hipLaunchKernelGGL((join_kernel<E, D, 4, kTurn, kWorkers4>), dim3((unsigned)rows), dim3(256), 0, stream, j);
-            else hipLaunchKernelGGL((join_kernel<E, D, 1, kTurn, kWorkers4>), grid_of(ceil_div64(rows, 4)), dim3(256), 0, stream, j);
-        }, transform != 0);
+            else if (join_waves(rows) == 16) hipLaunchKernelGGL((join_kernel<E, D, 16, kTurn, kWorkersOf>), dim3((unsigned)rows), dim3(1024), 0, stream, j);
+            else if (join_waves(rows) == 4) hipLaunchKernelGGL((join_kernel<E, D, 4, kTurn, kWorkersOf>), dim3((unsigned)rows), dim3(256), 0, stream, j);
+            else hipLaunchKernelGGL((join_kernel<E, D, 1, kTurn, kWorkersOf>), grid_of(ceil_div64(rows, 4)), dim3(256), 0, stream, j);
+        }, transform != 0, workgroups > kWorkgroups);
         return launched();
     });
 }
@@ -232,7 +235,7 @@ size_t wht_attention4_workspace_bytes(int64_t T, int32_t B, int32_t q_heads, int
                                       int64_t prefix_length, int32_t dtype) {
     using namespace wht;
     if (check_sizes(T, B, q_heads, heads, head_dim, max_q, max_length, prefix_length, dtype) != WHT_OK || T == 0) return 0;
-    return plan_attention(T, B, q_heads, heads, head_dim, max_q, max_length, prefix_length, kWorkers4).bytes;
+    return plan_attention(T, B, q_heads, heads, head_dim, max_q, max_length, prefix_length, kMostWorkers4).bytes;
 }
 
 int wht_attention_paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out, float* lse, int64_t T, int32_t q_heads,
@@ -242,7 +245,7 @@ int wht_attention_paged4(const wht_attention_rows_t* q, const wht_attention_rows
     using namespace wht;
     if (int rc = check_paged4(q, out, lse, T, q_heads, cache, batch, prefix_table, prefix_length, max_q, max_length, scale, dtype)) return rc;
     if (T == 0) return WHT_OK;
-    const AttentionPlan p = plan_attention(T, batch->B, q_heads, cache->heads, cache->head_dim, max_q, max_length, prefix_length, kWorkers4);
+    const AttentionPlan p = plan_attention(T, batch->B, q_heads, cache->heads, cache->head_dim, max_q, max_length, prefix_length, kMostWorkers4);
     if (p.bytes > 0 && (!workspace || workspace_bytes < p.bytes)) return WHT_ERR_WORKSPACE;
     if (((uintptr_t)workspace & 15u) != 0) return WHT_ERR_MISALIGNED;
     return paged4(q, out, lse, T, q_heads, cache, batch, prefix_table, prefix_length, max_q, max_length, scale, transform, dtype, p,
