@@ -454,13 +454,29 @@ __device__ __forceinline__ void few_rows4(const Attention4Args& args, int block,
 // Many rows: the pipeline of attention_device.h -- 128 rows a workgroup, 64 keys a step, keys and values in LDS twice over -- behind registers: a thread holds
 // the codes of the steps after those in LDS, and makes bfloat16 rows of them as a step begins.
 
+// Where chunks stand in LDS, as in Head, but for rows that are written from registers: a write takes eight rows' chunks at a time, which have to fill 128 bytes
+// (r0, r1, ...: the bits of a row's number).  Reads are as there: K's 16 rows at a time fill 256 bytes, V's 64 bytes of four rows.
+template <int D>
+struct Written : Head<bf16, D> {
+    static __device__ __forceinline__ int k_place(int r, int c) {
+        if constexpr (D == 128) return c ^ (r & 15);
+        else if constexpr (D == 64) return c ^ ((r >> 1 & 3) | ((r ^ r >> 3) & 1) << 2);
+        else { const int p = c + (r >> 2 & 1) + 2 * ((r >> 1 ^ r >> 3) & 1); return p >= 12 ? p - 12 : p; }
+    }
+    static __device__ __forceinline__ int v_place(int r, int c) {
+        if constexpr (D == 128) return c ^ ((r & 3) << 2 | (r >> 2 & 1) << 1 | (r >> 1 & 1));
+        else if constexpr (D == 64) return c ^ ((r >> 1 & 1) << 2 | (r >> 2 & 1) << 1 | (r & 1));
+        else return c ^ ((r >> 2 & 1) << 1 | (r >> 1 & 1));
+    }
+};
+
 template <class T, int D>
 struct Many4 {
     using L = Head<bf16, D>;
+    using W = Written<D>;
     static constexpr int kTermsOf = kTerms<T>;
-    static constexpr int kBytes = D == 64 ? 8 : 16;                 // of codes, that a thread takes of a step
+    static constexpr int kBytes = D == 64 ? 8 : 16;                 // of codes, that a lane takes of a step: a wave 16 rows
     static constexpr int kPieces = D / 2 / kBytes;                  // of a row: 4, 3, 4
-    static constexpr int kThreads = kStepKeys * kPieces;            // 256, 192 (96 wide)
     static constexpr int kWords = kBytes / 4;
     static constexpr int kTileBytes = kStepKeys * L::kRowBytes;
 
@@ -488,8 +504,8 @@ struct Many4 {
         const bool bad = __builtin_amdgcn_readfirstlane(list.bad[0] | list.bad[1] | list.bad[2] | list.bad[3]) != 0;
 
         // the thread's piece of a step's rows
-        const int r = threadIdx.x / kPieces, piece = threadIdx.x - r * kPieces;
-        const bool loads = kThreads == 256 || threadIdx.x < kThreads;
+        const int r = wave * 16 + (lane & 15), piece = lane >> 4;
+        const bool loads = piece < kPieces;
         const unsigned char *kc = a.k + head * a.head_stride, *vc = a.v + head * a.head_stride, *ks = args.ks + head * args.s_head_stride, *vs = args.vs + head * args.s_head_stride;
         auto fetch = [&](int t, const unsigned char* codes, const unsigned char* scales, Raw& x) {
             const bool own = t >= k.front;
@@ -519,7 +535,7 @@ struct Many4 {
             const unsigned at = buf + (t & 1) * kTileBytes + r * L::kRowBytes;
 #pragma unroll
             for (int i = 0; i < kWords; ++i)
-                *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(at + L::k_place(r, piece * kWords + i) * 16) = __builtin_bit_cast(u32x4, decode(x.code[i], f));
+                *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(at + W::k_place(r, piece * kWords + i) * 16) = __builtin_bit_cast(u32x4, decode(x.code[i], f));
         };
         // From this step on rows of the workgroup see different keys: blocks that are no numbers stay out of the product, and rows that see one get it at the end.
         const int uneven = k.front + level / kStepKeys;
@@ -540,7 +556,7 @@ struct Many4 {
             const unsigned at = buf + (2 + (t & 1)) * kTileBytes + r * L::kRowBytes;
 #pragma unroll
             for (int i = 0; i < kWords; ++i)
-                *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(at + L::v_place(r, piece * kWords + i) * 16) = __builtin_bit_cast(u32x4, decode(x.code[i], f));
+                *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(at + W::v_place(r, piece * kWords + i) * 16) = __builtin_bit_cast(u32x4, decode(x.code[i], f));
         };
         // the first or second 32 keys or values of step t
         auto keys_at = [&](int t, int half) { return fresh(buf + (t & 1) * kTileBytes + half * 32 * L::kRowBytes); };
@@ -564,9 +580,9 @@ struct Many4 {
 
         u32x4 frag[L::kSteps];                                      // keys of the block after the one whose scores are at hand
         auto read_keys = [&](unsigned at) {
-            const unsigned first_chunk = KeyReads<bf16, D>::first(at);
+            const unsigned first_chunk = KeyReads<bf16, D, W>::first(at);
 #pragma unroll
-            for (int i = 0; i < L::kSteps; ++i) frag[i] = lds_read<u32x4>(KeyReads<bf16, D>::chunk(first_chunk, i));
+            for (int i = 0; i < L::kSteps; ++i) frag[i] = lds_read<u32x4>(KeyReads<bf16, D, W>::chunk(first_chunk, i));
         };
         auto product = [&](f32x16& s) {
             s = f32x16{};
@@ -590,11 +606,51 @@ struct Many4 {
             for (int d = 0; d < L::kBlocks; ++d) {
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const bf16x8 v = values<D>(vat, half, d);
+                    const bf16x8 v = values<D, W>(vat, half, d);
 #pragma unroll
                     for (int e = kTermsOf - 1; e >= 0; --e) st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[e][half], st.o[d], 0, 0, 0);
                 }
                 asm volatile("" ::: "memory");                      // one block's values in registers at a time
+            }
+        };
+
+        // See full_block of ManyRange::stream.
+        auto full_block = [&](f32x16& s, f32x16& ahead, unsigned vat, unsigned kat, bool more) {
+            if constexpr (kTermsOf == 1) {
+                const unsigned first_chunk = KeyReads<bf16, D, W>::first(kat);
+                bf16x8 w[2];
+                float sum[2] = {0.0f, 0.0f};
+                ahead = f32x16{};
+#pragma unroll
+                for (int i = 0; i < L::kSteps; ++i) {
+                    ahead = score_step<bf16>(frag[i], q[0][i], ahead);
+                    frag[i] = __builtin_bit_cast(u32x4, values<D, W>(vat, i / L::kBlocks, i % L::kBlocks));
+#pragma unroll
+                    for (int e = 16 * i / L::kSteps; e < 16 * (i + 1) / L::kSteps; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale, -st.base));
+                        sum[e & 1] += p;
+                        w[e >> 3][e & 7] = (bf16)p;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                float mx = WHT_NEG_INF;
+#pragma unroll
+                for (int i = 0; i < L::kSteps; ++i) {
+                    st.o[i % L::kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, frag[i]), w[i / L::kBlocks], st.o[i % L::kBlocks], 0, 0, 0);
+                    frag[i] = lds_read<u32x4>(KeyReads<bf16, D, W>::chunk(first_chunk, i));
+                    // the last of `ahead` is a few instructions old
+                    if (i >= L::kSteps / 2)
+#pragma unroll
+                        for (int e = 16 * (2 * i - L::kSteps) / L::kSteps; e < 16 * (2 * i - L::kSteps + 2) / L::kSteps; ++e) mx = fmaxf(mx, ahead[e]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                st.l += sum[0] + sum[1];
+                if (more) ::wht::rebase<L, 8>(mx, a.scale, ahead, st);
+            } else {
+                product(ahead);
+                accumulate4(s, vat);
+                read_keys(kat);
+                if (more) ::wht::rebase<L, 8>(largest(ahead), a.scale, ahead, st);
             }
         };
 
@@ -616,14 +672,27 @@ struct Many4 {
         if (bad || !full(2 * lo)) hide(s, 2 * lo);
         ::wht::rebase<L, 8>(largest(s), a.scale, s, st);
         read_keys(keys_at(lo, 1));
-        for (int t = lo; t < hi; ++t) {
-            workgroup_barrier();                                    // V of this step and K of the next are in LDS; what is replaced next has been read
+        auto refill = [&](int t) {
             if (t + 1 < hi) put_v(t + 1, rv);
             if (t + 2 < hi) {
                 put_k(t + 2, rk);
                 fetch(t + 2, vc, vs, rv);
             }
             if (t + 3 < hi) fetch(t + 3, kc, ks, rk);
+        };
+        // A step's barrier stands in both loops below: a wave takes a step in either, whatever the others do.
+        for (int t = lo; t < hi; ++t) {
+            // steps whose blocks, and the first of the next one, are seen by all rows of the wave
+            const int blocks = 2 * t >= front || pre_full == front ? front + own_full : pre_full;
+            for (const int end = bad ? t : min(uneven, blocks >= 2 * hi ? hi : min(hi - 1, (blocks - 1) / 2)); t < end; ++t) {
+                workgroup_barrier();                                // V of this step and K of the next are in LDS; what is replaced next has been read
+                refill(t);
+                full_block(s, other, values_at(t, 0), keys_at(t + 1, 0), true);
+                full_block(other, s, values_at(t, 1), keys_at(t + 1, 1), t + 1 < hi);
+            }
+            if (t == hi) break;
+            workgroup_barrier();
+            refill(t);
 #pragma unroll 1
             for (int half = 0; half < 2; ++half) {
                 const int j = 2 * t + half;

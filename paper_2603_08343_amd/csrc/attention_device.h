@@ -311,9 +311,9 @@ __device__ __forceinline__ unsigned fresh(unsigned x) {
 template <class V>
 __device__ __forceinline__ V lds_read(unsigned at) { return *(const __attribute__((address_space(3))) V*)(uintptr_t)at; }
 
-template <class T, int D>
+template <class T, int D, class HEAD = Head<T, D>>
 struct KeyReads {                                                   // a lane reads chunks h, 2 + h, 4 + h, ... of row lane % 32
-    using H = Head<T, D>;
+    using H = HEAD;
     static constexpr bool kFlip = (H::kChunks & (H::kChunks - 1)) == 0;
     static __device__ __forceinline__ unsigned first(unsigned buf) {
         const int lane = threadIdx.x & 63, row = lane & 31, h = lane >> 5;
@@ -401,9 +401,8 @@ __device__ __forceinline__ void weigh(f32x16& s, float scale, RowState<H>& st) {
 
 // The A operand of the second product in bfloat16: 16 of 32 values in LDS at `buf` (ks: which), 32 columns from 32 d on.  A transposing read gives
 // lane i of 16 the i-th of 16 columns, four rows of it, that the 16 lanes address as 4 x 4 pieces of 8 bytes.
-template <int D>
+template <int D, class H = Head<bf16, D>>
 __device__ __forceinline__ bf16x8 values(unsigned buf, int ks, int d) {
-    using H = Head<bf16, D>;
     const int lane = threadIdx.x & 63, g = lane >> 4, in = lane & 15, row = (g >> 1) * 4 + (in >> 2), c = (g & 1) * 2 + ((in & 3) >> 1);
     const unsigned at = (H::kChunks & (H::kChunks - 1)) == 0 ? (buf + row * H::kRowBytes + H::v_place(row, c) * 16 + (in & 1) * 8) ^ (d * 64)
                                                              : buf + row * H::kRowBytes + H::v_place(row, d * 4 + c) * 16 + (in & 1) * 8;
