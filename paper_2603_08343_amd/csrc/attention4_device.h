@@ -507,17 +507,8 @@ struct Many4 {
         const int r = wave * 16 + (lane & 15), piece = lane >> 4;
         const bool loads = piece < kPieces;
         const unsigned char *kc = a.k + head * a.head_stride, *vc = a.v + head * a.head_stride, *ks = args.ks + head * args.s_head_stride, *vs = args.vs + head * args.s_head_stride;
-        auto fetch = [&](int t, const unsigned char* codes, const unsigned char* scales, Raw& x) {
-            const bool own = t >= k.front;
-            const int key = (own ? t - k.front : t) * kStepKeys + r, keys = own ? k.own : k.prefix, list_at = own ? own_at : pre_at;
-            const int page = loads && key < keys ? list.page[(key >> shift) + list_at] : -1;
-            const unsigned slot = (unsigned)(key & ((1 << shift) - 1));
-            const unsigned char* from = zero_chunk;
-            const unsigned char* scale = zero_chunk;
-            if (page >= 0) {
-                from = codes + ((uint64_t)(unsigned)page * a.page_stride + slot * a.token_stride + piece * kBytes);
-                scale = scales + ((uint64_t)(unsigned)page * args.s_page_stride + slot * args.s_token_stride + piece * kBytes / 16);
-            }
+        const unsigned code_off = (lane & 15) * a.token_stride + min(piece, kPieces - 1) * kBytes, scale_off = (lane & 15) * args.s_token_stride + min(piece, kPieces - 1) * kBytes / 16;
+        auto take = [&](const unsigned char* from, const unsigned char* scale, Raw& x) {
             if constexpr (kWords == 4) {
                 const u32x4 w = *reinterpret_cast<const u32x4*>(from);
 #pragma unroll
@@ -528,6 +519,25 @@ struct Many4 {
                 x.code[1] = (unsigned)(w >> 32);
             }
             x.scale = *scale;
+        };
+        // Where a step's keys are all there, in pages of 16 tokens at least, a wave's 16 are in one page, and a lane's place in it is the same every step.
+        auto fetch = [&](int t, const unsigned char* codes, const unsigned char* scales, Raw& x) {
+            const bool own = t >= k.front;
+            const int key0 = (own ? t - k.front : t) * kStepKeys, keys = own ? k.own : k.prefix, list_at = own ? own_at : pre_at;
+            if (!bad && shift >= 4 && key0 + kStepKeys <= keys) {
+                const int key = key0 + wave * 16;
+                const unsigned page = __builtin_amdgcn_readfirstlane(list.page[(key >> shift) + list_at]), slot = key & ((1 << shift) - 1);
+                take(codes + ((uint64_t)page * a.page_stride + slot * a.token_stride) + code_off, scales + ((uint64_t)page * args.s_page_stride + slot * args.s_token_stride) + scale_off, x);
+            } else {
+                const int key = key0 + r, page = loads && key < keys ? list.page[(key >> shift) + list_at] : -1;
+                const unsigned slot = (unsigned)(key & ((1 << shift) - 1));
+                const unsigned char *from = zero_chunk, *scale = zero_chunk;
+                if (page >= 0) {
+                    from = codes + ((uint64_t)(unsigned)page * a.page_stride + slot * a.token_stride + piece * kBytes);
+                    scale = scales + ((uint64_t)(unsigned)page * args.s_page_stride + slot * args.s_token_stride + piece * kBytes / 16);
+                }
+                take(from, scale, x);
+            }
         };
         auto put_k = [&](int t, const Raw& x) {
             if (!loads) return;
@@ -543,6 +553,7 @@ struct Many4 {
             if (!loads) return;
             if (t >= uneven && x.scale >= 253) {
                 list.odd[wave] = 1;
+#pragma unroll 1
                 for (int i = 0; i < kBytes * 2; ++i) {
                     const int col = piece * kBytes * 2 + i, key = (t - k.front) * kStepKeys + r;
                     atomicMin(&odd.above[col], key);
