@@ -29,7 +29,11 @@ __device__ __forceinline__ uint64_t near_lane(uint64_t x) {
 }
 template <int X> __device__ __forceinline__ double near_lane(double x) { return __builtin_bit_cast(double, near_lane<X>(__builtin_bit_cast(uint64_t, x))); }
 
-// Walsh-Hadamard transform of the 32 numbers that four lanes hold, eight each: three steps in registers, two between lanes.
+__device__ __forceinline__ float flip(float x, unsigned sign) { return __uint_as_float(__float_as_uint(x) ^ sign); }
+__device__ __forceinline__ double flip(double x, unsigned sign) { return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, x) ^ (uint64_t)sign << 32); }
+
+// Walsh-Hadamard transform of the 32 numbers that four lanes hold, eight each: three steps in registers, two between lanes (the neighbour's number and
+// one's own, with the sign that the lane's place gives it).
 template <class F>
 __device__ __forceinline__ void transform32(F (&x)[8]) {
 #pragma unroll
@@ -41,41 +45,45 @@ __device__ __forceinline__ void transform32(F (&x)[8]) {
                 x[i] = a + b;
                 x[i + h] = a - b;
             }
+    const unsigned odd1 = threadIdx.x << 31, odd2 = (threadIdx.x & 2) << 30;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { const F other = near_lane<1>(x[i]); x[i] = threadIdx.x & 1 ? other - x[i] : x[i] + other; }
+    for (int i = 0; i < 8; ++i) x[i] = near_lane<1>(x[i]) + flip(x[i], odd1);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { const F other = near_lane<2>(x[i]); x[i] = threadIdx.x & 2 ? other - x[i] : x[i] + other; }
+    for (int i = 0; i < 8; ++i) x[i] = near_lane<2>(x[i]) + flip(x[i], odd2);
 }
 
-// Codes of eight of a block's 32 numbers, and the block's scale byte.  The numbers are in 64 bits: a code is decided by which side of a border a
-// number is on, and what a sum in 32 bits is off by would now and then decide it.  They are made 32 bits wide with the last bit standing for whatever
-// was cut off, which leaves every border where it is, and go to the nearest code as the hardware does it.
-__device__ __forceinline__ unsigned encode(const double (&x)[8], unsigned& scale) {
-    constexpr uint64_t kMagnitude = ~(uint64_t)0 >> 1;
-    uint64_t most = 0;
+// Codes of eight of a block's 32 numbers times 2^power, and the block's scale byte.  The numbers are in 64 bits: a code is decided by which side of a border a
+// number is on, and what a sum in 32 bits is off by would now and then decide it.  Their upper 20 bits, with one more that stands for any lower ones, leave
+// every border where it is; as float32 numbers, in units of the scale, they go to the nearest code as the hardware does it.
+__device__ __forceinline__ unsigned encode(const double (&x)[8], int power, unsigned& scale) {
+    constexpr unsigned kMagnitude = 0x7fffffffu;
+    double most = __builtin_fabs(x[0]);
+    unsigned top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { const uint64_t m = __builtin_bit_cast(uint64_t, x[i]) & kMagnitude; most = m > most ? m : most; }
-    uint64_t other = near_lane<1>(most);
-    most = other > most ? other : most;
-    other = near_lane<2>(most);
-    most = other > most ? other : most;
-    const int exponent = (int)(most >> 52);                         // of the largest magnitude, + 1023
-    // the least e with most <= 1.5 * 2^(e + 2)
-    int e = exponent - 1023 - ((most & 0xfffffffffffffull) <= 0x8000000000000ull ? 2 : 1);
+    for (int i = 0; i < 8; ++i) {
+        most = __builtin_fmax(most, __builtin_fabs(x[i]));
+        top = max(top, (unsigned)(__builtin_bit_cast(uint64_t, x[i]) >> 32) & kMagnitude);          // a NaN, which the maximum passes over
+    }
+    most = __builtin_fmax(most, near_lane<1>(most));
+    most = __builtin_fmax(most, near_lane<2>(most));
+    top = max(top, near_lane<1>(top));
+    top = max(top, near_lane<2>(top));
+    if (top >= 0x7ff00000u) { scale = 255; return 0; }
+    const uint64_t bits = __builtin_bit_cast(uint64_t, most);
+    const int exponent = (int)(bits >> 52);                         // of the largest magnitude, + 1023
+    // the least e with most * 2^power <= 1.5 * 2^(e + 2)
+    int e = exponent + power - 1023 - ((bits & 0xfffffffffffffull) <= 0x8000000000000ull ? 2 : 1);
     e = exponent == 0 ? -124 : min(max(e, -124), 125);
-    if (exponent == 0x7ff) { scale = 255; return 0; }
     scale = (unsigned)(e + 127);
-    const double by = __builtin_bit_cast(double, (uint64_t)(1023 - e) << 52);
+    const int shift = (e - power) << 20;
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const double exact = x[i] * by;                             // a power of two
-        const float near = (float)exact;
-        const unsigned u = __float_as_uint(near);
-        const double back = (double)near;
-        // towards zero, then odd
-        const unsigned odd = (__builtin_fabs(back) > __builtin_fabs(exact) ? u - 1 : u) | 1;
-        y[i] = __uint_as_float(back == exact ? u : odd);
+        const uint64_t u = __builtin_bit_cast(uint64_t, x[i]);
+        // the exponent in units of the scale, not below 2^-23, which is a zero; then float32's bias
+        const int hi = max((int)((unsigned)(u >> 32) & kMagnitude) - shift, 1000 << 20);
+        const unsigned near = ((unsigned)hi << 3) - (896u << 23);
+        y[i] = __uint_as_float((near | min((unsigned)u, 1u)) | ((unsigned)(u >> 32) & ~kMagnitude));
     }
     unsigned w = 0;
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], 1.0f, 0);
@@ -88,10 +96,11 @@ __device__ __forceinline__ unsigned encode(const double (&x)[8], unsigned& scale
 }
 
 // ------------------------------------------------------------------------------------------------
-// Bound by memory where there are many tokens, and one token by the latency of its chain (length -> table entry -> store).  A workgroup, or a wave of
-// it (THREADS), takes a token.  A lane takes 8 elements, so that four lanes hold a block and a scale is two exchanges between neighbours; the elements that
-// turn with them are another lane's, and are read a second time, from the nearest cache.  Of the same place in every kHeads-th head, with that
-// place's cosines and sines in registers.
+// Many tokens are bound by what a lane computes beside its loads: of 30000 at 64 and 8 heads of 128 with the transform (1.26 GB: 272 us, 4.6 TB/s) the vector units are
+// busy most of the time, a key's or value's block in 64 bits with some 330 instructions a wave, a query's with 100.  One token is bound by the latency of its
+// chain (length -> table entry -> store).  A workgroup, or a wave of it (THREADS), takes a token.  A lane takes 8 elements, so that four lanes hold a block
+// and a scale is two exchanges between neighbours; the elements that turn with them are another lane's, and are read a second time, from the nearest
+// cache.  Of the same place in every kHeads-th head, with that place's cosines and sines in registers.
 
 struct Append4Args {
     Batch batch;
@@ -104,15 +113,26 @@ struct Append4Args {
     Turning turn;
 };
 
+// Eight elements as they stand in memory.
+template <class T> struct Eight { u32x4 w[sizeof(T) / 2]; };
 template <class T>
-__device__ __forceinline__ void load8(float (&f)[8], const unsigned char* p) {
-    if constexpr (sizeof(T) == 2) load16<T>(f, p);
-    else {
-        const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 16);
+__device__ __forceinline__ Eight<T> read8(const unsigned char* p) {
+    Eight<T> x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { f[i] = lo[i]; f[4 + i] = hi[i]; }
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) x.w[i] = reinterpret_cast<const u32x4*>(p)[i];
+    return x;
+}
+template <class T>
+__device__ __forceinline__ void widen(const Eight<T>& x, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const Vec16<T> v = __builtin_bit_cast(Vec16<T>, x.w[i]);
+#pragma unroll
+        for (int e = 0; e < Vec16<T>::n; ++e) f[i * Vec16<T>::n + e] = (float)v.e[e];
     }
 }
+template <class T>
+__device__ __forceinline__ void load8(float (&f)[8], const unsigned char* p) { widen<T>(read8<T>(p), f); }
 template <class T>
 __device__ __forceinline__ void store8(unsigned char* p, const float (&f)[8]) {
     if constexpr (sizeof(T) == 2) store16<T>(p, f);
@@ -124,7 +144,7 @@ __device__ __forceinline__ void store8(unsigned char* p, const float (&f)[8]) {
 
 template <class T, int D, int THREADS>
 __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
-    constexpr int kVectors = D / 8, kOfWave = 64 / kVectors, kHeads = kOfWave * (THREADS / 64), kSize = sizeof(T);
+    constexpr int kVectors = D / 8, kOfWave = 64 / kVectors, kHeads = kOfWave * (THREADS / 64), kSize = sizeof(T), kUnroll = sizeof(T) == 2 ? 4 : 2;
     const int lane = threadIdx.x & 63, vector = lane % kVectors, first = (threadIdx.x % THREADS >> 6) * kOfWave + lane / kVectors;
     const int t = THREADS == 256 ? block_of() : __builtin_amdgcn_readfirstlane(block_of() * (256 / THREADS) + threadIdx.x / THREADS);
     if (t >= a.batch.T) return;
@@ -166,57 +186,88 @@ __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
         }
     }
     // the eight elements and their partners
-    auto load = [&](const unsigned char* from, float (&x)[8], float (&y)[8]) {
-        load8<T>(x, from + e0 * kSize);
-        if (!turn) return;
-        if (a.turn.interleaved) {
+    const bool across = turn && !a.turn.interleaved;
+    struct Both { Eight<T> x, y; };
+    auto read = [&](const unsigned char* from) {
+        Both r;
+        r.x = r.y = read8<T>(from + e0 * kSize);
+        if (across) r.y = read8<T>(from + partner * kSize);
+        return r;
+    };
+    auto widen_both = [&](const Both& r, float (&x)[8], float (&y)[8]) {
+        widen<T>(r.x, x);
+        widen<T>(r.y, y);
+        if (turn && a.turn.interleaved)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
-        } else load8<T>(y, from + partner * kSize);
+            for (int i = 0; i < 8; i += 2) { const float u = y[i]; y[i] = y[i + 1]; y[i + 1] = u; }
     };
 
     if (a.q) {
-        for (int h = first; h < a.q_heads; h += kHeads) {
-            float x[8], y[8];
-            if (b >= 0 && known) {
-                load(a.q + t * a.q_ts + h * a.q_hs, x, y);
-                if (turn)
+        unsigned char* to = a.q_out + t * a.qo_ts + e0 * kSize;
+        if (b >= 0 && known) {
+            if (a.transform && turn)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = x[i] * c[i] + y[i] * s[i];
-                if (a.transform) {
-                    transform32(x);
+                for (int i = 0; i < 8; ++i) { c[i] *= 0.125f; s[i] *= 0.125f; }
+            const unsigned char* from = a.q + t * a.q_ts;
+            const int rounds = ceil_div(a.q_heads, kHeads);
+            for (int r0 = 0; r0 < rounds; r0 += kUnroll) {
+                Both raw[kUnroll];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] *= 0.125f;
+                for (int i = 0; i < kUnroll; ++i)
+                    if (r0 + i < rounds) raw[i] = read(from + min(first + (r0 + i) * kHeads, a.q_heads - 1) * a.q_hs);
+#pragma unroll
+                for (int i = 0; i < kUnroll; ++i) {
+                    if (r0 + i >= rounds) break;
+                    float x[8], y[8];
+                    widen_both(raw[i], x, y);
+                    if (turn) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = x[e] * c[e] + y[e] * s[e];
+                    } else if (a.transform) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] *= 0.125f;
+                    }
+                    if (a.transform) transform32(x);
+                    const int h = first + (r0 + i) * kHeads;
+                    if (h < a.q_heads) store8<T>(to + h * a.qo_hs, x);
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = b >= 0 ? __builtin_nanf("") : 0.0f;
             }
-            store8<T>(a.q_out + t * a.qo_ts + h * a.qo_hs + e0 * kSize, x);
+            if (a.transform && turn)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { c[i] *= 8.0f; s[i] *= 8.0f; }
+        } else {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = b >= 0 ? __builtin_nanf("") : 0.0f;
+            for (int h = first; h < a.q_heads; h += kHeads) store8<T>(to + h * a.qo_hs, x);
         }
     }
     if (!there && !a.k_out) return;
-    for (int n = first; n < 2 * a.heads; n += kHeads) {             // keys, then values
-        const bool key = n < a.heads;
-        const int h = key ? n : n - a.heads;
+    const int rounds = ceil_div(2 * a.heads, kHeads);
+    for (int r = 0; r < rounds; ++r) {                              // keys, then values
+        const int n = first + r * kHeads, at = min(n, 2 * a.heads - 1);
+        const bool key = at < a.heads;
+        const int h = key ? at : at - a.heads;
         unsigned codes = 0, scale = b >= 0 ? 255 : 127;             // of a token that is not stored: NaN; of padding: zero
         if (there) {
             float x[8], y[8];
             double z[8];
-            if (key) load(a.kn + t * a.k_ts + h * a.k_hs, x, y);
-            else load8<T>(x, a.vn + t * a.v_ts + h * a.v_hs + e0 * kSize);
+            widen_both(read(key ? a.kn + t * a.k_ts + h * a.k_hs : a.vn + t * a.v_ts + h * a.v_hs), x, y);
+            if (turn && key) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = key && turn ? (double)x[i] * c[i] + (double)y[i] * s[i] : (double)x[i];
-            if (a.transform) {
-                transform32(z);
+                for (int i = 0; i < 8; ++i) z[i] = (double)x[i] * c[i] + (double)y[i] * s[i];
+            } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) z[i] *= 0.25;
+                for (int i = 0; i < 8; ++i) z[i] = (double)x[i];
             }
-            codes = encode(z, scale);
-            *reinterpret_cast<unsigned*>((key ? a.k : a.v) + codes_at + h * a.head_stride + vector * 4) = codes;
-            if ((vector & 3) == 0) (key ? a.ks : a.vs)[scales_at + h * a.s_head_stride + vector / 4] = (unsigned char)scale;
+            if (a.transform) transform32(z);
+            codes = encode(z, a.transform ? -2 : 0, scale);
+            if (n < 2 * a.heads) {
+                *reinterpret_cast<unsigned*>((key ? a.k : a.v) + codes_at + h * a.head_stride + vector * 4) = codes;
+                if ((vector & 3) == 0) (key ? a.ks : a.vs)[scales_at + h * a.s_head_stride + vector / 4] = (unsigned char)scale;
+            }
         }
-        if (a.k_out) {
+        if (a.k_out && n < 2 * a.heads) {
             const bf16x8 v = decode(codes, scale_of(scale));
             float x[8];
 #pragma unroll

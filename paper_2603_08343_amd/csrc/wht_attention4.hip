@@ -47,8 +47,11 @@ static Turning turning(const float* rope, int64_t rope_rows, int32_t rotary, int
     return t;
 }
 
-// Vectors of 8 elements of a token's queries, keys and values from which on a workgroup takes it, not a wave.
-constexpr int kWideToken4 = 512;
+// A wave takes a token where there are enough of them to fill the chip, or where it has few vectors of 8 elements of its queries, keys and values; a workgroup
+// where few tokens have many, which is sooner done.  Workgroup / wave, in us: 32 and 8 x 128 (768 vectors) 256 tokens 7.1 / 12.3, 1024 11.7 / 16.4, 4096 27.7 / 26.9,
+// 16384 118 / 103; 16 x 96 (576) 256 7.4 / 13.2, 1024 13.0 / 16.5, 4096 31.9 / 29.7; 12 x 64 (288) 256 7.0 / 8.5, 1024 9.1 / 9.3, 4096 23.2 / 16.6;
+// 16 and 4 x 64 (192) 256 7.1 / 6.9, 1024 8.7 / 7.2.
+constexpr int kManyTokens4 = 2048, kWideToken4 = 256;
 
 static int append4(const wht_attention_rows_t* q, const wht_attention_rows_t* k, const wht_attention_rows_t* v, const wht_attention_rows_t* q_out,
                    const wht_attention_rows_t* k_out, const wht_attention_rows_t* v_out, int64_t T, int32_t q_heads, const wht_attention_cache4_t* c,
@@ -82,7 +85,7 @@ static int append4(const wht_attention_rows_t* q, const wht_attention_rows_t* k,
         using E = decltype(t);
         constexpr int D = decltype(d)::value;
         const int vectors = (int)((a.q ? q_heads : 0) + 2 * c->heads) * (D / 8);
-        if (vectors < kWideToken4) hipLaunchKernelGGL((append4_kernel<E, D, 64>), grid_of(ceil_div64(T, 4)), dim3(256), 0, stream, a);
+        if (T >= kManyTokens4 || vectors < kWideToken4) hipLaunchKernelGGL((append4_kernel<E, D, 64>), grid_of(ceil_div64(T, 4)), dim3(256), 0, stream, a);
         else hipLaunchKernelGGL((append4_kernel<E, D, 256>), grid_of(T), dim3(256), 0, stream, a);
         return launched();
     });
