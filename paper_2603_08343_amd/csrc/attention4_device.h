@@ -350,6 +350,29 @@ struct Few4 {
             }
         }
     }
+    // Queries, what they see, and empty sums of the rows of a sequence and a key head.
+    static __device__ __forceinline__ void begin(const AttentionArgs& a, const Sequence& s, int head, int rows, bf16x8 (&q)[TILES][kTermsOf][kWords], int (&limit)[TILES],
+                                                 int (&whole)[TILES], State (&st)[TILES]) {
+        const int c = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            const int row = i * kSmallTile + c, token = row / a.G, qh = head * a.G + row % a.G;
+            limit[i] = min(max(s.length - s.queries + token + 1, 0), s.length);
+            whole[i] = a.prefix;
+            const unsigned char* at = a.q + (s.first + token) * a.q_ts + qh * a.q_hs + g * kElements * sizeof(T);
+#pragma unroll
+            for (int e = 0; e < kWords; ++e) {
+                bf16x8 x[kTermsOf];
+                load_terms<T, kTermsOf>(at + e * 8 * sizeof(T), row < rows, x);
+#pragma unroll
+                for (int k = 0; k < kTermsOf; ++k) q[i][k][e] = x[k];
+            }
+            st[i].top = st[i].most = WHT_NEG_INF;
+            st[i].base = st[i].l = 0.0f;
+#pragma unroll
+            for (int d = 0; d < kBlocks; ++d) st[i].o[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
 };
 
 template <class T, int D, int TILES>
@@ -410,24 +433,7 @@ __device__ __forceinline__ void few_rows4(const Attention4Args& args, int block,
         bf16x8 q[TILES][F::kTermsOf][F::kWords];
         typename F::State st[TILES];
         int limit[TILES], whole[TILES];
-#pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-            const int row = i * kSmallTile + c, token = row / a.G, qh = head * a.G + row % a.G;
-            limit[i] = min(max(s.length - s.queries + token + 1, 0), s.length);
-            whole[i] = a.prefix;
-            const unsigned char* at = a.q + (s.first + token) * a.q_ts + qh * a.q_hs + g * F::kElements * sizeof(T);
-#pragma unroll
-            for (int e = 0; e < F::kWords; ++e) {
-                bf16x8 x[F::kTermsOf];
-                load_terms<T, F::kTermsOf>(at + e * 8 * sizeof(T), row < rows, x);
-#pragma unroll
-                for (int k = 0; k < F::kTermsOf; ++k) q[i][k][e] = x[k];
-            }
-            st[i].top = st[i].most = WHT_NEG_INF;
-            st[i].base = st[i].l = 0.0f;
-#pragma unroll
-            for (int d = 0; d < F::kBlocks; ++d) st[i].o[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        }
+        F::begin(a, s, head, rows, q, limit, whole, st);
 #pragma unroll 1
         for (int part = FRONT ? 1 : 0; part < 2; ++part) {          // the prefix, the sequence
             const int lo = part ? max(n0 - front, 0) : n0, hi = part ? n1 - front : min(n1, front);
@@ -447,6 +453,88 @@ __device__ __forceinline__ void few_rows4(const Attention4Args& args, int block,
             for (int d = 0; d < F::kBlocks; ++d) *reinterpret_cast<f32x4*>(a.part + at * D + d * 16 + g * 4) = st[i].o[d];
         }
         u += n1 - n0;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// A sequence's rows of a key head whole, by a workgroup, whose waves join their shares in LDS: one launch where the line and its join are two, for calls so
+// small that those are most of their time.  The waves of the line would be no more, or hardly.
+
+template <class T, int TILES> constexpr int kWholeWaves = sizeof(T) == 4 && TILES == 2 ? 4 : 8;
+
+template <class T, int D, int TILES>
+struct WholeShared {
+    static constexpr int kRows = TILES * kSmallTile, kWaves = kWholeWaves<T, TILES>;
+    union {
+        __align__(256) unsigned char buf[kWaves * Few4<T, D, TILES>::kWaveBytes];
+        float o[kWaves][kRows][D];
+    };
+    typename Few4<T, D, TILES>::Odd odd[kWaves];
+    float top[kWaves][kRows], l[kWaves][kRows];
+};
+
+template <class T, int D, int TILES, bool MULTI, bool NARROW>
+__global__ __launch_bounds__((64 * kWholeWaves<T, TILES>)) void whole_rows4_kernel(Attention4Args args) {
+    using F = Few4<T, D, TILES>;
+    using S = WholeShared<T, D, TILES>;
+    __shared__ S shared;
+    const AttentionArgs& a = args.base;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int b = blockIdx.x / a.heads, head = blockIdx.x - b * a.heads;
+    if ((a.batch.q_starts || a.batch.T > a.batch.B) && threadIdx.x < 256)         // rows of no sequence, and past max_q
+        for (int die = blockIdx.x; die < kDies; die += gridDim.x) fill_rows<T, D>(a, die);
+    const Sequence s = sequence(a.batch, b);
+    if (s.queries == 0) return;
+    const int rows = min(min(s.queries, a.max_q) * a.G, S::kRows);
+    const int front = a.use_prefix ? ceil_div(a.prefix, kBlockKeys) : 0;
+    const int all_see = min(max(s.length - s.queries + 1, 0), s.length);
+    const int keys = min(max(s.length - s.queries + min(s.queries, a.max_q), 0), s.length);
+    const int n = front + ceil_div(keys, kBlockKeys), per = ceil_div(n, S::kWaves), n0 = min(n, wave * per), n1 = min(n, n0 + per);
+    bf16x8 q[TILES][F::kTermsOf][F::kWords];
+    typename F::State st[TILES];
+    int limit[TILES], whole[TILES];
+    F::begin(a, s, head, rows, q, limit, whole, st);
+    const unsigned buf = __builtin_amdgcn_readfirstlane(lds_address(shared.buf)) + wave * F::kWaveBytes;
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {                          // the prefix, the sequence
+        const int lo = part ? max(n0 - front, 0) : n0, hi = part ? n1 - front : min(n1, front);
+        if (lo >= hi) continue;
+        const int* table = part ? a.batch.table + b * a.batch.table_stride : a.prefix_table;
+        F::template run<MULTI, NARROW, false>(args, table, lo, hi, part ? keys : a.prefix, part ? limit : whole, part ? all_see : a.prefix, head, buf, q, shared.odd[wave], st);
+    }
+    workgroup_barrier();                                            // the shares lie where values did
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+        const int row = i * kSmallTile + c;
+        st[i].l += __shfl_xor(st[i].l, 16);
+        st[i].l += __shfl_xor(st[i].l, 32);
+        if (g == 0) { shared.top[wave][row] = st[i].top * a.scale; shared.l[wave][row] = st[i].l; }
+#pragma unroll
+        for (int d = 0; d < F::kBlocks; ++d) *reinterpret_cast<f32x4*>(&shared.o[wave][row][d * 16 + g * 4]) = st[i].o[d];
+    }
+    __syncthreads();
+    // four outputs to a thread; a wave's rows are whole, and so are the eight threads of 32 outputs
+    constexpr int kLanes = D / 4, kRowsOfWave = 64 / kLanes;
+    for (int row0 = wave * kRowsOfWave; row0 < rows; row0 += S::kWaves * kRowsOfWave) {
+        const int row = min(row0 + lane / kLanes, S::kRows - 1), col = lane % kLanes * 4;
+        float m = WHT_NEG_INF, l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < S::kWaves; ++w) m = fmaxf(m, shared.top[w][row]);
+        const float base = m == WHT_NEG_INF ? 0.0f : m;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < S::kWaves; ++w) {
+            const float f = __builtin_amdgcn_exp2f(shared.top[w][row] - base);
+            l += shared.l[w][row] * f;
+            o += f * *reinterpret_cast<const f32x4*>(&shared.o[w][row][col]);
+        }
+        o *= l == 0.0f ? 0.0f : 1.0f / l;
+        if (args.transform) o = transform_outputs(o);
+        if (row0 + lane / kLanes >= rows || lane >= kRowsOfWave * kLanes) continue;
+        const int token = row / a.G, qh = head * a.G + row % a.G;
+        const int64_t t = s.first + token;
+        store4<T>(a.out + t * a.out_ts + qh * a.out_hs + col * sizeof(T), o);
+        if (a.lse && col == 0) a.lse[t * a.q_heads + qh] = l == 0.0f ? WHT_NEG_INF : (m + __builtin_amdgcn_logf(l)) * kLn2;
     }
 }
 

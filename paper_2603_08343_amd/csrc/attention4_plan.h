@@ -17,6 +17,23 @@ inline bool streams4(int32_t B, int32_t heads, int32_t head_dim, int64_t max_len
     return gang_log2 == 0 && ((double)B * max_length + prefix) * heads * (head_dim / 2 + head_dim / 32) * 2 >= 96e6;
 }
 
+// Whether a sequence's rows of a key head are taken whole, by a workgroup, in one launch: where all of these have a place at the same time, and the longest that
+// lengths can be is short, the shorter the fewer they are.  On the line with its join / whole, in us, sequences of 3/4 of that length and more, 32 and 8 x 128: 8 items
+// of up to 128 keys 9.7 / 6.9, 512 10.4 / 8.4, 1024 10.4 / 10.7; 32 of 512 10.9 / 8.8, 1024 11.1 / 11.1, 2048 13.0 / 15.5; 128 of 1024 14.1 / 11.5, 2048 17.0 / 16.2,
+// 4096 21.2 / 24.3; 256 of 512 15.2 / 9.3, 2048 22.4 / 17.5, 4096 32.3 / 26.7.  512 items have two rounds (512 keys 19.5 / 18.0), but of 64 wide, two to a
+// compute unit (512 keys 17.1 / 9.5, 2048 24.7 / 18.4).  The line deals ragged lengths out evenly, which a workgroup an item does not: lengths from 1 to the
+// longest take it the time of half of that, so that the rule stops where those break even.
+inline bool takes_whole(int64_t items, int32_t head_dim, int64_t keys) {
+    return items > 0 && items <= (head_dim == 64 ? 512 : 256) && keys <= 512 + 8 * (items < 256 ? items : 256);
+}
+struct AttentionPlan4 : AttentionPlan { bool whole; };
+inline AttentionPlan4 plan_attention4(int64_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t head_dim, int32_t max_q, int64_t max_length, int64_t prefix) {
+    AttentionPlan4 p{plan_attention(T, B, q_heads, heads, head_dim, max_q, max_length, prefix, kMostWorkers4), false};
+    p.whole = p.own_few && !p.front && takes_whole((int64_t)B * heads, head_dim, max_length + prefix);
+    if (p.whole) { p.combine = false; p.bytes = 0; }
+    return p;
+}
+
 constexpr int kMaxPairs = WHT_ROTARY_MAX_HEAD / 2;
 
 // rotary > 0: whether every pair's axis is one of those that positions have.

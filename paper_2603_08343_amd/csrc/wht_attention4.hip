@@ -110,7 +110,7 @@ static int rotate(const wht_attention_rows_t* x, const wht_attention_rows_t* out
 
 static int paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out, float* lse, int64_t T, int32_t q_heads,
                   const wht_attention_cache4_t* c, const wht_attention_batch_t* b, const int32_t* prefix_table, int64_t prefix, int32_t max_q,
-                  int64_t max_length, float scale, int32_t transform, int32_t dtype, const AttentionPlan& p, unsigned char* ws, hipStream_t stream) {
+                  int64_t max_length, float scale, int32_t transform, int32_t dtype, const AttentionPlan4& p, unsigned char* ws, hipStream_t stream) {
     const int64_t size = dtype == WHT_DTYPE_F32 ? 4 : 2;
     const int64_t table_keys = (int64_t)b->width * c->page_size;
     Attention4Args args{};
@@ -156,6 +156,21 @@ static int paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out
         using E = decltype(t);
         constexpr int D = decltype(d)::value;
         const dim3 grid((unsigned)(front_blocks + own_blocks)), block(256);
+        if (p.whole) {
+            with_flags([&](auto two, auto multi) {
+                constexpr int kTiles = decltype(two)::value ? 2 : 1;
+                constexpr bool kMulti = decltype(multi)::value;
+                const dim3 items((unsigned)(b->B * c->heads)), threads(64 * kWholeWaves<E, kTiles>);
+                if constexpr (kTiles == 2 && kMulti) {
+                    if (a.page_shift < 4) {
+                        hipLaunchKernelGGL((whole_rows4_kernel<E, D, kTiles, kMulti, true>), items, threads, 0, stream, args);
+                        return;
+                    }
+                }
+                hipLaunchKernelGGL((whole_rows4_kernel<E, D, kTiles, kMulti, false>), items, threads, 0, stream, args);
+            }, two_tiles, a.page_shift < 4 || max_q > 1);
+            return launched();
+        }
         if (!p.own_few) hipLaunchKernelGGL((many_rows4_kernel<E, D>), grid, block, 0, stream, args);
         else
             with_flags([&](auto two, auto multi, auto front, auto past) {
@@ -238,7 +253,7 @@ size_t wht_attention4_workspace_bytes(int64_t T, int32_t B, int32_t q_heads, int
                                       int64_t prefix_length, int32_t dtype) {
     using namespace wht;
     if (check_sizes(T, B, q_heads, heads, head_dim, max_q, max_length, prefix_length, dtype) != WHT_OK || T == 0) return 0;
-    return plan_attention(T, B, q_heads, heads, head_dim, max_q, max_length, prefix_length, kMostWorkers4).bytes;
+    return plan_attention4(T, B, q_heads, heads, head_dim, max_q, max_length, prefix_length).bytes;
 }
 
 int wht_attention_paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out, float* lse, int64_t T, int32_t q_heads,
@@ -248,7 +263,7 @@ int wht_attention_paged4(const wht_attention_rows_t* q, const wht_attention_rows
     using namespace wht;
     if (int rc = check_paged4(q, out, lse, T, q_heads, cache, batch, prefix_table, prefix_length, max_q, max_length, scale, dtype)) return rc;
     if (T == 0) return WHT_OK;
-    const AttentionPlan p = plan_attention(T, batch->B, q_heads, cache->heads, cache->head_dim, max_q, max_length, prefix_length, kMostWorkers4);
+    const AttentionPlan4 p = plan_attention4(T, batch->B, q_heads, cache->heads, cache->head_dim, max_q, max_length, prefix_length);
     if (p.bytes > 0 && (!workspace || workspace_bytes < p.bytes)) return WHT_ERR_WORKSPACE;
     if (((uintptr_t)workspace & 15u) != 0) return WHT_ERR_MISALIGNED;
     return paged4(q, out, lse, T, q_heads, cache, batch, prefix_table, prefix_length, max_q, max_length, scale, transform, dtype, p,

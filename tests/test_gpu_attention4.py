@@ -179,15 +179,20 @@ ATTENDS = [  # B, queries, lengths, heads, page, prefix, order, transformed, dty
 ]
 
 
+# Few rows are taken item by item where the longest that lengths can be is short, and on a line of all items' blocks else: the caller's max_length decides.
+LONG = 1 << 20
+
+
 @pytest.mark.parametrize("case", ATTENDS, ids=str)
 def test_attend(case):
     B, queries, lengths, heads, page, prefix, order, transformed, dtype = case
     c = check.make4(B, queries, lengths, heads, page, prefix, dtype, order)
     out, lse, tol, tol_lse = check.attend4(c, transformed)
-    got, got_lse = call_paged(c, transform=transformed, want_lse=True)
-    attention_check.same(got, out, tol, "out")
-    attention_check.same(got_lse, lse, tol_lse, "lse")
-    assert torch.equal(call_paged(c, transform=transformed), got)
+    for max_length in (c["max_length"], LONG):
+        got, got_lse = call_paged(c, transform=transformed, want_lse=True, max_length=max_length)
+        attention_check.same(got, out, tol, "out")
+        attention_check.same(got_lse, lse, tol_lse, "lse")
+        assert torch.equal(call_paged(c, transform=transformed, max_length=max_length), got)
 
 
 @pytest.mark.parametrize("case", [c for c in ATTENDS if sum(c[1]) > 1][::2], ids=str)
@@ -210,9 +215,23 @@ def test_what_a_row_does_not_see_takes_no_part(case):
             c["v_scales"][int(table[b, p // page]), 0, p % page, 1] = 253
             c["k_scales"][int(table[b, p // page]), heads[1] - 1, p % page, 0] = 254
     out, lse, tol, tol_lse = check.attend4(c, transformed)
-    got, got_lse = call_paged(c, transform=transformed, want_lse=True)
+    for max_length in (c["max_length"], LONG):
+        got, got_lse = call_paged(c, transform=transformed, want_lse=True, max_length=max_length)
+        attention_check.same(got, out, tol, "out")
+        attention_check.same(got_lse, lse, tol_lse, "lse")
+
+
+@pytest.mark.parametrize("queries,heads", [([1, 1, 1], (8, 2, 128)), ([3, 1, 2], (12, 4, 96)), ([5, 2, 1], (20, 4, 64))], ids=str)
+def test_codes_past_the_caches(queries, heads):
+    """A table that can hold enough for the rule that reads codes past the caches."""
+    c = check.make4(3, queries, [300, 77, 150], heads, 16, 40)
+    wide = torch.full((3, LONG // 16), -1, dtype=torch.int32, device=DEV)
+    wide[:, :c["table"].shape[1]] = c["table"]
+    out, lse, tol, tol_lse = check.attend4(c, True)
+    got, got_lse = call_paged({**c, "table": wide}, want_lse=True, max_length=LONG)
     attention_check.same(got, out, tol, "out")
     attention_check.same(got_lse, lse, tol_lse, "lse")
+    assert torch.equal(got, call_paged(c, max_length=LONG))
 
 
 @pytest.mark.parametrize("queries,heads", [([1, 1], (4, 2, 64)), ([6, 3], (8, 2, 128)), ([60, 40], (4, 2, 96))], ids=str)
@@ -225,9 +244,10 @@ def test_bad_pages_lengths_and_rows(queries, heads, dtype):
     c["q"] = torch.cat((c["q"], torch.full_like(c["q"][:3], math.nan)))
     limit = max(queries) - 1 if max(queries) > 1 else None
     out, lse, tol, tol_lse = check.attend4(c, True, limit=limit)
-    got, got_lse = call_paged(c, max_q=limit or 1, want_lse=True)
-    attention_check.same(got, out, tol, "out")
-    attention_check.same(got_lse, lse, tol_lse, "lse")
+    for max_length in (c["max_length"], LONG):
+        got, got_lse = call_paged(c, max_q=limit or 1, want_lse=True, max_length=max_length)
+        attention_check.same(got, out, tol, "out")
+        attention_check.same(got_lse, lse, tol_lse, "lse")
 
 
 @pytest.mark.parametrize("queries,heads", [([1, 1], (4, 2, 64)), ([3, 2], (8, 2, 128)), ([40, 9], (4, 2, 96))], ids=str)
@@ -247,14 +267,15 @@ def test_scales_of_any_size(byte, queries, heads):
     attention_check.same(got, out, tol, "out")
 
 
+@pytest.mark.parametrize("max_length", [200, LONG])
 @pytest.mark.parametrize("peak", [60.0, 4e4])
 @pytest.mark.parametrize("queries", [[1, 1], [40, 33]], ids=str)
-def test_large_scores(peak, queries):
+def test_large_scores(peak, queries, max_length):
     """Scores of hundreds and of 2^20: one key takes all the weight, or a few; the row's maximum is taken off exactly."""
     c = check.make4(2, queries, [200, 60], (4, 2, 64), 16, 40, F32)
     c["q"] *= peak
     out, lse, tol, tol_lse = check.attend4(c, True)
-    got, got_lse = call_paged(c, want_lse=True)
+    got, got_lse = call_paged(c, want_lse=True, max_length=max_length)
     attention_check.same(got, out, tol, "out")
     attention_check.same(got_lse, lse, tol_lse, "lse")
 
@@ -280,40 +301,43 @@ def test_a_long_cache_past_32_bits():
     assert all(torch.equal(twin[n], small[n]) for n in twin)
 
 
-def test_other_streams_and_a_workspace_of_the_callers():
+@pytest.mark.parametrize("max_length", [100, LONG])
+def test_other_streams_and_a_workspace_of_the_callers(max_length):
     c = check.make4(3, [1, 1, 1], [100, 20, 60], (8, 2, 128), 16, 30)
-    want = call_paged(c)
+    want = call_paged(c, max_length=max_length)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     out, lse = torch.empty_like(c["q"]), torch.empty(3, 8, device=DEV)
-    need = wht.wht_attention4_workspace_bytes(3, 3, 8, 2, 128, 1, 100, 30, 1)
-    workspace = torch.full((need,), 255, dtype=torch.uint8, device=DEV)
-    got = call_paged(c, out=out, lse=lse, workspace=workspace, stream=side)
+    need = wht.wht_attention4_workspace_bytes(3, 3, 8, 2, 128, 1, max_length, 30, 1)
+    assert (need > 0) == (max_length == LONG)
+    workspace = torch.full((max(need, 16),), 255, dtype=torch.uint8, device=DEV)
+    got = call_paged(c, out=out, lse=lse, workspace=workspace, stream=side, max_length=max_length)
     side.synchronize()
     assert got[0] is out and got[1] is lse and torch.equal(out, want)
     with torch.cuda.stream(side):
-        again = call_paged(c)
+        again = call_paged(c, max_length=max_length)
     side.synchronize()
     assert torch.equal(again, want)
-    with pytest.raises(attention4.WhtAttention4Error):
-        call_paged(c, workspace=workspace[:need - 16])
+    if need:
+        with pytest.raises(attention4.WhtAttention4Error):
+            call_paged(c, workspace=workspace[:need - 16], max_length=max_length)
 
 
-@pytest.mark.parametrize("queries", [[1, 1, 1], [40, 2, 5]], ids=str)
-def test_captured_steps_follow_the_arrays(queries):
+@pytest.mark.parametrize("queries,max_length", [([1, 1, 1], 80), ([1, 1, 1], LONG), ([40, 2, 5], 80)], ids=str)
+def test_captured_steps_follow_the_arrays(queries, max_length):
     """Append and attention in one graph, replayed with new inputs, lengths and eager work between; two graphs of one workspace in turn."""
     lengths = [50 + q for q in queries]
     c = check.make4(3, queries, lengths, (8, 2, 128), 16, 30)
     c["table"] = torch.arange(15, dtype=torch.int32, device=DEV).view(3, 5)
     rope = wht.wht_attention_rope_table(200, 128, device=DEV)
-    q0, need = c["q"].clone(), wht.wht_attention4_workspace_bytes(sum(queries), 3, 8, 2, 128, max(queries), 80, 30, 1)
+    q0, need = c["q"].clone(), wht.wht_attention4_workspace_bytes(sum(queries), 3, 8, 2, 128, max(queries), max_length, 30, 1)
     workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=DEV)
     out = [torch.empty_like(q0) for _ in range(2)]
 
     def step(i, ws):
         q = call_append(c, rope, position=30)
         return wht.wht_attention_paged4(q, c["k_pages"], c["v_pages"], c["k_scales"], c["v_scales"], c["table"], c["lengths"], q_starts=c["starts"],
-                                        prefix_table=c["prefix_table"], prefix_length=30, max_q=max(queries), max_length=80, out=out[i], workspace=ws)
+                                        prefix_table=c["prefix_table"], prefix_length=30, max_q=max(queries), max_length=max_length, out=out[i], workspace=ws)
 
     step(0, workspace)
     torch.cuda.synchronize()
@@ -363,6 +387,23 @@ def test_a_blocks_steps_together(dtype):
     stored = check.transform(check.decode(pages[1], pages[3]), 8)
     last = stored[int(table[0, (length - 1) // 16]), :, (length - 1) % 16]
     assert float((last - v[new - 1].cpu().double()).norm() / v[new - 1].cpu().double().norm()) < 0.25
+
+
+def test_rows_without_a_sequence_and_batches_without_one():
+    """More rows than sequences (padding), no sequence at all, sequences without new tokens: zeros, on either way of few rows."""
+    c = check.make4(2, [1, 1], [30, 20], (4, 2, 64), 16)
+    for max_length in (30, LONG):
+        for starts, live in (([0, 1, 2], [0, 1]), ([0, 0, 1], [0]), ([0, 0, 0], [])):
+            q = torch.cat((c["q"], torch.full_like(c["q"], 3.0)))
+            d = {**c, "q": q, "starts": torch.tensor(starts, dtype=torch.int32, device=DEV)}
+            out, lse, tol, tol_lse = check.attend4(d, True)
+            got, got_lse = call_paged(d, want_lse=True, max_length=max_length)
+            attention_check.same(got, out, tol)
+            attention_check.same(got_lse, lse, tol_lse)
+            assert not got[len(live):].any() and torch.isneginf(got_lse[len(live):]).all()
+        none = {**c, "table": c["table"][:0], "lengths": c["lengths"][:0], "starts": torch.zeros(1, dtype=torch.int32, device=DEV)}
+        got = call_paged(none, max_length=max_length)
+        assert got.shape == c["q"].shape and not got.any()
 
 
 def test_results_do_not_depend_on_the_way_the_call_is_marshalled(monkeypatch):
