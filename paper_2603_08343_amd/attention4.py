@@ -155,7 +155,7 @@ def wht_attention_append4(q, k, v, k_pages, v_pages, k_scales, v_scales, table, 
         if done is not None:
             if type(done) is int:
                 raise WhtAttention4Error(done, "wht_attention_append4")
-            return None if done == () else done
+            return None if type(done) is tuple and not done else done
     from . import rotary as _rotary
     torch = _torch()
     cache = _cache4(k_pages, v_pages, k_scales, v_scales, torch)

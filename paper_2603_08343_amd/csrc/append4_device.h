@@ -96,11 +96,12 @@ __device__ __forceinline__ unsigned encode(const double (&x)[8], int power, unsi
 }
 
 // ------------------------------------------------------------------------------------------------
-// Many tokens are bound by what a lane computes beside its loads: of 30000 at 64 and 8 heads of 128 with the transform (1.26 GB: 272 us, 4.6 TB/s) the vector units are
+// Many tokens are bound by what a lane computes beside its loads: of 30000 at 64 and 8 heads of 128 with the transform (1.26 GB: 280 us, 4.5 TB/s) the vector units are
 // busy most of the time, a key's or value's block in 64 bits with some 330 instructions a wave, a query's with 100.  One token is bound by the latency of its
-// chain (length -> table entry -> store).  A workgroup, or a wave of it (THREADS), takes a token.  A lane takes 8 elements, so that four lanes hold a block
-// and a scale is two exchanges between neighbours; the elements that turn with them are another lane's, and are read a second time, from the nearest
-// cache.  Of the same place in every kHeads-th head, with that place's cosines and sines in registers.
+// chain (length -> table entry -> store) and of its instructions (4.2 us; 5.0 with queries, keys and values by the same workgroup).  A workgroup, or a wave of it
+// (THREADS), takes a token.  A lane takes 8 elements, so that four lanes hold a block and a scale is two exchanges between neighbours; the elements that
+// turn with them are another lane's, and are read a second time, from the nearest cache.  Of the same place in every kHeads-th head, with that place's cosines
+// and sines in registers.
 
 struct Append4Args {
     Batch batch;
@@ -148,7 +149,36 @@ __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
     const int lane = threadIdx.x & 63, vector = lane % kVectors, first = (threadIdx.x % THREADS >> 6) * kOfWave + lane / kVectors;
     const int t = THREADS == 256 ? block_of() : __builtin_amdgcn_readfirstlane(block_of() * (256 / THREADS) + threadIdx.x / THREADS);
     if (t >= a.batch.T) return;
-    const int b = sequence_of(a.batch, t);
+    // This lane's eight elements, and the eight that turn with them.  A workgroup's first rounds are on their way before it is known where they go.
+    const int half = a.turn.rotary / 2, e0 = vector * 8;
+    const bool turns = e0 < a.turn.rotary, low = a.turn.interleaved || e0 < half, across = turns && !a.turn.interleaved;
+    const int partner = low ? e0 + half : e0 - half;
+    struct Both { Eight<T> x, y; };
+    auto read = [&](const unsigned char* from) {
+        Both r;
+        r.x = r.y = read8<T>(from + e0 * kSize);
+        if (across) r.y = read8<T>(from + partner * kSize);
+        return r;
+    };
+    const unsigned char* q_from = a.q + t * a.q_ts;
+    // where there are few tokens, queries are one workgroup's and keys and values another's
+    const bool apart = THREADS == 256 && gridDim.z == 2, does_q = a.q && (!apart || blockIdx.z == 0), does_kv = !apart || blockIdx.z == 1;
+    const int q_rounds = does_q ? ceil_div(a.q_heads, kHeads) : 0, rounds = ceil_div(2 * a.heads, kHeads);
+    auto read_q = [&](int round) { return read(q_from + min(first + round * kHeads, a.q_heads - 1) * a.q_hs); };
+    auto read_kv = [&](int round) {                                 // keys, then values
+        const int n = min(first + round * kHeads, 2 * a.heads - 1);
+        return read(n < a.heads ? a.kn + t * a.k_ts + n * a.k_hs : a.vn + t * a.v_ts + (n - a.heads) * a.v_hs);
+    };
+    Both raw[kUnroll], raw_kv;
+    if constexpr (THREADS == 256) {
+        if (does_kv) raw_kv = read_kv(0);
+#pragma unroll
+        for (int i = 0; i < kUnroll; ++i)
+            if (i < q_rounds) raw[i] = read_q(i);
+    }
+
+    const int b = sequence_of(a.batch, t);                          // by whole waves
+    if (lane >= kOfWave * kVectors) return;                         // 96 wide: the lanes are no multiple of the vectors
     bool there = false, known = true;
     int64_t codes_at = 0, scales_at = 0;
     Places p{};
@@ -166,12 +196,9 @@ __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
             scales_at = page * a.s_page_stride + slot * a.s_token_stride;
         }
     }
-    if (lane >= kOfWave * kVectors) return;                         // 96 wide: the lanes are no multiple of the vectors
 
-    // this lane's elements' partners, and the angles; an element's own angle turns it by +, its partner's way by -
-    const int half = a.turn.rotary / 2, e0 = vector * 8;
-    const bool turn = known && b >= 0 && e0 < a.turn.rotary, low = a.turn.interleaved || e0 < half;
-    const int partner = low ? e0 + half : e0 - half;
+    // the angles; an element's own turns it by +, its partner's way by -
+    const bool turn = known && b >= 0 && turns;
     float c[8], s[8];
     if (turn) {
         if (a.turn.interleaved) {
@@ -185,15 +212,6 @@ __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
             for (int i = 0; i < 8; ++i) s[i] = low ? -s[i] : s[i];
         }
     }
-    // the eight elements and their partners
-    const bool across = turn && !a.turn.interleaved;
-    struct Both { Eight<T> x, y; };
-    auto read = [&](const unsigned char* from) {
-        Both r;
-        r.x = r.y = read8<T>(from + e0 * kSize);
-        if (across) r.y = read8<T>(from + partner * kSize);
-        return r;
-    };
     auto widen_both = [&](const Both& r, float (&x)[8], float (&y)[8]) {
         widen<T>(r.x, x);
         widen<T>(r.y, y);
@@ -202,22 +220,20 @@ __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
             for (int i = 0; i < 8; i += 2) { const float u = y[i]; y[i] = y[i + 1]; y[i + 1] = u; }
     };
 
-    if (a.q) {
+    if (does_q) {
         unsigned char* to = a.q_out + t * a.qo_ts + e0 * kSize;
         if (b >= 0 && known) {
             if (a.transform && turn)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) { c[i] *= 0.125f; s[i] *= 0.125f; }
-            const unsigned char* from = a.q + t * a.q_ts;
-            const int rounds = ceil_div(a.q_heads, kHeads);
-            for (int r0 = 0; r0 < rounds; r0 += kUnroll) {
-                Both raw[kUnroll];
+            for (int r0 = 0; r0 < q_rounds; r0 += kUnroll) {
+                if (THREADS != 256 || r0 > 0)
 #pragma unroll
-                for (int i = 0; i < kUnroll; ++i)
-                    if (r0 + i < rounds) raw[i] = read(from + min(first + (r0 + i) * kHeads, a.q_heads - 1) * a.q_hs);
+                    for (int i = 0; i < kUnroll; ++i)
+                        if (r0 + i < q_rounds) raw[i] = read_q(r0 + i);
 #pragma unroll
                 for (int i = 0; i < kUnroll; ++i) {
-                    if (r0 + i >= rounds) break;
+                    if (r0 + i >= q_rounds) break;
                     float x[8], y[8];
                     widen_both(raw[i], x, y);
                     if (turn) {
@@ -242,9 +258,8 @@ __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
             for (int h = first; h < a.q_heads; h += kHeads) store8<T>(to + h * a.qo_hs, x);
         }
     }
-    if (!there && !a.k_out) return;
-    const int rounds = ceil_div(2 * a.heads, kHeads);
-    for (int r = 0; r < rounds; ++r) {                              // keys, then values
+    if (!does_kv || (!there && !a.k_out)) return;
+    for (int r = 0; r < rounds; ++r) {
         const int n = first + r * kHeads, at = min(n, 2 * a.heads - 1);
         const bool key = at < a.heads;
         const int h = key ? at : at - a.heads;
@@ -252,7 +267,8 @@ __global__ __launch_bounds__(256) void append4_kernel(Append4Args a) {
         if (there) {
             float x[8], y[8];
             double z[8];
-            widen_both(read(key ? a.kn + t * a.k_ts + h * a.k_hs : a.vn + t * a.v_ts + h * a.v_hs), x, y);
+            if (THREADS != 256 || r > 0) raw_kv = read_kv(r);
+            widen_both(raw_kv, x, y);
             if (turn && key) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = (double)x[i] * c[i] + (double)y[i] * s[i];

@@ -86,7 +86,7 @@ static int append4(const wht_attention_rows_t* q, const wht_attention_rows_t* k,
         constexpr int D = decltype(d)::value;
         const int vectors = (int)((a.q ? q_heads : 0) + 2 * c->heads) * (D / 8);
         if (T >= kManyTokens4 || vectors < kWideToken4) hipLaunchKernelGGL((append4_kernel<E, D, 64>), grid_of(ceil_div64(T, 4)), dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((append4_kernel<E, D, 256>), grid_of(T), dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((append4_kernel<E, D, 256>), dim3((unsigned)T, 1, a.q ? 2 : 1), dim3(256), 0, stream, a);
         return launched();
     });
 }
