@@ -36,11 +36,19 @@ __device__ __forceinline__ void load_terms(const unsigned char* p, bool there, b
         if (there) load8<T>(x, p);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
+            // an infinity or NaN is its first term, a finite number's is finite: what bfloat16's largest leaves of it is the second's
+            const bool finite = fabsf(x[i]) < __builtin_inff();
+            const float most = __uint_as_float(0x7f7f0000u);
             bf16 t[TERMS];
-            split<TERMS>(x[i], t);
-            // an infinity is its first term
+            t[0] = (bf16)(finite ? fminf(fmaxf(x[i], -most), most) : x[i]);
+            float rest = finite ? x[i] - (float)t[0] : 0.0f;
 #pragma unroll
-            for (int k = 0; k < TERMS; ++k) q[k][i] = k > 0 && !(fabsf(x[i]) < __builtin_inff()) ? (bf16)0.0f : t[k];
+            for (int k = 1; k < TERMS; ++k) {
+                t[k] = (bf16)rest;
+                rest -= (float)t[k];
+            }
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k) q[k][i] = t[k];
         }
     }
 }
@@ -171,7 +179,7 @@ struct Few4 {
         const AttentionArgs& a = args.base;
         const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, shift = a.page_shift;
         const unsigned char *kc = a.k + head * a.head_stride, *vc = a.v + head * a.head_stride, *ks = args.ks + head * args.s_head_stride, *vs = args.vs + head * args.s_head_stride;
-        const unsigned code_off = c * a.token_stride + g * (kElements / 2), scale_off = c * args.s_token_stride + scale_index(0);
+        const unsigned slot0 = NARROW ? c & 7 : c, code_off = slot0 * a.token_stride + g * (kElements / 2), scale_off = slot0 * args.s_token_stride + scale_index(0);
         const int last = min(n1 * kBlockKeys, keys);
         int key0 = n0 * kBlockKeys;
         while (key0 < last) {
@@ -204,7 +212,7 @@ struct Few4 {
                     for (int i = 0; i < 2; ++i) {
                         uint64_t more_codes, more_scales;
                         row_of(from + 16 * i + 8, more_codes, more_scales);
-                        const uint64_t at = c < 8 ? codes[i] : more_codes - 8 * a.token_stride, scale = c < 8 ? scales[i] : more_scales - 8 * args.s_token_stride;
+                        const uint64_t at = c < 8 ? codes[i] : more_codes, scale = c < 8 ? scales[i] : more_scales;
                         load<STREAM>(k, i, kc + at, ks + scale, code_off, scale_off);
                         load<STREAM>(v, i, vc + at, vs + scale, code_off, scale_off);
                     }

@@ -489,8 +489,9 @@ at::Tensor turned(const at::Tensor& x, const at::Tensor& rope, const at::Tensor&
 // torch.autograd.grad itself takes: 63 us as a Python Function, 42 here.
 // (named: the graph's nodes and torch's error messages show the type)
 struct WhtRotaryFunction : torch::autograd::Function<WhtRotaryFunction> {
-    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& rope, const at::Tensor& positions, const std::string& axes,
+    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& rope, const std::optional<at::Tensor>& given, const std::string& axes,
                               bool interleaved, bool inverse) {
+        const at::Tensor positions = given ? *given : at::Tensor();
         const at::Tensor y = turned(x, rope, positions, axes, interleaved, inverse);
         if (!y.defined()) throw Declined{};
         ctx->save_for_backward({rope, positions});                  // their versions are checked: angles that have changed since raise
@@ -509,7 +510,7 @@ struct WhtRotaryFunction : torch::autograd::Function<WhtRotaryFunction> {
         const bool ordinary = !modes_active() && Call::is_plain(dy) && (dy.scalar_type() == at::kFloat || dy.scalar_type() == at::kBFloat16) && guard.getDevice() == dy.device();
         if (ordinary && at::GradMode::is_enabled()) {               // a gradient of the gradient is asked for
             try {
-                out[0] = apply(dy, saved[0], saved[1], axes, interleaved, inverse);
+                out[0] = apply(dy, saved[0], saved[1].defined() ? std::optional<at::Tensor>(saved[1]) : std::nullopt, axes, interleaved, inverse);
                 return out;
             } catch (const Declined&) {
             }
@@ -557,7 +558,7 @@ PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (interleaved < 0) return nullptr;
     if (!c.ok) return none();
     const std::string axes = a.pair_axes ? std::string(reinterpret_cast<const char*>(a.pair_axes), a.rotary / 2) : std::string();
-    const at::Tensor positions = a.positions ? THPVariable_Unpack(args[2]) : at::Tensor();
+    const std::optional<at::Tensor> positions = a.positions ? std::optional<at::Tensor>(THPVariable_Unpack(args[2])) : std::nullopt;
     try {
         return THPVariable_Wrap(WhtRotaryFunction::apply(*x, THPVariable_Unpack(args[1]), positions, axes, interleaved != 0, false));
     } catch (const Declined&) {

@@ -176,6 +176,12 @@ ATTENDS = [  # B, queries, lengths, heads, page, prefix, order, transformed, dty
     (9, [2] * 9, [30] * 9, (24, 12, 96), 16, 2000, "head", True, B16),
     (8, [1] * 8, [50] * 8, (32, 32, 64), 16, 700, "head", True, B16),             # a front of few rows
     (20, [1] * 20, [300] * 20, (16, 16, 96), 16, 0, "token", True, B16),          # heads side by side
+    (2, [5, 1], [2, 7], (8, 2, 128), 16, 0, "head", True, B16),                   # more new tokens than the sequence has
+    (2, [50, 3], [20, 9], (4, 2, 64), 16, 0, "head", True, F32),
+    (1, [40], [700], (4, 1, 96), 16, 300, "head", True, B16),                     # a tile's keys in shares
+    (2, [45, 20], [900, 20], (4, 2, 128), 32, 0, "token", False, F32),
+    (3, [2, 4, 1], [60, 40, 90], (20, 4, 64), 8, 0, "head", True, B16),           # pages of 8
+    (2, [33, 40], [70, 41], (4, 2, 128), 8, 21, "head", True, B16),
 ]
 
 
@@ -235,10 +241,11 @@ def test_codes_past_the_caches(queries, heads):
 
 
 @pytest.mark.parametrize("queries,heads", [([1, 1], (4, 2, 64)), ([6, 3], (8, 2, 128)), ([60, 40], (4, 2, 96))], ids=str)
+@pytest.mark.parametrize("page", [8, 16])
 @pytest.mark.parametrize("dtype", [B16, F32], ids=str)
-def test_bad_pages_lengths_and_rows(queries, heads, dtype):
+def test_bad_pages_lengths_and_rows(queries, heads, dtype, page):
     """Page numbers outside the cache count as not there, on both sides; too small a max_q gives rows of NaN, padding rows zeros."""
-    c = check.make4(2, queries, [90, 70], heads, 16, 60, dtype)
+    c = check.make4(2, queries, [90, 70], heads, page, 60, dtype)
     c["table"][0, 1], c["table"][1, 2] = -1, 2 ** 31 - 1
     c["prefix_table"][1] = c["k_pages"].shape[0]
     c["q"] = torch.cat((c["q"], torch.full_like(c["q"][:3], math.nan)))
@@ -278,6 +285,24 @@ def test_large_scores(peak, queries, max_length):
     got, got_lse = call_paged(c, want_lse=True, max_length=max_length)
     attention_check.same(got, out, tol, "out")
     attention_check.same(got_lse, lse, tol_lse, "lse")
+
+
+@pytest.mark.parametrize("queries", [[1, 1], [40, 33]], ids=str)
+def test_queries_that_are_not_finite_or_hardly(queries):
+    """A float32 query past bfloat16's largest number is finite, and its scores with small keys are; NaN and infinity stay in their own rows."""
+    c = check.make4(2, queries, [200, 60], (4, 2, 64), 16, 0, F32)
+    c["k_scales"].sub_(110)
+    c["q"][:] = c["q"] * 1e20
+    c["q"][0, 0, 0] = torch.finfo(F32).max
+    out, lse, tol, tol_lse = check.attend4(c, True)
+    got, got_lse = call_paged(c, want_lse=True, scale=0.125)
+    attention_check.same(got, out, tol, "out")
+    attention_check.same(got_lse, lse, tol_lse, "lse")
+    c["q"][0, 1, 5], c["q"][0, 2, 7] = math.nan, math.inf
+    bad = call_paged(c, scale=0.125)
+    same = torch.ones(bad.shape[:2], dtype=torch.bool)
+    same[0, 1:3] = False
+    assert torch.equal(bad[same.to(DEV)], got[same.to(DEV)]) and torch.isnan(bad[0, 1:3]).all()
 
 
 def test_a_long_cache_past_32_bits():
@@ -420,6 +445,21 @@ def test_results_do_not_depend_on_the_way_the_call_is_marshalled(monkeypatch):
     native = all_calls()
     monkeypatch.setattr(attention4, "_native_module", attention4._NoNative)
     assert all(torch.equal(torch.nan_to_num(a), torch.nan_to_num(b)) for a, b in zip(native, all_calls()))
+
+
+def test_plain_calls_are_marshalled_natively():
+    c = check.make4(2, [1, 2], [20, 5], (4, 2, 64), 16)
+    native, rope = attention4._native(), wht.wht_attention_rope_table(30, 64, device=DEV)
+    pages = [c[n] for n in ("k_pages", "v_pages", "k_scales", "v_scales")]
+    rest = [c["table"], c["lengths"]]
+    for q, want, kind in ((c["q"], False, torch.Tensor), (c["q"], True, tuple), (None, False, tuple), (None, True, tuple)):
+        got = native.append4(q, c["k"], c["v"], *pages, *rest, rope, c["starts"], 0, None, None, False, True, None, None, None, want)
+        assert isinstance(got, kind)
+        again = wht.wht_attention_append4(q, c["k"], c["v"], *pages, *rest, rope, q_starts=c["starts"], want_values=want)
+        assert (again is None) if q is None and not want else isinstance(again, kind)
+    assert native.paged4(c["q"], *pages, *rest, c["starts"], None, 0, 2, 20, None, True, None, None, False, None).shape == c["q"].shape
+    assert native.rotate(c["q"], rope, None, None, False, False, None).shape == c["q"].shape
+    assert native.append4(c["q"].half(), c["k"], c["v"], *pages, *rest, rope, c["starts"], 0, None, None, False, True, None, None, None, False) is None
 
 
 def test_refusals_name_the_argument():

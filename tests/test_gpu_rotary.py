@@ -161,6 +161,20 @@ def test_shapes_broadcasts_and_second_derivatives():
         wht_rotary(x, rope, positions[:, :3], axes)
 
 
+def test_without_positions_or_axes():
+    rope = wht.wht_attention_rope_table(40, 64, device=DEV)
+    x = torch.randn(15, 3, 64, device=DEV, requires_grad=True)
+    y = wht_rotary(x, rope)
+    assert torch.equal(y.detach(), wht.wht_rotary_rotate(x.detach(), rope))
+    dy = torch.randn_like(y)
+    assert torch.equal(torch.autograd.grad(y, x, dy)[0], wht.wht_rotary_rotate(dy, rope, inverse=True))
+    dy.requires_grad_(True)
+    dx, = torch.autograd.grad(wht_rotary(x, rope), x, dy, create_graph=True)
+    assert torch.equal(torch.autograd.grad(dx, dy, x.detach())[0], y)
+    listed = wht_rotary(x, rope, torch.arange(15, dtype=torch.int32, device=DEV), axes=[0] * 32)
+    assert torch.equal(listed, y)
+
+
 def test_changed_angles_raise():
     x, positions, rope = make(4, 2, 32, 32, (8, 8), F32)
     y = wht_rotary(x.requires_grad_(True), rope, positions, wht.wht_rotary_axes((8, 8)))
