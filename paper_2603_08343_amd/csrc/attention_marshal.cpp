@@ -485,8 +485,8 @@ at::Tensor turned(const at::Tensor& x, const at::Tensor& rope, const at::Tensor&
 
 }  // namespace
 
-// autograd.wht_rotary as a node of torch's C++ autograd (autograd.WhtRotaryFunction says what it does).  Forward and gradient of a step, with what
-// torch.autograd.grad itself takes: 63 us as a Python Function, 42 here.
+// autograd.wht_rotary as a node of torch's C++ autograd (autograd.WhtRotaryFunction says what it does).  Forward and gradient of a step by
+// torch.autograd.grad, of the host's time: 38.6 us as a Python Function, 31.7 here, a product by a constant 24.0.
 // (named: the graph's nodes and torch's error messages show the type)
 struct WhtRotaryFunction : torch::autograd::Function<WhtRotaryFunction> {
     static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& rope, const std::optional<at::Tensor>& given, const std::string& axes,
