@@ -50,7 +50,7 @@ static int rotate(int D, int rotary, int count, const uint8_t *pairs, int64_t T)
     return wht_rotary_rotate(&x, &x, T, 4, D, (const float *)16, 10, rotary, 0, count > 1 ? (const int32_t *)16 : NULL, count, pairs, 0, WHT_DTYPE_BF16, NULL);
 }
 int main(void) {
-    size_t need = wht_attention4_workspace_bytes(3, 3, 8, 4, 128, 1, 128, 0, WHT_DTYPE_BF16);
+    size_t need = wht_attention4_workspace_bytes(3, 3, 8, 4, 128, 1, 1 << 20, 0, WHT_DTYPE_BF16);
     const int32_t *at = (const int32_t *)16;
     c = good;
     EXPECT(WHT_OK, append(&r, 0, 64, at, 3, WHT_DTYPE_BF16));
@@ -80,9 +80,9 @@ int main(void) {
     c.page_stride = 4096; EXPECT(WHT_ERR_MISALIGNED, append(&r, 0, 0, NULL, 1, WHT_DTYPE_BF16));            /* written pages overlap */
     EXPECT(WHT_OK, paged(0, 8, 128, 1.0f, NULL, 0)); c = good;                                              /* read ones may */
     c.scale_page_stride = 256; EXPECT(WHT_ERR_MISALIGNED, append(&r, 0, 0, NULL, 1, WHT_DTYPE_BF16)); c = good;
-    EXPECT(WHT_ERR_WORKSPACE, paged(3, 8, 128, 1.0f, NULL, 0));
-    EXPECT(WHT_ERR_WORKSPACE, paged(3, 8, 128, 1.0f, (void *)16, need - 1));
-    EXPECT(WHT_ERR_MISALIGNED, paged(3, 8, 128, 1.0f, (void *)24, need));
+    EXPECT(WHT_ERR_WORKSPACE, paged(3, 8, 1 << 20, 1.0f, NULL, 0));
+    EXPECT(WHT_ERR_WORKSPACE, paged(3, 8, 1 << 20, 1.0f, (void *)16, need - 1));
+    EXPECT(WHT_ERR_MISALIGNED, paged(3, 8, 1 << 20, 1.0f, (void *)24, need));
     EXPECT(WHT_ERR_BAD_DIM, paged(3, 7, 128, 1.0f, (void *)16, need));
     EXPECT(WHT_ERR_BAD_DIM, paged(3, 8, 128, 0.0f, (void *)16, need));
     EXPECT(WHT_ERR_BAD_DIM, paged(3, 8, 128, 3e38f, (void *)16, need));
@@ -136,6 +136,14 @@ def test_axes():
     for bad in ((), (1, 2, 3, 4, 5), (1, -1)):
         with pytest.raises(ValueError, match="sections must be"):
             wht.wht_rotary_axes(bad)
+
+
+def test_short_items_need_no_workspace():
+    """They are taken whole, in one launch; more or longer ones leave partial results."""
+    need = lambda B, heads, length, prefix=0, D=128: wht.wht_attention4_workspace_bytes(B, B, heads, heads, D, 1, length, prefix, 1)
+    assert need(4, 8, 768) == 0 and need(4, 8, 769) > 0 and need(4, 8, 700, 69) > 0
+    assert need(32, 8, 2560) == 0 and need(33, 8, 2560) > 0
+    assert need(64, 8, 2560, D=64) == 0 and need(65, 8, 100, D=64) > 0
 
 
 @pytest.mark.parametrize("x,error", [(1 << 31, ValueError), (2.5, ValueError), (None, TypeError), ("x", TypeError)])
