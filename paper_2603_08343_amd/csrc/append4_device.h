@@ -4,7 +4,6 @@
 
 namespace wht {
 
-typedef float f32x8 __attribute__((ext_vector_type(8)));
 
 // A scale byte as the number that the conversions take: they look at its exponent, and a NaN makes NaN of every code.
 __device__ __forceinline__ float scale_of(unsigned byte) { return __uint_as_float(byte >= 253 ? 0x7fc00000u : byte << 23); }

@@ -131,8 +131,12 @@ inline AttentionPlan plan_attention(int64_t T, int32_t B, int32_t q_heads, int32
 struct Slots { int64_t first; int count; };
 template <int WORKERS = kWorkers>
 WHT_HD int line_share(int total, int rows, int gang_log2) {
-    constexpr unsigned kAll = WORKERS;                              // a power of two is a shift
-    const int even = (int)((((uint64_t)(unsigned)total << gang_log2) + kAll - 1) / kAll), least = even > 1 ? (rows + 7) >> 3 : 1;
+    int even;
+    if constexpr ((WORKERS & (WORKERS - 1)) == 0) {
+        const int workers_log2 = __builtin_ctz(WORKERS) - gang_log2;
+        even = (total + (1 << workers_log2) - 1) >> workers_log2;
+    } else even = (int)((((uint64_t)(unsigned)total << gang_log2) + WORKERS - 1) / WORKERS);
+    const int least = even > 1 ? (rows + 7) >> 3 : 1;
     return even > least ? even : least;
 }
 template <int WORKERS = kWorkers>
