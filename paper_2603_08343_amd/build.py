@@ -5,6 +5,7 @@ into the extension modules _torch_marshal.so and _attention_marshal.so, in-tree.
 hipcc cross-compiles without a GPU; the extension modules take the host compiler and torch's headers.
 Run as `python -m paper_2603_08343_amd.build`.
 """
+import concurrent.futures
 import importlib.metadata
 import importlib.util
 import os
@@ -63,15 +64,16 @@ SOURCES = [SRC, HEADER] + [os.path.join(HERE, "csrc", f) for f in ("wht_device.h
 
 
 def build(verbose: bool = False, extra=()) -> str:
-    _compile(COPY_SRC, COPY_LIB, verbose, extra)
-    _compile(SRC, POISON_LIB, verbose, (*extra, "-DWHT_POISON_LDS"))
-    _compile_marshal(MARSHAL_SRC, MARSHAL_LIB, verbose)
-    _compile_marshal(ATTENTION_MARSHAL_SRC, ATTENTION_MARSHAL_LIB, verbose)
-    _compile_rules(ROUTE_SRC, ROUTE_LIB, verbose)
-    _compile_rules(ATTENTION_QUERY_SRC, ATTENTION_QUERY_LIB, verbose)
-    _compile(ATTENTION_SRC, ATTENTION_LIB, verbose, extra)
-    _compile(ATTENTION4_SRC, ATTENTION4_LIB, verbose, extra)
-    return _compile(SRC, LIB, verbose, extra)
+    jobs = [(_compile, SRC, LIB, verbose, extra), (_compile, SRC, POISON_LIB, verbose, (*extra, "-DWHT_POISON_LDS")),
+            (_compile, ATTENTION4_SRC, ATTENTION4_LIB, verbose, extra), (_compile, ATTENTION_SRC, ATTENTION_LIB, verbose, extra),
+            (_compile, COPY_SRC, COPY_LIB, verbose, extra),
+            (_compile_marshal, MARSHAL_SRC, MARSHAL_LIB, verbose), (_compile_marshal, ATTENTION_MARSHAL_SRC, ATTENTION_MARSHAL_LIB, verbose),
+            (_compile_rules, ROUTE_SRC, ROUTE_LIB, verbose), (_compile_rules, ATTENTION_QUERY_SRC, ATTENTION_QUERY_LIB, verbose)]
+    # four at a time: each takes a core and up to 2 GB
+    with concurrent.futures.ThreadPoolExecutor(4) as pool:
+        for done in [pool.submit(*job) for job in jobs]:
+            done.result()
+    return LIB
 
 
 def _compile_marshal(src: str, lib: str, verbose: bool) -> None:
