@@ -157,29 +157,40 @@ struct Angles {
     int32_t axes = 1;
     const uint8_t* pair_axes = nullptr;
 };
+// Each is false for a tensor, or axes, that the library would read past, or as what they are not.
+bool take_rope(Angles& a, const at::Tensor& r, c10::Device device) {
+    if (!Call::is_plain(r) || r.scalar_type() != at::kFloat || r.dim() != 3 || r.size(2) != 2 || !r.is_contiguous() || r.device() != device || r.numel() == 0 ||
+        r.size(1) > INT32_MAX / 2) return false;
+    a.rope = static_cast<const float*>(r.data_ptr());
+    a.rope_rows = r.size(0);
+    a.rotary = 2 * r.size(1);
+    return true;
+}
+bool take_positions(Angles& a, const at::Tensor& p, c10::Device device, int64_t T) {
+    if (!Call::is_plain(p) || p.scalar_type() != at::kInt || p.dim() < 1 || p.dim() > 2 || p.size(0) != T || !p.is_contiguous() || p.device() != device ||
+        (p.dim() == 2 && (p.size(1) < 1 || p.size(1) > WHT_ROTARY_MAX_AXES))) return false;
+    a.positions = static_cast<const int32_t*>(p.data_ptr());
+    a.axes = p.dim() == 2 ? (int32_t)p.size(1) : 1;
+    return true;
+}
+bool take_axes(Angles& a, const char* axes, int64_t n) {
+    if (n != a.rotary / 2) return false;
+    a.pair_axes = reinterpret_cast<const uint8_t*>(axes);
+    for (int64_t i = 0; i < n; ++i)
+        if (a.pair_axes[i] >= a.axes) return false;
+    return true;
+}
 void take_angles(Call& c, Angles& a, PyObject* rope, PyObject* positions, PyObject* axes, int64_t T) {
     if (!c.ok) return;
     if (rope != Py_None) {
         const at::Tensor* r = c.plain(rope);
-        if (!r || r->scalar_type() != at::kFloat || r->dim() != 3 || r->size(2) != 2 || !r->is_contiguous() || r->device() != c.device || r->numel() == 0 ||
-            r->size(1) > INT32_MAX / 2) { c.ok = false; return; }
-        a.rope = static_cast<const float*>(r->data_ptr());
-        a.rope_rows = r->size(0);
-        a.rotary = 2 * r->size(1);
+        if (!r || !take_rope(a, *r, c.device)) { c.ok = false; return; }
     }
     if (positions != Py_None) {
         const at::Tensor* p = c.plain(positions);
-        if (!p || p->scalar_type() != at::kInt || p->dim() < 1 || p->dim() > 2 || p->size(0) != T || !p->is_contiguous() || p->device() != c.device ||
-            (p->dim() == 2 && (p->size(1) < 1 || p->size(1) > WHT_ROTARY_MAX_AXES))) { c.ok = false; return; }
-        a.positions = static_cast<const int32_t*>(p->data_ptr());
-        a.axes = p->dim() == 2 ? (int32_t)p->size(1) : 1;
+        if (!p || !take_positions(a, *p, c.device, T)) { c.ok = false; return; }
     }
-    if (axes != Py_None) {
-        if (!PyBytes_CheckExact(axes) || PyBytes_GET_SIZE(axes) != a.rotary / 2) { c.ok = false; return; }
-        a.pair_axes = reinterpret_cast<const uint8_t*>(PyBytes_AS_STRING(axes));
-        for (int64_t i = 0; i < a.rotary / 2; ++i)
-            if (a.pair_axes[i] >= a.axes) { c.ok = false; return; }
-    }
+    if (axes != Py_None && (!PyBytes_CheckExact(axes) || !take_axes(a, PyBytes_AS_STRING(axes), PyBytes_GET_SIZE(axes)))) c.ok = false;
 }
 
 // A Python int in [least, most]; `ok` is false for anything else.
@@ -458,9 +469,13 @@ PyObject* rotate(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 
 struct Declined {};                     // the library refused the call: rotary.py's code says why
 
-// The rotation of x [..., heads, head_dim], by a table and positions that were looked over; nothing where a plain call does not do it.
+// The rotation of x [..., heads, head_dim]; nothing where a plain call does not do it.  The table and the positions are looked over each time: of a backward pass
+// they are what a graph's hooks for saved tensors made of them.
 at::Tensor turned(const at::Tensor& x, const at::Tensor& rope, const at::Tensor& positions, const std::string& axes, bool interleaved, bool inverse) {
     const int64_t D = x.size(-1), heads = x.size(-2), T = x.numel() / (heads * D), step = 16 / (int64_t)x.element_size();
+    Angles a;
+    if (!take_rope(a, rope, x.device()) || (positions.defined() && !take_positions(a, positions, x.device(), T)) ||
+        (!axes.empty() && !take_axes(a, axes.data(), (int64_t)axes.size()))) return {};
     at::Tensor rows = x.reshape({T, heads, D});
     if (rows.stride(2) != 1 || rows.stride(1) % step != 0 || rows.stride(0) % step != 0 || rows.stride(1) < D || ((uintptr_t)rows.data_ptr() & 15u) != 0)
         rows = rows.clone(at::MemoryFormat::Contiguous);            // strides that the library does not take
@@ -476,10 +491,8 @@ at::Tensor turned(const at::Tensor& x, const at::Tensor& rope, const at::Tensor&
         PyGILState_Release(gil);
         if (!found) return {};
     }
-    const int rc = lib_rotate(&in, &out, T, (int32_t)heads, (int32_t)D, static_cast<const float*>(rope.data_ptr()), rope.size(0), (int32_t)(2 * rope.size(1)), interleaved,
-                              positions.defined() ? static_cast<const int32_t*>(positions.data_ptr()) : nullptr,
-                              positions.defined() && positions.dim() == 2 ? (int32_t)positions.size(1) : 1,
-                              axes.empty() ? nullptr : reinterpret_cast<const uint8_t*>(axes.data()), inverse, x.scalar_type() == at::kFloat ? WHT_DTYPE_F32 : WHT_DTYPE_BF16, stream);
+    const int rc = lib_rotate(&in, &out, T, (int32_t)heads, (int32_t)D, a.rope, a.rope_rows, (int32_t)a.rotary, interleaved, a.positions, a.axes, a.pair_axes, inverse,
+                              x.scalar_type() == at::kFloat ? WHT_DTYPE_F32 : WHT_DTYPE_BF16, stream);
     return rc == WHT_OK ? y : at::Tensor();
 }
 
