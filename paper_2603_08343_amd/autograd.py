@@ -82,10 +82,12 @@ class WhtRotaryFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, rope, positions, axes, interleaved, inverse):
-        y = rotary.wht_rotary_rotate(_heads(x), rope, positions, axes, interleaved, inverse)
+        heads = _heads(x)
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)        # whole: a view made here could not be changed in place
+        rotary.wht_rotary_rotate(heads, rope, positions, axes, interleaved, inverse, out=y.view(heads.shape))
         ctx.save_for_backward(rope, positions)              # their versions are checked: angles that have changed since raise
         ctx.how = axes, interleaved, not inverse
-        return y.view(x.shape)
+        return y
 
     @staticmethod
     def backward(ctx, dy):

@@ -55,7 +55,7 @@ def _same(call, monkeypatch, label, fails=None):
         assert fails is None or general[0] is fails, general
         return
     assert fails is None, (label, general)
-    assert not isinstance(native, tuple) and len(native) == len(general), (label, native)
+    assert isinstance(native, list) and len(native) == len(general), (label, native)
     for n, g in zip(native, general):
         if isinstance(n, tuple) and isinstance(n[-1], torch.Tensor):
             assert n[:3] == g[:3] and torch.equal(n[3].nan_to_num(7.0), g[3].nan_to_num(7.0)), label
@@ -156,6 +156,13 @@ def test_modes_hooks_and_transforms(monkeypatch):
         y = wht_rotary(x.requires_grad_(True), rope, p, AXES)
         return (*torch.autograd.grad(y, x, dy, retain_graph=retain), *torch.autograd.grad(y, x, dy))
 
+    def result_changed(shape):
+        x, dy, rope, p = _tensors()
+        y = wht_rotary(x.requires_grad_(True).view(shape), rope, p.view(*shape[:-2], 3), AXES)
+        y.add_(1.0)
+        y[0].zero_()
+        return (y, y._base is None, *torch.autograd.grad(y, x, dy.view(shape)))
+
     def table_changed():
         x, dy, rope, p = _tensors()
         y = wht_rotary(x.requires_grad_(True), rope, p, AXES)
@@ -189,6 +196,8 @@ def test_modes_hooks_and_transforms(monkeypatch):
     _same(inference_saved, monkeypatch, "inference tensor to be saved")
     _same(lambda: twice(True), monkeypatch, "retained graph")
     _same(lambda: twice(False), monkeypatch, "freed graph")
+    for shape in ((T, H, D), (2, T // 2, H, D)):
+        _same(lambda: result_changed(shape), monkeypatch, f"result changed in place, {shape}")
     _same(table_changed, monkeypatch, "table changed in place")
     _same(side_stream, monkeypatch, "side stream")
     _same(lambda: torch.vmap(lambda t: wht_rotary(t, rope, p, AXES))(torch.stack((x, x))), monkeypatch, "vmap")
