@@ -107,7 +107,7 @@ def wht_rotary(x, rope, positions=None, axes=None, interleaved=False):
     Neither the table nor the positions have a gradient.  Plain calls go to the extension module's node of torch's C++ autograd
     (csrc/attention_marshal.cpp), the others, and everything under a compiler's trace, to WhtRotaryFunction.
 
-    A capture into a graph is refused for a leaf whose gradient a living graph from outside the capture gathers: the backward pass would wait for that
+    A capture into a graph that records a gradient is refused for a leaf whose gradient a living graph from outside the capture gathers: the backward pass would wait for that
     graph's stream, which is not captured, and torch ends the process over it."""
     if positions is not None and x.dim() != 3:
         lead = positions.shape[:x.dim() - 2]

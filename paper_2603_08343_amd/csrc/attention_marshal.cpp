@@ -580,11 +580,11 @@ PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
-// leaf_elsewhere(x): whether x's gradient is gathered on another stream than the current one, by a graph that lives.
+// leaf_elsewhere(x): whether a call would record a gradient for x that a living graph gathers on another stream than the current one.
 PyObject* leaf_elsewhere(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
     if (!expect(nargs, 1)) return nullptr;
-    if (!THPVariable_Check(args[0])) Py_RETURN_FALSE;
+    if (!THPVariable_Check(args[0]) || !at::GradMode::is_enabled()) Py_RETURN_FALSE;
     const at::Tensor& x = THPVariable_Unpack(args[0]);
     if (!x.is_cuda() || !x.requires_grad() || !x.is_leaf()) Py_RETURN_FALSE;
     const auto node = torch::autograd::impl::try_get_grad_accumulator(x);

@@ -246,3 +246,24 @@ def test_compiled_autograd_of_a_graph_built_eagerly():
     with compiled_autograd._enable(torch.compile(backend="eager")):
         y.backward(dy)
     assert torch.equal(x.grad, want)
+
+
+@pytest.mark.parametrize("without", [torch.no_grad, torch.inference_mode])
+def test_a_capture_without_a_gradient_takes_any_leaf(without):
+    """Of a leaf that a living graph holds a capture is refused where it records a gradient; without one there is nothing to wait for."""
+    x, _, rope, p = _tensors()
+    x.requires_grad_(True)
+    alive = wht_rotary(x, rope, p, AXES)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with without():
+            y = wht_rotary(x, rope, p, AXES)
+        with pytest.raises(RuntimeError, match="let go of that graph"):
+            wht_rotary(x, rope, p, AXES)
+    for _ in range(3):
+        with torch.no_grad():
+            x.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, wht.wht_rotary_rotate(x.detach(), rope, p, AXES))
+    assert alive.requires_grad and not y.requires_grad
