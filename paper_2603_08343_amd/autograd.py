@@ -103,12 +103,15 @@ def _heads(x):
 
 
 def wht_rotary(x, rope, positions=None, axes=None, interleaved=False):
-    """Differentiable rotary.wht_rotary_rotate; x: [..., heads, head_dim] bfloat16|float32 on the GPU, positions int32 [...] or [..., axes].
+    """Differentiable rotary.wht_rotary_rotate; x: [..., heads, head_dim] bfloat16|float32 on the GPU, positions int32 [...] or [..., axes]
+    (None: token s of x [..., tokens, heads, head_dim] has position s, in each batch of tokens from 0 on).
     Neither the table nor the positions have a gradient.  Plain calls go to the extension module's node of torch's C++ autograd
     (csrc/attention_marshal.cpp), the others, and everything under a compiler's trace, to WhtRotaryFunction.
 
     A capture into a graph that records a gradient is refused for a leaf whose gradient a living graph from outside the capture gathers: the backward pass would wait for that
     graph's stream, which is not captured, and torch ends the process over it."""
+    if positions is None and x.dim() > 3 and x.shape[:-3].numel() != 1:
+        positions = torch.arange(x.shape[-3], dtype=torch.int32, device=x.device).expand(x.shape[:-2])
     if positions is not None and x.dim() != 3:
         lead = positions.shape[:x.dim() - 2]
         if lead != x.shape[:-2]:

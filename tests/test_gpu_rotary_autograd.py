@@ -267,3 +267,24 @@ def test_a_capture_without_a_gradient_takes_any_leaf(without):
         torch.cuda.synchronize()
         assert torch.equal(y, wht.wht_rotary_rotate(x.detach(), rope, p, AXES))
     assert alive.requires_grad and not y.requires_grad
+
+
+@pytest.mark.parametrize("lead", [(1,), (3,), (2, 2), (0,), (1, 4)], ids=str)
+def test_without_positions_tokens_count_within_their_batch(lead, monkeypatch):
+    """x [..., tokens, heads, head_dim]: each batch begins at 0, and a table of as many rows as it has tokens is long enough."""
+    n = 10
+    rope = wht.wht_attention_rope_table(n, 32)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x, dy = (torch.empty(*lead, n, H, D, device="cuda").normal_(generator=g) for _ in range(2))
+    want = [torch.stack([wht.wht_rotary_rotate(t, rope, inverse=back) for t in u.reshape(-1, n, H, D)]).view(u.shape) if u.numel() else u
+            for u, back in ((x, False), (dy, True))]
+
+    def call():
+        t = x.clone().requires_grad_(True)
+        y = wht_rotary(t, rope)
+        dx, = torch.autograd.grad(y, t, dy)
+        assert torch.equal(y, want[0]) and torch.equal(dx, want[1]) and not torch.isnan(y).any()
+        return y, dx
+
+    call()
+    _same(call, monkeypatch, f"no positions, {lead}")
