@@ -82,6 +82,7 @@ class WhtRotaryFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, rope, positions, axes, interleaved, inverse):
+        axes = rotary._axis_bytes(axes)                     # as they are now: the backward pass needs the same
         heads = _heads(x)
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)        # whole: a view made here could not be changed in place
         rotary.wht_rotary_rotate(heads, rope, positions, axes, interleaved, inverse, out=y.view(heads.shape))

@@ -3,6 +3,8 @@
 Argument marshalling only, as in `attention`; a call on the current stream first goes to the extension module.  `autograd.wht_rotary` is
 the same with a gradient.
 """
+import operator
+
 from . import attention4
 from .attention import Rows, _empty, device_dummy
 from .binding import DTYPE_BF16, DTYPE_F32, _DeviceGuard, _stream_handle, _torch
@@ -36,14 +38,21 @@ def wht_rotary_axes(sections, cyclic=False) -> bytes:
     return bytes(out)
 
 
-def _axes(axes, rotary, count):
-    """The bytes that the library reads: one for each pair, below `count`."""
-    if axes is None:
-        return None
+def _axis_bytes(axes):
+    """axes as bytes, number by number: bytes() of a number is so many zeros, of an array its memory."""
+    if axes is None or type(axes) is bytes:
+        return axes
     try:
-        axes = bytes(axes)
+        return bytes([operator.index(a) for a in axes])
     except (TypeError, ValueError):
         raise TypeError("axes must be the axis of each pair: bytes, or small whole numbers") from None
+
+
+def _axes(axes, rotary, count):
+    """The bytes that the library reads: one for each pair, below `count`."""
+    axes = _axis_bytes(axes)
+    if axes is None:
+        return None
     if len(axes) != rotary // 2:
         raise ValueError(f"axes must have one number for each of the {rotary // 2} pairs, got {len(axes)}")
     if axes and max(axes) >= count:

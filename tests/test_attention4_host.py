@@ -5,12 +5,13 @@ import os
 import re
 import subprocess
 
+import numpy as np
 import pytest
 import torch
 
 import attention4_check as check
 import paper_2603_08343_amd as wht
-from paper_2603_08343_amd import attention4, build
+from paper_2603_08343_amd import attention4, build, rotary
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -181,3 +182,20 @@ def test_the_definition_by_hand():
     e0[0, 3] = 4.0
     h = check.transform(e0, 4)                                       # one large element becomes 32 of the same size
     assert torch.equal(h.abs(), torch.ones_like(h)) and torch.equal(check.transform(h, 8), e0)
+
+
+def test_axes_are_taken_number_by_number():
+    """bytes() of an array is its memory, of a number so many zeros."""
+    want = bytes([0, 1, 2, 1, 0, 2, 2, 1])
+    for kind in (bytes, bytearray, list, tuple, iter, memoryview, lambda a: np.array(list(a)), lambda a: np.array(list(a), dtype=np.int16),
+                 lambda a: np.array(list(a), dtype=np.uint8)[::1], lambda a: torch.tensor(list(a)), lambda a: torch.tensor(list(a), dtype=torch.int8)):
+        assert rotary._axes(kind(want), 16, 3) == want
+    assert rotary._axes(None, 16, 3) is None
+    for bad in (8, True, "01210221", [0.0] * 8, [300] * 8, [-1] * 8, np.zeros(8), torch.zeros(8), [None] * 8):
+        with pytest.raises(TypeError, match="axes must be the axis of each pair"):
+            rotary._axes(bad, 16, 3)
+    for bad in (np.zeros(4, np.int16), np.zeros(2, np.int32), [0] * 7):
+        with pytest.raises(ValueError, match="one number for each of the 8 pairs"):
+            rotary._axes(bad, 16, 3)
+    with pytest.raises(ValueError, match="below 2"):
+        rotary._axes(np.array(list(want)), 16, 2)

@@ -1,6 +1,7 @@
 """autograd.wht_rotary as a node of torch's C++ autograd (csrc/attention_marshal.cpp) against the Python Function that it stands for: values bit for
 bit, and the same answer -- a result or an error -- under every mode that looks into an autograd function, and for whatever a graph's hooks
 make of the table and the positions that it saved."""
+import numpy as np
 import pytest
 import torch
 
@@ -288,3 +289,19 @@ def test_without_positions_tokens_count_within_their_batch(lead, monkeypatch):
 
     call()
     _same(call, monkeypatch, f"no positions, {lead}")
+
+
+@pytest.mark.parametrize("kind", [list, iter, lambda a: np.array(list(a), dtype=np.int16), torch.tensor], ids=["list", "iterator", "array", "tensor"])
+def test_axes_of_any_kind_are_those_of_the_call(kind):
+    """The backward pass turns back by the axes that the call had, whatever became of them."""
+    x, dy, rope, p = _tensors()
+    want = wht.wht_rotary_rotate(x, rope, p, AXES), wht.wht_rotary_rotate(dy, rope, p, AXES, inverse=True)
+    axes = kind(list(AXES))
+    y = wht_rotary(x.requires_grad_(True), rope, p, axes)
+    if hasattr(axes, "__setitem__"):
+        axes[3] = 1
+    assert torch.equal(y, want[0]) and torch.equal(torch.autograd.grad(y, x, dy)[0], want[1])
+    c = [t.cuda() for t in (torch.zeros(2, 1, 16, 32, dtype=torch.uint8), torch.zeros(2, 1, 16, 2, dtype=torch.uint8))]
+    table, lengths, k = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda"), torch.randn(1, 1, D, device="cuda")
+    q = [wht.wht_attention_append4(k, k, k, c[0], c[0].clone(), c[1], c[1].clone(), table, lengths, rope, positions=p[:1], axes=a) for a in (AXES, kind(list(AXES)))]
+    assert torch.equal(*q)
