@@ -125,7 +125,7 @@ def ensure_built(verbose: bool = False) -> str:
     elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_MARSHAL_LIB) for f in (ATTENTION_MARSHAL_SRC, ATTENTION_HEADER, *ATTENTION4_HEADERS, HEADER)):
         raise RuntimeError(f"{ATTENTION_MARSHAL_LIB} is older than its source: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_QUERY_LIB)
-             for f in (ATTENTION_QUERY_SRC, os.path.join(HERE, "csrc", "attention_plan.h"), ATTENTION_HEADER, HEADER)):
+             for f in (ATTENTION_QUERY_SRC, *(os.path.join(HERE, "csrc", f) for f in ("attention_plan.h", "attention4_plan.h")), ATTENTION_HEADER, *ATTENTION4_HEADERS, HEADER)):
         raise RuntimeError(f"{ATTENTION_QUERY_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")
     elif any(os.path.getmtime(f) > os.path.getmtime(ATTENTION_LIB) for f in ATTENTION_SOURCES):
         raise RuntimeError(f"{ATTENTION_LIB} is older than its sources: run `python -m paper_2603_08343_amd.build`")

@@ -62,8 +62,6 @@ __device__ __forceinline__ void load_terms(const unsigned char* p, bool there, b
 //
 // A lane's scores are of row lane % 16, keys 4 (lane / 16) + i of either half of the block, and its weights the second product's operand as they stand.
 
-constexpr int kSmallTile = 16;
-
 template <class T, int D, int TILES>
 struct Few4 {
     static constexpr int kElements = D / 4;                         // of a row, that a lane holds

@@ -6,6 +6,10 @@
 
 namespace wht {
 
+// The few-rows kernel takes a sequence's rows of a key head as one or two tiles of 16; pages of 8 tokens have kernels for two alone.
+constexpr int kSmallTile = 16;
+constexpr int tiles4(int page_size, int own_cap) { return page_size < kSmallTile || own_cap > kSmallTile ? 2 : 1; }
+
 // The few-rows kernel's workgroups, of four workers: three on a compute unit where a worker's registers allow it, else two.  Heads of 128 need more of
 // them for the rows they sum up, and have more to do between two loads.  Two / three, in us: 48 sequences of 2 to 5 new tokens and up to 6000 of their own at
 // 16 x 96 77 / 71; 256 of up to 8192 at 32 and 8 x 128 204 / 212, one of 65001 22.3 / 25.7.

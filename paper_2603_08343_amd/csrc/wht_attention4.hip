@@ -147,7 +147,7 @@ static int paged4(const wht_attention_rows_t* q, const wht_attention_rows_t* out
     a.splits = p.own_splits; a.rows_cap = p.own_cap;
     a.part = reinterpret_cast<float*>(ws + p.own_at); a.sums = reinterpret_cast<float*>(ws + p.own_sums_at);
     a.cum = reinterpret_cast<int*>(ws + p.cum_at);
-    const bool two_tiles = a.page_shift < 4 || p.own_cap > kSmallTile;
+    const bool two_tiles = tiles4(c->page_size, p.own_cap) == 2;
     const int workgroups = workgroups4(dtype == WHT_DTYPE_F32, c->head_dim, two_tiles ? 2 : 1, front_blocks > 0);
     const int64_t each = die_blocks(T, b->B, a.G, max_q, (int64_t)c->heads * a.splits), own_blocks = p.own_few ? workgroups : (each + 1) * kDies;
     if (front_blocks + own_blocks > kMostWorkgroups) return WHT_ERR_BAD_DIM;

@@ -12,6 +12,7 @@ import torch
 import attention4_check as check
 import paper_2603_08343_amd as wht
 from paper_2603_08343_amd import attention4, build, rotary
+from test_host_sanitizers import CSRC, SAN, _run
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -199,3 +200,19 @@ def test_axes_are_taken_number_by_number():
             rotary._axes(bad, 16, 3)
     with pytest.raises(ValueError, match="below 2"):
         rotary._axes(np.array(list(want)), 16, 2)
+
+
+def test_selftest_under_sanitizers(tmp_path):
+    exe = str(tmp_path / "attention4_san")
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", *SAN, "-o", exe, os.path.join(CSRC, "attention4_selftest.cpp")], check=True)
+    assert "attention4_selftest: ok" in _run(exe)
+
+
+@pytest.mark.parametrize("source", ["attention4_plan.h", *build.ATTENTION4_HEADERS])
+def test_older_rules_are_refused(source, monkeypatch):
+    source = os.path.join(build.HERE, "csrc", source)
+    real = os.path.getmtime
+    build.ensure_built()
+    monkeypatch.setattr(os.path, "getmtime", lambda f: real(source) - 1.0 if f == build.ATTENTION_QUERY_LIB else max(real(f), real(source)) if f.endswith(".so") else real(f))
+    with pytest.raises(RuntimeError, match="attention_query.so is older than its source"):
+        build.ensure_built()

@@ -1,0 +1,209 @@
+"""Attention over the cache in 4 bits on each of the ways that a call can take (attention4_plan.h), at sizes where a worker has many blocks: codes on their way two blocks
+ahead, shares that go on to the next head and sequence, lists of pages that are read more than once.  What a case is there for is asked of the library's own rules.
+Results against the definition in 64 bits (attention4_check); places that no token has written hold bytes of 255: NaN."""
+import math
+import random
+import zlib
+
+import pytest
+import torch
+
+import attention4_check as check
+import attention4_routes as routes
+import attention_check
+
+B16, F32 = torch.bfloat16, torch.float32
+
+
+def _ragged(B, most, seed):
+    r = random.Random(seed)
+    return [0, 1, most] + [r.randint(0, most) for _ in range(B - 3)]
+
+
+def _queries(B, most, seed):
+    r = random.Random(seed)
+    return [0, most] + [r.randint(1, most) for _ in range(B - 2)]
+
+
+# name: (queries, lengths, heads, page, prefix, order, table's width or None, what the call has to take; numbers but 0 and 1: at least)
+CASES = {
+    # the line: through a sequence, to the next head, the next sequence; more than 64 sequences; a wave a joined row
+    "line_64": ([1] * 100, _ragged(100, 1300, 5), (32, 16, 64), 16, 0, "head", None, {"front": 0, "whole": 0, "gang": 0, "tiles": 1, "share": 8, "join_waves": 1}),
+    "line_96": ([1] * 90, _ragged(90, 1300, 6), (12, 12, 96), 32, 0, "head", None, {"front": 0, "gang": 0, "tiles": 1, "share": 5, "join_waves": 4}),
+    "line_128": ([1] * 64, _ragged(64, 2200, 7), (32, 8, 128), 64, 0, "head", None, {"front": 0, "gang": 0, "tiles": 1, "share": 8}),
+    "line_gang_96": ([1] * 80, _ragged(80, 1700, 8), (12, 12, 96), 16, 0, "token", None, {"gang": 1, "tiles": 1, "share": 8}),
+    "line_gang_128": ([1] * 70, _ragged(70, 2000, 9), (16, 8, 128), 128, 0, "token", None, {"gang": 1, "tiles": 1, "share": 8}),
+    "line_behind_prefix": ([1] * 100, _ragged(100, 1100, 10), (16, 8, 64), 16, 100, "head", None, {"front": 0, "own_few": 1, "gang": 0, "share": 5}),
+    "line_pages_of_8": ([1] * 100, _ragged(100, 2500, 11), (16, 16, 64), 8, 0, "head", None, {"tiles": 2, "share": 17}),           # 64 pages are 16 blocks
+    "line_gang_pages_of_8": ([1] * 70, _ragged(70, 1700, 12), (12, 12, 96), 8, 0, "token", None, {"gang": 1, "tiles": 2, "share": 8}),
+    "line_pages_of_16_long": ([1] * 50, _ragged(50, 10500, 13), (16, 16, 64), 16, 0, "head", None, {"tiles": 1, "share": 33}),     # 64 pages are 32 blocks
+    "line_drafts": (_queries(70, 4, 14), _ragged(70, 1800, 14), (32, 8, 128), 16, 0, "head", None, {"tiles": 1, "own_cap": 16, "share": 5}),
+    "line_drafts_two_tiles": (_queries(120, 4, 15), _ragged(120, 1800, 15), (20, 4, 64), 16, 0, "head", None, {"tiles": 2, "own_cap": 20, "share": 5}),
+    "line_drafts_96": (_queries(60, 5, 16), _ragged(60, 1600, 16), (16, 16, 96), 32, 0, "head", None, {"tiles": 1, "share": 5}),
+    "line_drafts_gang": (_queries(60, 3, 17), _ragged(60, 1600, 17), (16, 16, 96), 16, 0, "token", None, {"gang": 1, "share": 5}),
+    "line_drafts_pages_of_8": (_queries(70, 4, 18), _ragged(70, 1900, 18), (16, 8, 64), 8, 0, "head", None, {"tiles": 2, "share": 5}),
+    # a sequence's rows of a key head by a workgroup
+    "whole_128": ([1] * 32, _ragged(32, 2500, 19), (32, 8, 128), 16, 0, "head", None, {"whole": 1, "tiles": 1, "share": 8}),
+    "whole_pages_of_8": ([1] * 16, _ragged(16, 2560, 20), (16, 16, 64), 8, 0, "token", None, {"whole": 1, "tiles": 2, "share": 10}),
+    "whole_drafts": (_queries(40, 5, 21), _ragged(40, 1700, 21), (20, 4, 64), 16, 0, "head", None, {"whole": 1, "tiles": 2, "share": 5}),
+    "whole_behind_prefix": (_queries(16, 3, 22), _ragged(16, 800, 22), (16, 8, 96), 16, 700, "token", None, {"whole": 1, "front": 0, "share": 5}),
+    # the prefix apart: the rows of all sequences are one more item on the line
+    "front_few": ([1] * 4, [0, 1, 33, 300], (8, 8, 64), 16, 30011, "head", None, {"front": 1, "front_few": 1, "share": 3}),
+    "front_few_drafts": ([2, 1, 3, 1], [2, 9, 65, 300], (16, 8, 128), 16, 20203, "head", None, {"front": 1, "front_few": 1, "share": 3}),
+    "front_few_gang": ([1] * 4, [0, 1, 33, 300], (12, 12, 96), 8, 14003, "token", None, {"front": 1, "front_few": 1, "gang": 1, "share": 3}),
+    # ... tiles of the many-rows kernel, beside the line
+    "front_tiles": ([1] * 40, _ragged(40, 2500, 23), (32, 8, 128), 16, 1703, "head", None, {"front": 1, "front_few": 0, "share": 5, "front_splits": 2}),
+    "front_tiles_drafts": (_queries(44, 3, 24), _ragged(44, 4000, 24), (8, 2, 128), 32, 1703, "head", None, {"front": 1, "front_few": 0, "share": 3, "front_splits": 2}),
+    "front_tiles_gang": ([1] * 50, _ragged(50, 1300, 25), (12, 12, 96), 16, 300, "token", None, {"front": 1, "front_few": 0, "gang": 1, "share": 5}),
+    "front_tiles_pages_of_8": ([1] * 70, _ragged(70, 1500, 26), (16, 8, 64), 8, 250, "head", None, {"front": 1, "front_few": 0, "front_splits": 1, "share": 5}),
+    # codes past the caches, by what the table can hold
+    "past_64": ([1] * 60, _ragged(60, 1500, 27), (16, 16, 64), 16, 0, "head", 512, {"past": 1, "tiles": 1, "share": 5}),
+    "past_128": ([1] * 30, _ragged(30, 3500, 28), (8, 8, 128), 16, 40, "head", 1024, {"past": 1, "tiles": 1, "share": 5}),
+    "past_drafts": (_queries(20, 4, 29), _ragged(20, 2600, 29), (16, 8, 128), 64, 0, "head", 128, {"past": 1, "tiles": 1, "share": 3}),
+    "past_drafts_two_tiles": (_queries(40, 4, 30), _ragged(40, 1800, 30), (40, 8, 64), 32, 0, "head", 512, {"past": 1, "tiles": 2, "share": 3}),
+    "past_beside_tiles": ([1] * 40, _ragged(40, 3000, 31), (16, 4, 128), 16, 1100, "head", 1024, {"past": 1, "front": 1, "front_few": 0, "share": 3}),
+    # a share of more pages than the many-rows kernel lists at a time: of the prefix, of a prefix and the sequence's own
+    "pages_listed_twice": ([5], [5], (512, 64, 64), 8, 17003, "head", None, {"own_few": 0, "own_splits": 4}),
+    "pages_listed_twice_own": ([7], [4500], (1000, 200, 64), 8, 701, "head", None, {"own_few": 0, "own_splits": 1}),
+}
+OLD = 120                                                            # pages that any sequence may have tokens in
+
+
+def _seed(name):
+    return zlib.crc32(name.encode()) % 1000
+
+
+def make(name, dtype, device):
+    """Sequences share their older pages; the last page of each, and all of the third one's, are its own."""
+    queries, lengths, heads, page, prefix, order, width, _ = CASES[name]
+    lengths = [max(n, q) for n, q in zip(lengths, queries)]
+    Hq, Hkv, D = heads
+    g = torch.Generator().manual_seed(_seed(name))
+    own, front = [-(-n // page) for n in lengths], -(-prefix // page)
+    alone = [n if b == 2 else min(n, 1) for b, n in enumerate(own)]
+    total = front + sum(alone) + OLD + 3
+    perm = torch.randperm(total, generator=g).to(torch.int32)
+    table = torch.full((len(queries), width or max([1, *own])), -1, dtype=torch.int32)
+    at, old = front, perm[front + sum(alone):front + sum(alone) + OLD]
+    for b, n in enumerate(own):
+        table[b, :n - alone[b]] = old[torch.randint(0, OLD, (n - alone[b],), generator=g)]
+        table[b, n - alone[b]:n] = perm[at:at + alone[b]]
+        at += alone[b]
+    T = sum(queries)
+    c = {"q": torch.randn(T, Hq, D, generator=g).to(dtype), "table": table, "lengths": torch.tensor(lengths, dtype=torch.int32),
+         "starts": torch.tensor([0] + queries).cumsum(0).to(torch.int32), "prefix_table": perm[:front].clone()}
+    used = torch.zeros(total, page, dtype=torch.bool)
+    for row, n, q in [(c["prefix_table"], prefix, 1), *zip(table, lengths, queries)]:
+        i = torch.arange(n if q else 0)
+        used[row.long()[i // page], i % page] = True
+    back = {"head": lambda t: t, "token": lambda t: t.transpose(1, 2).contiguous().transpose(1, 2)}[order]
+    for n in ("k", "v"):
+        codes = torch.randint(0, 256, (total, Hkv, page, D // 2), generator=g, dtype=torch.uint8)
+        scales = torch.randint(122, 128, (total, Hkv, page, D // 32), generator=g, dtype=torch.uint8)
+        for t in (codes, scales):
+            t[(~used)[:, None].expand(-1, Hkv, -1)] = 255
+        c[n + "_pages"], c[n + "_scales"] = back(codes), back(scales)
+    c = {n: t.to(device) for n, t in c.items()}
+    for n in ("k_pages", "v_pages", "k_scales", "v_scales"):         # a copy to the GPU keeps the order in memory only of dense tensors
+        assert order == "head" or c[n].transpose(1, 2).is_contiguous()
+    return {**c, "prefix": prefix, "page": page, "max_q": max([1, *queries]), "max_length": None if width else max([0, *lengths])}
+
+
+def takes(name, c, **more):
+    r, want = routes.route(c, max_length=c["max_length"], **more), CASES[name][-1]
+    f32 = c["q"].dtype == F32
+    for key, value in want.items():
+        if key == "gang":
+            assert (r["gang_log2"] > 0) == bool(value), (key, r)
+        elif key == "past":
+            assert r["past"] == (0 if f32 else 1) and not r["gang_log2"], (key, r)
+        elif value > 1 and key in ("share", "front_splits"):
+            assert r[key] >= value, (key, r)
+        else:
+            assert r[key] == value, (key, r)
+    if name.startswith("pages_listed_twice"):
+        steps = -(-(-(-c["prefix"] // 64) - (-int(c["lengths"][0]) // 64)) // r["own_splits"])
+        assert steps * 64 // c["page"] > 508, steps
+    if r["own_few"]:
+        blocks = {"line_pages_of_8": 16, "line_pages_of_16_long": 32, "whole_pages_of_8": 16 if f32 else 0}.get(name, 0)
+        assert r["share"] > blocks, r                                # a list of 64 pages and more
+
+
+@pytest.mark.parametrize("dtype", [B16, F32], ids=str)
+@pytest.mark.parametrize("name", CASES)
+def test_cases_take_the_ways_that_they_name(name, dtype):
+    c = make(name, dtype, "cpu")
+    takes(name, c)
+    takes(name, c, rows=c["q"].shape[0] + 3)
+
+
+def _paged(c, transformed, **more):
+    import paper_2603_08343_amd as wht
+    return wht.wht_attention_paged4(c["q"], c["k_pages"], c["v_pages"], c["k_scales"], c["v_scales"], c["table"], c["lengths"], transform=transformed,
+                                    want_lse=True, **{"q_starts": c["starts"], "prefix_table": c["prefix_table"], "prefix_length": c["prefix"], "max_q": c["max_q"],
+                                                      "max_length": c["max_length"], **more})
+
+
+def _transformed(name, dtype):
+    return (_seed(name) % 2 == 0) == (dtype == B16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [B16, F32], ids=str)
+@pytest.mark.parametrize("name", CASES)
+def test_every_way(name, dtype):
+    c = make(name, dtype, "cuda:0")
+    takes(name, c)
+    transformed = _transformed(name, dtype)
+    single = c["max_q"] == 1 and c["q"].shape[0] == c["lengths"].shape[0]
+    out, lse = _paged(c, transformed, **({"q_starts": None} if single else {}))
+    want, want_lse, tol, tol_lse = check.attend4(c, transformed)
+    attention_check.same(out, want, tol, "out")
+    attention_check.same(lse, want_lse, tol_lse, "lse")
+    for _ in range(2):
+        again = _paged(c, transformed)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [B16, F32], ids=str)
+@pytest.mark.parametrize("name", CASES)
+def test_every_way_around_bad_pages_and_blocks_that_are_no_numbers(name, dtype):
+    """Numbers that name no page, in the prefix (its last one, in part, as well) and in the sequences' own; blocks of NaN that all rows of a sequence see, and ones
+    that only some do; rows of NaN behind the sequences' own."""
+    c = make(name, dtype, "cuda:0")
+    r, pages, page, Hkv = random.Random(_seed(name)), c["k_pages"].shape[0], c["page"], c["k_pages"].shape[1]
+    lengths, starts, table, front = c["lengths"].tolist(), c["starts"].tolist(), c["table"].cpu(), c["prefix_table"]
+    for b, n in enumerate(lengths):
+        if b == 2 and n:                                             # its pages are its own: in the middle of a share
+            for side, p in (("v", n // 2), ("k", n // 3)):
+                c[side + "_scales"][int(table[b, p // page]), r.randrange(Hkv), p % page, r.randrange(2)] = 253
+        elif n > 2 and starts[b + 1] - starts[b] > 1 and (n - 2) // page == (n - 1) // page:
+            for side, byte in (("v", 253), ("k", 254)):              # the newest but one
+                c[side + "_scales"][int(table[b, (n - 2) // page]), r.randrange(Hkv), (n - 2) % page, r.randrange(2)] = byte
+    for i in {0, len(front) // 3, len(front) - 1} if len(front) else ():
+        front[i] = r.choice([-1, pages, 1 << 30, -(1 << 31)])
+    for b, n in enumerate(lengths):
+        if n and b % 3 == 0:
+            c["table"][b, r.randrange(-(-n // page))] = r.choice([-7, pages, (1 << 31) - 1])
+    transformed, T = not _transformed(name, dtype), c["q"].shape[0]
+    want, want_lse, tol, tol_lse = check.attend4(c, transformed)
+    takes(name, c, rows=T + 3)
+    q = torch.cat((c["q"], torch.full_like(c["q"][:1], math.nan).expand(3, -1, -1)))
+    out, lse = _paged({**c, "q": q}, transformed)
+    attention_check.same(out[:T], want, tol, "out")
+    attention_check.same(lse[:T], want_lse, tol_lse, "lse")
+    assert (out[T:] == 0).all() and (lse[T:] == -math.inf).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", [n for n, c in CASES.items() if max(c[0]) > 2])
+@pytest.mark.parametrize("dtype", [B16, F32], ids=str)
+def test_every_way_with_a_max_q_that_is_too_small(name, dtype):
+    c = make(name, dtype, "cuda:0")
+    limit, transformed = c["max_q"] - 1, _transformed(name, dtype)
+    out, lse = _paged(c, transformed, max_q=limit)
+    want, want_lse, tol, tol_lse = check.attend4(c, transformed, limit=limit)
+    attention_check.same(out, want, tol, "out")
+    attention_check.same(lse, want_lse, tol_lse, "lse")
+
