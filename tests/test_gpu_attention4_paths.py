@@ -207,3 +207,32 @@ def test_every_way_with_a_max_q_that_is_too_small(name, dtype):
     attention_check.same(out, want, tol, "out")
     attention_check.same(lse, want_lse, tol_lse, "lse")
 
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [B16, F32], ids=str)
+@pytest.mark.parametrize("transformed", [False, True])
+@pytest.mark.parametrize("byte", [251, 252, 253])
+@pytest.mark.parametrize("queries,lengths,heads", [([1, 1], [1, 1], (4, 2, 64)), ([1, 1], [90, 33], (4, 2, 96)), ([3, 2], [40, 2], (20, 4, 128)), ([40, 9], [40, 100], (4, 2, 96)),
+                                                   ([35, 1], [300, 1], (8, 2, 128))], ids=str)
+def test_the_largest_scales(queries, lengths, heads, byte, transformed, dtype):
+    """2^125 is a scale as any other, 253 is no number, of codes of zero as well.  Only the first key has codes other than zero -- with the transform one in 32, so that
+    its block's sums are its own size -- and the base of a row's weights is no less than its score: sums stay below 6 * 2^125, and every result is finite."""
+    c = check.make4(2, queries, lengths, heads, 16, dtype=dtype)
+    D = heads[2]
+    first = [(int(c["table"][b, 0]), h) for b in range(2) for h in range(heads[1])]
+    c["v_pages"].zero_()
+    c["v_scales"].fill_(byte)
+    for i, (g, h) in enumerate(first):
+        codes = torch.zeros(D, dtype=torch.uint8)
+        if transformed:
+            codes[torch.arange(0, D, 32) + (5 * i + 3) % 32] = torch.tensor([7, 15, 13, 1], dtype=torch.uint8)[:D // 32]
+        else:
+            codes[:] = (torch.arange(D) * 7 + i) % 16
+        c["v_pages"][g, h, 0] = (codes[0::2] | codes[1::2] << 4).to(c["v_pages"].device)
+    out, lse, tol, tol_lse = check.attend4(c, transformed)
+    assert torch.isnan(out).all() if byte == 253 else torch.isfinite(out).all() and float(out.abs().max()) >= 2.0 ** (byte - 127 - 40)       # the first key has some weight
+    for max_length in (max(lengths), 1 << 20):
+        got, got_lse = _paged(c, transformed, max_length=max_length)
+        attention_check.same(got, out, tol, "out")
+        attention_check.same(got_lse, lse, tol_lse, "lse")
