@@ -65,7 +65,7 @@ inline int check_cache4(const wht_attention_cache4_t* c, const wht_attention_bat
     if (dtype != WHT_DTYPE_F32 && dtype != WHT_DTYPE_BF16) return WHT_ERR_BAD_DTYPE;
     if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return WHT_ERR_BAD_DIM;
     if (c->page_size < WHT_ATTENTION_MIN_PAGE || c->page_size > WHT_ATTENTION_MAX_PAGE || (c->page_size & (c->page_size - 1)) != 0) return WHT_ERR_BAD_DIM;
-    if (c->heads < 1 || c->heads > 1024 || c->pages < 1 || b->B < 0 || b->width < 1 || b->table_stride < 0) return WHT_ERR_BAD_DIM;
+    if (c->heads < 1 || c->heads > 1024 || c->pages < 1 || b->B < 0 || b->B > 1 << 30 || b->width < 1 || b->table_stride < 0) return WHT_ERR_BAD_DIM;
     if ((int64_t)b->width * c->page_size > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
     // a page's number is multiplied by its stride in bytes (both 32 bits), and a row's place in its page stays below 31
     auto fits = [&](int64_t page, int64_t head, int64_t token, int row) {

@@ -101,7 +101,21 @@ static void plans() {
     CHECK(tiles4(8, 1) == 2 && tiles4(16, 16) == 1 && tiles4(16, 17) == 2 && tiles4(1024, kFewRows) == 2);
 }
 
+// The search for a token's sequence adds to their number in 32 bits.
+static void sequences() {
+    const wht_attention_rows_t r{(void*)16, 1024, 128}, none{nullptr, 0, 0};
+    for (int32_t B : {0, 3, 1 << 30, (1 << 30) + 1, INT32_MAX - 62, INT32_MAX}) {
+        const wht_attention_batch_t b{(const int32_t*)16, (const int32_t*)16, (const int32_t*)16, 1, B, 1};
+        const wht_attention_cache_t c{(void*)16, (void*)16, 8 * 16 * 128, 16 * 128, 128, 4, 8, 16, 128};
+        const wht_attention_cache4_t c4{(void*)16, (void*)16, (uint8_t*)16, (uint8_t*)16, 8 * 16 * 64, 16 * 64, 64, 8 * 16 * 4, 16 * 4, 4, 4, 8, 16, 128};
+        const int want = B <= 1 << 30 ? WHT_OK : WHT_ERR_BAD_DIM;
+        CHECK(check_append(&none, &r, &r, &none, 3, 0, &c, &b, nullptr, 0, 0, 0, WHT_DTYPE_BF16) == want);
+        CHECK(check_append4(&none, &r, &r, &none, &none, &none, 3, 0, &c4, &b, nullptr, 0, 0, 0, nullptr, 1, nullptr, WHT_DTYPE_BF16) == want);
+    }
+}
+
 int main() {
+    sequences();
     std::mt19937 rng(5);
     for (int i = 0; i < 300; ++i) {
         std::vector<int> blocks(rng() % 200);

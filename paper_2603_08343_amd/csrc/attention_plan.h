@@ -194,7 +194,7 @@ inline int check_cache(const wht_attention_cache_t* c, const wht_attention_batch
     const int size = dtype == WHT_DTYPE_F32 ? 4 : 2;
     if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return WHT_ERR_BAD_DIM;
     if (c->page_size < WHT_ATTENTION_MIN_PAGE || c->page_size > WHT_ATTENTION_MAX_PAGE || (c->page_size & (c->page_size - 1)) != 0) return WHT_ERR_BAD_DIM;
-    if (c->heads < 1 || c->heads > 1024 || c->pages < 1 || b->B < 0 || b->width < 1 || b->table_stride < 0) return WHT_ERR_BAD_DIM;
+    if (c->heads < 1 || c->heads > 1024 || c->pages < 1 || b->B < 0 || b->B > 1 << 30 || b->width < 1 || b->table_stride < 0) return WHT_ERR_BAD_DIM;
     if ((int64_t)b->width * c->page_size > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
     // the kernels multiply a page's number by its stride in bytes (both 32 bits) and keep a row's place in its page in 31
     if (c->page_stride < 0 || c->page_stride * size >= (int64_t)1 << 32 || c->token_stride < c->head_dim ||
