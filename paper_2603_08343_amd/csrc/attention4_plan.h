@@ -69,7 +69,7 @@ inline int check_cache4(const wht_attention_cache4_t* c, const wht_attention_bat
     if ((int64_t)b->width * c->page_size > (int64_t)1 << 30) return WHT_ERR_BAD_DIM;
     // a page's number is multiplied by its stride in bytes (both 32 bits), and a row's place in its page stays below 31
     auto fits = [&](int64_t page, int64_t head, int64_t token, int row) {
-        return page >= 0 && page < (int64_t)1 << 32 && token >= row && token < (int64_t)1 << 31 && (c->page_size - 1) * token < (int64_t)1 << 31 && head >= 0 && head < (int64_t)1 << 31;
+        return page >= 0 && page < (int64_t)1 << 32 && token >= row && token < (int64_t)1 << 31 && (c->page_size - 1) * token < (int64_t)1 << 31 && head >= 0;
     };
     if (!fits(c->page_stride, c->head_stride, c->token_stride, c->head_dim / 2) ||
         !fits(c->scale_page_stride, c->scale_head_stride, c->scale_token_stride, c->head_dim / 32)) return WHT_ERR_BAD_DIM;

@@ -114,8 +114,20 @@ static void sequences() {
     }
 }
 
+// Heads may be any distance apart: their offsets are 64 bits.
+static void heads_apart() {
+    const wht_attention_rows_t r{(void*)16, 1024, 128};
+    const wht_attention_batch_t b{(const int32_t*)16, (const int32_t*)16, nullptr, 1, 3, 1};
+    for (int64_t head : {(int64_t)16, (int64_t)4 * 16 * 64, (int64_t)1 << 31, (int64_t)70000 << 16, (int64_t)1 << 60}) {
+        const wht_attention_cache4_t c{(void*)16, (void*)16, (uint8_t*)16, (uint8_t*)16, 16 * 64, head, 64, 16 * 4, head / 16, 4, 4, 8, 16, 128};
+        CHECK(check_paged4(&r, &r, nullptr, 3, 8, &c, &b, nullptr, 0, 1, 16, 1.0f, WHT_DTYPE_BF16) == WHT_OK);
+        CHECK(check_append4(&r, &r, &r, &r, &r, &r, 3, 8, &c, &b, nullptr, 0, 0, 0, nullptr, 1, nullptr, WHT_DTYPE_BF16) == (head == 16 ? WHT_ERR_MISALIGNED : WHT_OK));
+    }
+}
+
 int main() {
     sequences();
+    heads_apart();
     std::mt19937 rng(5);
     for (int i = 0; i < 300; ++i) {
         std::vector<int> blocks(rng() % 200);

@@ -274,7 +274,7 @@ const char* wht_attention4_status_string(int status) {
     switch (status) {
     case WHT_OK:             return "ok";
     case WHT_ERR_NULL_PTR:   return "a required pointer is NULL";
-    case WHT_ERR_BAD_DIM:    return "a size is not taken: head_dim 64, 96 or 128; page_size a power of two, 8 to 1024; q_heads a multiple of heads, at most 1024; rotary a multiple of 16 up to head_dim; up to 4 axes, and every pair's among them; counts not negative and below 2^30; strides of at least a row, a page below 4 GiB, a head below 2 GiB; scale > 0 and at most 2.3e38";
+    case WHT_ERR_BAD_DIM:    return "a size is not taken: head_dim 64, 96 or 128; page_size a power of two, 8 to 1024; q_heads a multiple of heads, at most 1024; rotary a multiple of 16 up to head_dim; up to 4 axes, and every pair's among them; counts not negative and below 2^30; strides of at least a row, a page below 4 GiB; scale > 0 and at most 2.3e38";
     case WHT_ERR_BAD_DTYPE:  return "dtype must be WHT_DTYPE_F32 or WHT_DTYPE_BF16";
     case WHT_ERR_MISALIGNED: return "tensors and codes must be 16-byte aligned and their strides 16-byte steps of at least a row (heads: below 2 GiB); what is written must not overlap itself";
     case WHT_ERR_WORKSPACE:  return "workspace is NULL or smaller than wht_attention4_workspace_bytes";

@@ -236,3 +236,30 @@ def test_the_largest_scales(queries, lengths, heads, byte, transformed, dtype):
         got, got_lse = _paged(c, transformed, max_length=max_length)
         attention_check.same(got, out, tol, "out")
         attention_check.same(got_lse, lse, tol_lse, "lse")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("queries,max_length", [([3], 100), ([3], 1 << 20), ([60], 100)], ids=str)
+def test_heads_far_apart(queries, max_length):
+    """Heads outside pages, more than 4 GiB apart: offsets in 64 bits, of the append as well."""
+    pages, page, D, device = 70000, 1024, 128, "cuda:0"
+    small = check.make4(1, queries, [100], (4, 2, D), page)
+    wide = dict(small)
+    for n in ("k_pages", "v_pages", "k_scales", "v_scales"):         # 9.2 GB of codes a side
+        t = torch.zeros(2, pages, page, small[n].shape[3], dtype=torch.uint8, device=device).transpose(0, 1)
+        t[pages - 1] = small[n][int(small["table"][0, 0])]
+        wide[n] = t
+    wide["table"] = torch.full_like(small["table"], pages - 1)
+    assert wide["k_pages"].stride(1) > 1 << 32
+    got = _paged(wide, True, max_length=max_length)
+    want, want_lse, tol, tol_lse = check.attend4(small, True)
+    attention_check.same(got[0], want, tol, "out")
+    attention_check.same(got[1], want_lse, tol_lse, "lse")
+    import paper_2603_08343_amd as wht
+    rope = wht.wht_attention_rope_table(100, D)
+    for c in (small, wide):
+        c["q_out"] = wht.wht_attention_append4(c["q"], c["k"], c["v"], c["k_pages"], c["v_pages"], c["k_scales"], c["v_scales"], c["table"], c["lengths"], rope,
+                                               q_starts=c["starts"])
+    assert torch.equal(small["q_out"], wide["q_out"])
+    for n in ("k_pages", "v_pages", "k_scales", "v_scales"):
+        assert torch.equal(small[n][int(small["table"][0, 0])], wide[n][pages - 1]), n
