@@ -24,8 +24,9 @@
  * magnitude than 6 * 2^125 becomes that).  A block with an element that is not finite is stored as not a number, codes 0.
  *
  * Attention.  As wht_attention_paged, with the numbers that the cache stands for; where `transform`, q is q' as the append gives it and
- * out = H (sum_t p_t v'_t) / 8, in float32, rounded once.  Results have the type of q.  The sums in front of the division by the sum of the weights
- * are float32: of values with scales up to 2^80 (byte 207) they are finite for any number of keys, of larger ones they may not be.
+ * out = H (sum_t p_t v'_t) / 8, in float32, rounded once.  Results have the type of q.  For bfloat16 queries the weights are rounded to bfloat16 for the product with
+ * v' (their sum is not); float32 queries and their weights enter the products with 24 bits (what is below 2^-109 of them as a multiple of 2^-133).  The sums in front of
+ * the division by the sum of the weights are float32: of values with scales up to 2^80 (byte 207) they are finite for any number of keys, of larger ones they may not be.
  *
  * What is said there of page numbers, lengths, places, positions and padding rows holds here too; the value of a token that a
  * row does not see takes no part in that row, whatever its bytes.  So do the conventions of its entry points.
@@ -66,7 +67,10 @@ int wht_attention_append4(const wht_attention_rows_t *q, const wht_attention_row
                           const float *rope, int64_t rope_rows, int32_t rotary, int32_t interleaved, int64_t position,
                           const int32_t *positions, int32_t axes, const uint8_t *pair_axes, int32_t transform, int32_t dtype, void *stream);
 
-/* Bytes of device scratch that wht_attention_paged4 needs for such a call (see wht_attention_workspace_bytes). */
+/*
+ * Bytes of device scratch that wht_attention_paged4 needs for such a call (see wht_attention_workspace_bytes).  More sequences, rows or keys may need fewer: 8 sequences of
+ * up to 2560 keys at 8 key heads need megabytes, 32 of them, which are taken whole, none.  A workspace for calls of several sizes has the largest of their needs.
+ */
 size_t wht_attention4_workspace_bytes(int64_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t head_dim,
                                       int32_t max_q, int64_t max_length, int64_t prefix_length, int32_t dtype);
 

@@ -208,6 +208,7 @@ def wht_attention_paged4(q, k_pages, v_pages, k_scales, v_scales, table, lengths
       max_q: at least the largest number of new tokens of a sequence (None: 1 without q_starts, T with them)
       max_length: at least the largest of lengths (None: what the table can hold); goes into how the work is split
       scale: None for 1 / sqrt(head_dim);  transform: as the tokens were appended
+      workspace: wht_attention4_workspace_bytes of this call's sizes (None: allocated); a larger batch may need fewer
     For serving: nothing here is recorded for a backward pass.
     """
     if stream is None:

@@ -2,7 +2,9 @@
 //
 // A code times its scale has three significant bits, which bfloat16 holds exactly: keys and values become bfloat16 on their way to the matrix
 // cores, one instruction for two of them, scale included, and the products are those of attention_device.h.  Float32 queries and weights enter the same
-// products as the sum of three bfloat16 terms (24 bits), three products each, where products in float32 would take sixteen times the cycles.
+// products as the sum of three bfloat16 terms (24 bits), three products each, where products in float32 would take sixteen times the cycles.  The weights of bfloat16
+// queries are rounded to bfloat16, as with the 16-bit cache: a second term would double the products with the values.  Their sum is not rounded.  Results of 65001 keys are
+// off by 0.0017 of their norm then, of prompts and behind a long prefix by 0.0022, where the rounding of the results alone is 0.0016 to 0.0017.
 #pragma once
 #include "append4_device.h"
 

@@ -12,11 +12,15 @@ constexpr int tiles4(int page_size, int own_cap) { return page_size < kSmallTile
 
 // The few-rows kernel's workgroups, of four workers: three on a compute unit where a worker's registers allow it, else two.  Heads of 128 need more of
 // them for the rows they sum up, and have more to do between two loads.  Two / three, in us: 48 sequences of 2 to 5 new tokens and up to 6000 of their own at
-// 16 x 96 77 / 71; 256 of up to 8192 at 32 and 8 x 128 204 / 212, one of 65001 22.3 / 25.7.
+// 16 x 96 77 / 71, at 12 x 64 52 / 44; single new tokens, 128 sequences of up to 4096 at 12 x 64 71 / 60, 256 of up to 2048 at 16 and 4 x 64 36 / 32, 64 of up to 8192
+// 32 / 27, 200 of up to 2048 at 16 x 96 110 / 103; but one of 65001 at 16 and 4 x 64 15.1 / 16.4, at 12 and 4 x 96 18.7 / 20.6, where the join has half as many pieces again;
+// 256 of up to 8192 at 32 and 8 x 128 204 / 212, one of 65001 22.3 / 25.7.
 constexpr int workgroups4(bool f32, int head_dim, int tiles, bool front) { return f32 || head_dim == 128 || tiles == 2 || front ? 512 : 768; }
 constexpr int kMostWorkers4 = 4 * 768;
 
-// Whether the few-rows kernel reads a call's own codes past the caches: by the rule of streams() in attention_plan.h, with a row's bytes here.
+// Whether the few-rows kernel reads a call's own codes past the caches: as streams() in attention_plan.h, with a row's bytes here.  Three caches read in turn, kept / past,
+// in us: 1 sequence at 32 and 8 x 128, 80 MB 24.3 / 25.1, 96 MB 27.4 / 27.5, 112 MB 31.8 / 30.1, 256 MB 55.9 / 49.8; 16 of them 22.6 / 23.3, 26.9 / 27.0, 31.6 / 29.3,
+// 56.5 / 49.9; 128 at 12 x 64 24.7 / 27.7, 33.2 / 33.1, 36.0 / 33.9, 68.3 / 63.5; 16 at 16 and 4 x 64 25.4 / 28.0, 29.6 / 30.6, 36.2 / 34.2, 65.6 / 61.5.
 inline bool streams4(int32_t B, int32_t heads, int32_t head_dim, int64_t max_length, int64_t prefix, int32_t gang_log2) {
     return gang_log2 == 0 && ((double)B * max_length + prefix) * heads * (head_dim / 2 + head_dim / 32) * 2 >= 96e6;
 }

@@ -62,7 +62,7 @@ __device__ __forceinline__ void angles(const Turning& t, const Places& p, int fi
 }
 
 // ------------------------------------------------------------------------------------------------
-// Every element is read and written once: memory.  32760 tokens of 40 heads of 128 in bfloat16 (671 MB): 124 us, 5.4 TB/s; 773 tokens of 20 heads of 64: 4.1 us,
+// Every element is read and written once: memory.  32760 tokens of 40 heads of 128 in bfloat16 (671 MB): 127 us, 5.3 TB/s; 773 tokens of 20 heads of 64: 4.1 us,
 // most of it the chain position -> angle (4.8 with the elements read behind it).  A wave takes a token, so that positions and angles are looked up once; a
 // lane takes the same pair of 16-byte vectors, which hold each other's partners, of every heads_at_once-th head.
 
