@@ -160,9 +160,21 @@ def test_every_way(name, dtype):
     want, want_lse, tol, tol_lse = check.attend4(c, transformed)
     attention_check.same(out, want, tol, "out")
     attention_check.same(lse, want_lse, tol_lse, "lse")
-    for _ in range(2):
-        again = _paged(c, transformed)
-        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    again = _paged(c, transformed)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+    # into the middle of larger buffers, by a workspace of no numbers: nothing in front of them, between or behind
+    import paper_2603_08343_amd as wht
+    (T, Hq, D), (Hkv, page) = c["q"].shape, c["k_pages"].shape[1:3]
+    most = c["table"].shape[1] * page if c["max_length"] is None else c["max_length"]
+    need = wht.wht_attention4_workspace_bytes(T, c["lengths"].shape[0], Hq, Hkv, D, c["max_q"], most, c["prefix"], 0 if dtype == F32 else 1)
+    workspace, outs, lses = (torch.full(n, x, dtype=t, device="cuda:0") for n, x, t in (((need + 1024,), 255, torch.uint8), ((T + 2, Hq + 1, D + 16), 7.0, dtype), ((T + 2, Hq), 7.0, F32)))
+    at = outs[1:-1, :Hq, 8:D + 8]
+    _paged(c, transformed, out=at, lse=lses[1:-1], workspace=workspace[512:512 + need])
+    assert torch.equal(at, out) and torch.equal(lses[1:-1], lse)
+    at.fill_(7.0)
+    lses[1:-1].fill_(7.0)
+    assert (outs == 7.0).all() and (lses == 7.0).all() and (workspace[:512] == 255).all() and (workspace[512 + need:] == 255).all()
 
 
 @pytest.mark.gpu
