@@ -305,3 +305,17 @@ def test_axes_of_any_kind_are_those_of_the_call(kind):
     table, lengths, k = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda"), torch.randn(1, 1, D, device="cuda")
     q = [wht.wht_attention_append4(k, k, k, c[0], c[0].clone(), c[1], c[1].clone(), table, lengths, rope, positions=p[:1], axes=a) for a in (AXES, kind(list(AXES)))]
     assert torch.equal(*q)
+
+
+def test_under_a_compilers_trace():
+    """The trace breaks at the call, which goes to the Python Function: values and gradients of the eager call."""
+    x, dy, rope, p = _tensors()
+    x.requires_grad_(True)
+    y = wht_rotary(x * 2, rope, p, AXES) + 1
+    want, = torch.autograd.grad(y, x, dy)
+    compiled = torch.compile(lambda t: wht_rotary(t * 2, rope, p, AXES) + 1, backend="eager")
+    for _ in range(2):
+        z = compiled(x)
+        assert torch.equal(z, y) and torch.equal(torch.autograd.grad(z, x, dy)[0], want)
+    batch = torch.compile(lambda t: wht_rotary(t, rope), backend="eager")
+    assert torch.equal(batch(x.detach().view(2, 12, H, D)), wht_rotary(x.detach().view(2, 12, H, D), rope))
